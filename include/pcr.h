@@ -465,6 +465,102 @@ int pcr_enable_stage_timing(pcr_record* rec, int on);
 int pcr_last_stage_ms(pcr_record* rec, float* stage_ms);
 int pcr_stage_ms_history(pcr_record* rec, double* sum_ms, uint32_t* launches, uint32_t* calls);
 
+/* ---- from a decoded record to a transformer that trains on it ----
+ *
+ * Pictures to patch rows with positions, positions into queries and keys, and the loss of a student that sees a low scan group
+ * against the top logits of a teacher that saw the full one (Section 4: the fidelity is the training's to choose; both
+ * pictures of a batch come from one record by pcr_decode_batch and pcr_upgrade_batch).
+ *
+ * All of these take the device's number, work on device memory, enqueue on hip_stream and allocate nothing.  `dtype` is the type of
+ * what is read and written; sums, statistics and angles are held in 32 bits or more and every result is rounded once.
+ * Strides and offsets count elements and may pass 32 bits.  An element lies at a multiple of its size; wider alignment is used where
+ * it is there and not needed.  Results do not depend on anything but the inputs (no order of atomics).  Errors: PCR_E_ARG null
+ * pointers, unknown types; PCR_E_RANGE sizes outside what is said; PCR_E_DEVICE; with any of them nothing is enqueued. */
+enum { PCR_FLOAT = 0, PCR_HALF = 1, PCR_BFLOAT = 2 };          /* IEEE 32 bits, IEEE 16 bits, the upper 16 bits of IEEE 32 */
+
+/* Normalised patch rows of n pictures at their own sizes, one picture's after another's, with their positions.
+ *   d_pixels    uint8, picture i at d_pixels[d_offset[i]] as H x W x channels (the layout of pcr_decode_batch)
+ *   d_shape     int32 [n][2]: H, W (both at least 1; less counts as a picture without rows)
+ *   d_offset    int64 [n]: where picture i begins.  A picture that does not lie in the first pixel_bytes bytes is not read (its rows are 0)
+ *   d_first     int64 [n + 1], ascending: the first row of picture i; [n]: rows there are.  Picture i has
+ *               ceil(H / (patch merge)) merge x ceil(W / (patch merge)) merge rows
+ *   rows        rows that d_out and d_positions have (host): no more are written
+ *   patch       side, 1 .. 128; merge: 1 .. 16.  Rows go through windows of merge x merge patches, window after window and, in a window,
+ *               line after line (merge 1: line after line through the picture), so that patches that are merged later are neighbours
+ *   frames      pictures of a clip: the first position is i mod frames (1: zero for single pictures)
+ *   channels    1 or 3; mean, inv_std (host): as in pcr_crop_resize_batch
+ *   d_out       dtype [rows][channels][patch][patch]: (pixel / 255 - mean) inv_std, 0 outside the picture; rows that belong to no
+ *               picture's grid are 0
+ *   d_positions int32 [3][rows], may be NULL: frame, row and column of the patch (0 for rows of no picture) */
+int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, const int32_t* d_shape, const int64_t* d_offset, const int64_t* d_first, int64_t n,
+                   int64_t rows, int patch, int merge, int frames, int channels, const float* mean, const float* inv_std, int dtype,
+                   void* d_out, int32_t* d_positions, void* hip_stream);
+
+/* Positions of several axes (time, height, width; up to 4) turned into the heads of queries and keys: pair j of a head's `pairs` is
+ * turned by d_position[d_axis[j]][batch][token] * d_frequency[j] radians, (x, y) -> (x cos - y sin, x sin + y cos).  A pair is
+ * (j, j + pairs), or (2 j, 2 j + 1) where `adjacent` is set; elements from 2 * pairs on are not turned.
+ * The angle is the product of the position and the frequency as 32-bit floats, rounded to one (2^-24 of itself off, as where a program multiplies
+ * a table of frequencies by positions); its sine and cosine are taken to 2^-22 however large it is.  Positions may be negative.
+ *   d_position  int32, or int64 where `wide` is set, with its strides;  d_frequency: float [pairs];  d_axis: int32 [pairs], 0 .. axes - 1
+ *               (another value counts as the nearest of these)
+ *   batch, tokens, dim (1 .. 512), pairs (0 .. dim / 2): the same for queries and keys
+ * pcr_heads: one of the two sides, [batch][tokens][heads][dim] with its strides, elements of a head contiguous; heads 0: left out
+ *   (pointers may be NULL).  out may be in itself with the same strides; otherwise they must not overlap.
+ *
+ * pcr_rotate_axes: the rotation alone.  inverse != 0: by minus the angle, which is its gradient (grad is not used).
+ * pcr_norm_rotate: y = rotation of x r w, r = 1 / sqrt(mean x^2 + eps) over the head; weight: dim elements of weight_dtype, NULL: ones.
+ * pcr_norm_rotate_backward: grad: the gradient of y; in: x; out: the gradient of x (it may be grad or in itself); weight_grad: float [dim],
+ *   the weight's gradient summed over batch, tokens and heads in a fixed order (NULL: not asked for; needs d_work otherwise).
+ *   d_work: pcr_norm_rotate_workspace bytes, its content is of no account before and after.
+ * No tokens: weight gradients are zeros. */
+typedef struct pcr_rotation {
+    const void* position; int64_t axis_stride, batch_stride, token_stride;
+    const float* frequency; const int32_t* axis;
+    int64_t batch, tokens;
+    int32_t wide, axes, dim, pairs, adjacent, reserved;
+} pcr_rotation;
+typedef struct pcr_heads {
+    const void* in; int64_t in_batch, in_token, in_head;
+    void* out; int64_t out_batch, out_token, out_head;
+    const void* grad; int64_t grad_batch, grad_token, grad_head;
+    const void* weight; float* weight_grad;
+    int64_t heads;
+} pcr_heads;
+int pcr_rotate_axes(int device_id, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* rotation, int inverse, int dtype, void* hip_stream);
+int pcr_norm_rotate(int device_id, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* rotation, float eps, int dtype, int weight_dtype,
+                    void* hip_stream);
+int pcr_norm_rotate_workspace(int64_t tokens, int dim, size_t* nbytes);
+int pcr_norm_rotate_backward(int device_id, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* rotation, float eps, int dtype,
+                             int weight_dtype, void* d_work, size_t work_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits, with the loss of labels beside it.  Of a row with logits z over `classes`, the teacher's kept
+ * logits t_k at classes i_k (k < top), temperature T, p = softmax of t / T over the entries with 0 <= i_k < classes and t_k > -inf:
+ *   loss = distill_part T^2 sum_k p_k (log p_k - log softmax(z / T)[i_k]) + label_part (logsumexp z - z[label])
+ * A term without entries, or with a label outside 0 .. classes - 1, is left out; a class may be kept twice.
+ *   logits       dtype [rows] with row_stride; top_index int32, or int64 where index_wide is set, [rows][top]; top_logits top_dtype [rows][top]
+ *   labels       int64 [rows] or NULL (label_part then has no effect);  classes 1 .. 2^31 - 1, top 1 .. 1024, temperature > 0
+ * pcr_distill_forward: loss float [rows]; sums float [rows][2]: logsumexp(z / T), and logsumexp(z) where there are labels and label_part is not 0
+ *   (else 0), which the backward pass takes.  (Where all logits of a row are so far from 0 that 32 bits hold no logarithm beside them -- the type's
+ *   lowest value throughout -- the sums hold none, and the backward pass misses it; pcr_distill_step of many rows does not.)
+ * pcr_distill_backward: row_grad float [rows]: the gradient of each row's loss; out: dtype, the gradient of the logits with out_stride.  A row
+ *   whose row_grad is 0, or that has no term, is zeros whatever its logits hold.
+ * pcr_distill_step: loss[n] = row_weight[n] * the row's loss and the gradient of the sum of these, in one pass; a row of weight 0, or without a
+ *   term, is left out: its loss is 0 and its gradient zeros, whatever its logits hold.
+ * out may be the logits themselves with the same stride (then nothing else keeps them); otherwise they must not overlap.
+ * d_work: pcr_distill_workspace bytes (0 for many rows), for forward and step. */
+typedef struct pcr_distill {
+    const void* logits; int64_t row_stride;
+    const void* top_index; const void* top_logits; const int64_t* labels;
+    int64_t rows, classes;
+    int32_t top, dtype, top_dtype, index_wide;
+    float temperature, distill_part, label_part, reserved;
+} pcr_distill;
+int pcr_distill_workspace(int64_t rows, int64_t classes, size_t* nbytes);
+int pcr_distill_forward(int device_id, const pcr_distill* d, float* loss, float* sums, void* d_work, size_t work_bytes, void* hip_stream);
+int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums, const float* row_grad, void* out, int64_t out_stride, void* hip_stream);
+int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weight, float* loss, void* out, int64_t out_stride, void* d_work,
+                     size_t work_bytes, void* hip_stream);
+
 /* Diagnostics: the rate (10^9 instructions per second, whole device) at which `waves_per_cu` (1..32)
  * resident wavefronts per compute unit issue chains of dependent scalar-ALU instructions -- the kind of
  * work the wave-uniform entropy decoders consist of (Section 4.2 of the paper names the decode as the

@@ -83,6 +83,15 @@ SYMBOLS = {
     "pcr_loader_decode_crop": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, _vp, _vp, ctypes.c_size_t, ctypes.c_int, ctypes.c_int,
                                               ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_float), _vp, ctypes.c_size_t, _vp]),
     "pcr_loader_wait": (ctypes.c_int, [_vp, ctypes.c_int]),
+    "pcr_patch_rows": (ctypes.c_int, [ctypes.c_int, _vp, ctypes.c_size_t] + [_vp] * 3 + [ctypes.c_int64] * 2 + [ctypes.c_int] * 4 + [_vp, _vp, ctypes.c_int, _vp, _vp, _vp]),
+    "pcr_rotate_axes": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, ctypes.c_int, ctypes.c_int, _vp]),
+    "pcr_norm_rotate": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, ctypes.c_float, ctypes.c_int, ctypes.c_int, _vp]),
+    "pcr_norm_rotate_workspace": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "pcr_norm_rotate_backward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, ctypes.c_float, ctypes.c_int, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "pcr_distill_workspace": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)]),
+    "pcr_distill_forward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "pcr_distill_backward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp]),
+    "pcr_distill_step": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp, ctypes.c_size_t, _vp]),
     "pcr_strerror": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -289,6 +298,12 @@ class Record:
         _check(lib().pcr_crop_resize_batch(self._h, pixels.data_ptr(), crops.data_ptr(), out_h, out_w, m, sd, out.data_ptr(),
                                            out.numel() * 2, s), "pcr_crop_resize_batch")
         return out
+
+    def patch_layout(self, patch, merge=1):
+        """(shapes, offsets, first_rows, rows) of this record's pictures for patch_rows: three CUDA tensors and the number of rows."""
+        from .train import patch_layout
+        sizes = [self.image_info(i)[:3] for i in range(self.n)]
+        return patch_layout([(h, w) for w, h, _ in sizes], sizes[0][2], patch, merge, offsets=self.output_layout(), device=self.device)
 
     def msssim_batch(self, a, b, out=None, stream=None):
         """Multi-scale structural similarity of every image's pictures in two decoded batches (uint8 CUDA tensors

@@ -1,0 +1,310 @@
+// The loss of a student's logits against a teacher's top logits, with the loss of labels beside it, and its gradient.
+//
+// A row: logits z over V classes, kept teacher logits t_k at classes i_k, temperature T; p = softmax of t / T over the entries that count.
+//   L = logsumexp(z / T), L1 = logsumexp z;   loss = a T^2 sum p_k (log p_k - z_{i_k} / T + L) + b (L1 - z_label)
+//   dz_v = g (a T P exp(z_v / T - L) + b exp(z_v - L1))  +  sum over entries at v of their delta,   P = 1 (0: no entry counts),
+// with delta = -g a T p_k for a kept logit and -g b for the label: the dense part is written first and the few classes with a delta again
+// behind it, every one with the deltas of all entries at its class, in their order.
+//
+// Both sums over a row are made in one pass with a running maximum, in 32 bits, relative to it.  Bound by memory: a row is read once for the
+// loss, and read and written once for the gradient.
+#pragma once
+#include "pcr_vec.h"
+
+namespace pcr {
+
+struct DistillArgs {
+    const void* logits; const void* top_index; const void* top_logits; const int64_t* labels;
+    const float* sums_in; const float* row_grad;              // backward: saved sums; step: row_grad holds the rows' weights
+    float* loss; float* sums; void* out; float* part;
+    int64_t row_stride, out_stride, rows, V;
+    int64_t chunk; int chunks;                                 // classes of a workgroup's share of a row, shares of a row
+    int K, top_dtype, wide, two;
+    float T, inv_T, a, b;
+};
+
+constexpr float kLog2e = 1.4426950408889634074f;
+enum { kLoss = 0, kGrad = 1, kStep = 2 };
+
+template <int TEAM> __device__ __forceinline__ void team_sync() {
+    if (TEAM > 64) __syncthreads();
+    else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+// Maximum and sum over a team, the same bits in all of it.  `lds`: a float for every wavefront of the team.
+template <int TEAM, bool MAX> __device__ __forceinline__ float team_join(float v, float* lds) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const float o = __shfl_xor(v, d);
+        v = MAX ? fmaxf(v, o) : v + o;
+    }
+    if (TEAM == 64) return v;
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[wave] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < TEAM / 64; w++) v = MAX ? fmaxf(v, lds[w]) : v + lds[w];
+    return v;
+}
+
+__device__ __forceinline__ float top_logit(const DistillArgs& A, int64_t at) {
+    if (A.top_dtype == 0) return ((const float*)A.top_logits)[at];
+    if (A.top_dtype == 1) return (float)((const _Float16*)A.top_logits)[at];
+    return (float)((const __bf16*)A.top_logits)[at];
+}
+// The class of an entry, -1 if it does not count.
+__device__ __forceinline__ int64_t top_class(const DistillArgs& A, int64_t at) {
+    const int64_t v = A.wide ? ((const int64_t*)A.top_index)[at] : (int64_t)((const int32_t*)A.top_index)[at];
+    return v >= 0 && v < A.V ? v : -1;
+}
+
+// exp((x - m) / T) and exp(x - m) of a run, added to s and s1, with m raised first where the run holds more.
+struct RowSums { float m, s, s1; };
+template <int N, bool TWO> __device__ __forceinline__ void add_run(RowSums& R, const float (&x)[N], float c) {
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < N; i++) most = fmaxf(most, x[i]);
+    if (most > R.m) {
+        R.s *= __builtin_amdgcn_exp2f((R.m - most) * c);
+        if (TWO) R.s1 *= __builtin_amdgcn_exp2f((R.m - most) * kLog2e);
+        R.m = most;
+    }
+    const float m = R.m == -INFINITY ? 0.f : R.m;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        R.s += __builtin_amdgcn_exp2f((x[i] - m) * c);
+        if (TWO) R.s1 += __builtin_amdgcn_exp2f((x[i] - m) * kLog2e);
+    }
+}
+
+// Sums over z[0 .. count) by a team: elements in front of the first 16-byte boundary, whole runs, the rest.
+template <typename T, int TEAM, bool TWO> __device__ __forceinline__ RowSums row_sums(const T* z, int64_t count, float c, int tid) {
+    constexpr int N = 16 / sizeof(T), U = 4;
+    RowSums R = {-INFINITY, 0.f, 0.f};
+    const int64_t lead = min(count, (int64_t)((-(uintptr_t)z & 15) / sizeof(T)));
+    const int64_t runs = (count - lead) / N, tail = lead + runs * N;
+    if (tid < lead) { float x[1]; load_run<T, 1>(z + tid, x); add_run<1, TWO>(R, x, c); }
+    if (tail + tid < count) { float x[1]; load_run<T, 1>(z + tail + tid, x); add_run<1, TWO>(R, x, c); }
+    int64_t r = tid;
+    for (; r + (U - 1) * TEAM < runs; r += U * TEAM) {
+        float x[U][N];
+#pragma unroll
+        for (int u = 0; u < U; u++) load_run<T, N>(z + lead + (r + u * TEAM) * N, x[u]);
+#pragma unroll
+        for (int u = 0; u < U; u++) add_run<N, TWO>(R, x[u], c);
+    }
+    for (; r < runs; r += TEAM) {
+        float x[N];
+        load_run<T, N>(z + lead + r * N, x);
+        add_run<N, TWO>(R, x, c);
+    }
+    return R;
+}
+
+__device__ __forceinline__ float scaled(float s, float m, float most, float c) { return m == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f((m - most) * c); }
+
+// The dense part of the gradient of one element.
+struct Dense { float inv_T, L, L1, ca, cb; };
+template <bool TWO> __device__ __forceinline__ float dense_of(float x, const Dense& D) {
+    float v = D.ca * __builtin_amdgcn_exp2f(__builtin_fmaf(x, D.inv_T, -D.L) * kLog2e);
+    if (TWO) v = __builtin_fmaf(D.cb, __builtin_amdgcn_exp2f((x - D.L1) * kLog2e), v);
+    return v;
+}
+template <typename T, int TEAM, bool TWO> __device__ __forceinline__ void write_dense(const T* z, T* out, int64_t count, const Dense& D, int tid) {
+    constexpr int N = 16 / sizeof(T), U = 4;
+    const int64_t lead = min(count, (int64_t)((-(uintptr_t)out & 15) / sizeof(T)));
+    const int64_t runs = (count - lead) / N, tail = lead + runs * N;
+    if (tid < lead) { float x[1]; load_run<T, 1>(z + tid, x); x[0] = dense_of<TWO>(x[0], D); store_run<T, 1>(out + tid, x); }
+    if (tail + tid < count) { float x[1]; load_run<T, 1>(z + tail + tid, x); x[0] = dense_of<TWO>(x[0], D); store_run<T, 1>(out + tail + tid, x); }
+    int64_t r = tid;
+    for (; r + (U - 1) * TEAM < runs; r += U * TEAM) {
+        float x[U][N];
+#pragma unroll
+        for (int u = 0; u < U; u++) load_run<T, N>(z + lead + (r + u * TEAM) * N, x[u]);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+#pragma unroll
+            for (int i = 0; i < N; i++) x[u][i] = dense_of<TWO>(x[u][i], D);
+            store_run<T, N>(out + lead + (r + u * TEAM) * N, x[u]);
+        }
+    }
+    for (; r < runs; r += TEAM) {
+        float x[N];
+        load_run<T, N>(z + lead + r * N, x);
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = dense_of<TWO>(x[i], D);
+        store_run<T, N>(out + lead + r * N, x);
+    }
+}
+template <typename T, int TEAM> __device__ __forceinline__ void write_zeros(T* out, int64_t count, int tid) {
+    constexpr int N = 16 / sizeof(T);
+    const int64_t lead = min(count, (int64_t)((-(uintptr_t)out & 15) / sizeof(T)));
+    const int64_t runs = (count - lead) / N, tail = lead + runs * N;
+    const float one[1] = {0.f}, none[N] = {};
+    if (tid < lead) store_run<T, 1>(out + tid, one);
+    if (tail + tid < count) store_run<T, 1>(out + tail + tid, one);
+    for (int64_t r = tid; r < runs; r += TEAM) store_run<T, N>(out + lead + r * N, none);
+}
+
+// A team of TEAM threads takes a row, or one of the shares of a row (gradient alone).  MODE: the loss and the sums, the gradient from saved sums, or both.
+template <typename T, int TEAM, bool TWO, int MODE>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs A) {
+    extern __shared__ float lds[];                             // a team's: joins [16], and of entry e: class, delta, logit
+    const int tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    const int64_t unit = (int64_t)blockIdx.x * (TEAM < 256 ? 256 / TEAM : 1) + team;
+    if (unit >= A.rows * A.chunks) return;                     // (a whole wavefront, or nobody of a workgroup that shares a row)
+    const int64_t n = unit / A.chunks;
+    const int share = (int)(unit - n * A.chunks), E = A.K + 1;
+    const int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
+    float* join = lds + team * (16 + 3 * E);
+    int* at = (int*)(join + 16);
+    float* delta = join + 16 + E;
+    float* logit = delta + E;
+    const T* z = (const T*)A.logits + n * A.row_stride;
+    T* out = MODE == kLoss ? nullptr : (T*)A.out + n * A.out_stride + v0;
+    const float g = MODE == kLoss ? 1.f : A.row_grad[n];
+
+    if (MODE != kLoss && g == 0.f) {
+        write_zeros<T, TEAM>(out, count, tid);
+        if (MODE == kStep && tid == 0) A.loss[n] = 0.f;
+        return;
+    }
+    // entries: softmax of the teacher's logits over those that count
+    float most = -INFINITY;
+    for (int k = tid; k < A.K; k += TEAM) {
+        const int64_t v = A.a != 0.f ? top_class(A, n * A.K + k) : -1;
+        const float t = v >= 0 ? top_logit(A, n * A.K + k) * A.inv_T : -INFINITY;
+        at[k] = t == -INFINITY ? -1 : (int)v;
+        delta[k] = t;
+        logit[k] = t == -INFINITY ? 0.f : (float)z[v];
+        most = fmaxf(most, t == t ? t : INFINITY);             // (of a NaN all that follows is one)
+    }
+    most = team_join<TEAM, true>(most, join);
+    float total = 0.f;
+    for (int k = tid; k < A.K; k += TEAM) if (at[k] >= 0) total += __builtin_amdgcn_exp2f((delta[k] - most) * kLog2e);
+    total = team_join<TEAM, false>(total, join);
+    const bool kept = most != -INFINITY;
+    const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
+    const bool labelled = label >= 0 && label < A.V;
+    const float zl = labelled ? (float)z[label] : 0.f;
+
+    // What the dense part is taken against: the saved sums, or (exact also where the logarithm is lost beside it) the maximum and the sum's reciprocal.
+    float L, L1, over = 1.f, over1 = 1.f;
+    if (MODE == kGrad) {
+        L = A.sums_in[2 * n]; L1 = A.sums_in[2 * n + 1];
+    } else {
+        if (MODE == kStep && !kept && !labelled) {
+            write_zeros<T, TEAM>(out, count, tid);
+            if (tid == 0) A.loss[n] = 0.f;
+            return;
+        }
+        RowSums R = row_sums<T, TEAM, TWO>(z, A.V, A.inv_T * kLog2e, tid);
+        const float m = team_join<TEAM, true>(R.m, join);
+        const float s = team_join<TEAM, false>(scaled(R.s, R.m, m, A.inv_T * kLog2e), join);
+        const float s1 = TWO ? team_join<TEAM, false>(scaled(R.s1, R.m, m, kLog2e), join) : s;
+        const float log_s = logf(s), log_s1 = TWO ? logf(s1) : log_s;
+        L = m * A.inv_T; L1 = m;
+        over = 1.f / s; over1 = 1.f / s1;
+        float sum = 0.f;
+        for (int k = tid; k < A.K; k += TEAM)
+            if (at[k] >= 0) {
+                const float t = delta[k] - most, e = __builtin_amdgcn_exp2f(t * kLog2e);
+                if (e > 0.f || t != t) sum += e * ((t - logf(total)) - ((logit[k] * A.inv_T - L) - log_s));
+            }
+        sum = team_join<TEAM, false>(sum, join);
+        if (tid == 0) {
+            float loss = kept ? A.a * A.T * A.T * (sum / total) : 0.f;
+            if (labelled) loss += A.b * (log_s1 - (zl - m));
+            A.loss[n] = g * loss;
+            if (MODE == kLoss) { A.sums[2 * n] = L + log_s; A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f; }
+        }
+    }
+    if (MODE == kLoss) return;
+    if (!kept && !labelled) {
+        write_zeros<T, TEAM>(out, count, tid);
+        return;
+    }
+    Dense D = {A.inv_T, L, L1, kept ? g * A.a * A.T * over : 0.f, labelled ? g * A.b * over1 : 0.f};
+    if (!TWO) D.ca += D.cb;
+    team_sync<TEAM>();                                         // the joins above are read
+    for (int k = tid; k < A.K; k += TEAM) delta[k] = at[k] >= 0 ? -g * A.a * A.T * (__builtin_amdgcn_exp2f((delta[k] - most) * kLog2e) / total) : 0.f;
+    if (tid == 0) { at[A.K] = labelled ? (int)label : -1; delta[A.K] = -g * A.b; logit[A.K] = zl; }
+    team_sync<TEAM>();
+    write_dense<T, TEAM, TWO>(z + v0, out, count, D, tid);
+    team_sync<TEAM>();
+    for (int e = tid; e < E; e += TEAM) {
+        const int64_t v = at[e];
+        if (v < v0 || v >= v0 + count) continue;
+        float x[1] = {dense_of<TWO>(logit[e], D)}, more = 0.f;
+        for (int k = 0; k < E; k++) more += at[k] == (int)v ? delta[k] : 0.f;
+        x[0] += more;
+        store_run<T, 1>(out + (v - v0), x);
+    }
+}
+
+// Few rows: shares of a row are summed by workgroups of their own and joined by k_distill_join, a wavefront to a row.
+template <typename T, bool TWO>
+__global__ __launch_bounds__(256) void k_distill_part(DistillArgs A) {
+    __shared__ float join[16];
+    const int64_t n = blockIdx.x / A.chunks;
+    const int share = (int)(blockIdx.x - n * A.chunks);
+    const int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
+    const float c = A.inv_T * kLog2e;
+    RowSums R = row_sums<T, 256, TWO>((const T*)A.logits + n * A.row_stride + v0, count, c, threadIdx.x);
+    const float m = team_join<256, true>(R.m, join);
+    const float s = team_join<256, false>(scaled(R.s, R.m, m, c), join);
+    const float s1 = TWO ? team_join<256, false>(scaled(R.s1, R.m, m, kLog2e), join) : 0.f;
+    if (threadIdx.x == 0) {
+        float* p = A.part + 3 * (int64_t)blockIdx.x;
+        p[0] = m; p[1] = s; p[2] = s1;
+    }
+}
+
+template <typename T, bool TWO>
+__global__ __launch_bounds__(64) void k_distill_join(DistillArgs A) {
+    const int64_t n = blockIdx.x;
+    const int lane = threadIdx.x;
+    const float c = A.inv_T * kLog2e;
+    const T* z = (const T*)A.logits + n * A.row_stride;
+    float m = -INFINITY, s = 0.f, s1 = 0.f;
+    for (int j = lane; j < A.chunks; j += 64) m = fmaxf(m, A.part[3 * (n * A.chunks + j)]);
+    m = team_join<64, true>(m, nullptr);
+    for (int j = lane; j < A.chunks; j += 64) {
+        const float* p = A.part + 3 * (n * A.chunks + j);
+        s += scaled(p[1], p[0], m, c);
+        if (TWO) s1 += scaled(p[2], p[0], m, kLog2e);
+    }
+    s = team_join<64, false>(s, nullptr);
+    const float L = m * A.inv_T, log_s = logf(s), log_s1 = TWO ? logf(team_join<64, false>(s1, nullptr)) : log_s;
+    float most = -INFINITY, total = 0.f, sum = 0.f;
+    for (int k = lane; k < A.K; k += 64) {
+        const int64_t v = A.a != 0.f ? top_class(A, n * A.K + k) : -1;
+        const float t = v >= 0 ? top_logit(A, n * A.K + k) * A.inv_T : -INFINITY;
+        most = fmaxf(most, t == t ? t : INFINITY);             // (of a NaN all that follows is one)
+    }
+    most = team_join<64, true>(most, nullptr);
+    for (int k = lane; k < A.K; k += 64) {
+        const int64_t v = A.a != 0.f ? top_class(A, n * A.K + k) : -1;
+        const float t = v >= 0 ? top_logit(A, n * A.K + k) * A.inv_T - most : -INFINITY;
+        if (v < 0 || t == -INFINITY) continue;
+        const float e = __builtin_amdgcn_exp2f(t * kLog2e);
+        total += e;
+        if (e > 0.f || t != t) sum += e * (t - (((float)z[v] * A.inv_T - L) - log_s));
+    }
+    total = team_join<64, false>(total, nullptr);
+    sum = team_join<64, false>(sum, nullptr);
+    if (lane == 0) {
+        const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
+        float loss = most != -INFINITY ? A.a * A.T * A.T * (sum / total - logf(total)) : 0.f;
+        if (label >= 0 && label < A.V) loss += A.b * (log_s1 - ((float)z[label] - m));
+        const float g = A.row_grad ? A.row_grad[n] : 1.f;
+        A.loss[n] = g == 0.f ? 0.f : g * loss;
+        A.sums[2 * n] = L + log_s; A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f;
+    }
+}
+
+}  // namespace pcr

@@ -1,0 +1,318 @@
+// C ABI of the operators behind the decode (see include/pcr.h): checks of arguments, choice of a kernel, launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/pcr.h"
+#include "pcr_axes.h"
+#include "pcr_distill.h"
+#include "pcr_patch.h"
+
+using namespace pcr;
+
+#define HIP_TRY(expr) do { if ((expr) != hipSuccess) { (void)hipGetLastError(); return PCR_E_DEVICE; } } while (0)
+
+namespace {
+
+constexpr int64_t kMaxGrid = 2147483647;
+
+int launched() { return hipGetLastError() == hipSuccess ? PCR_OK : PCR_E_DEVICE; }
+
+// The type that a dtype stands for, as an argument of f.
+template <typename F> void with_type(int dtype, F f) {
+    if (dtype == PCR_FLOAT) f(float());
+    else if (dtype == PCR_HALF) f((_Float16)0);
+    else f((__bf16)0);
+}
+
+// ---- rotation ----
+
+// Largest run of elements (at most 16 bytes) that every place of a side is a multiple of.
+int run_of(const void* p, const int64_t* strides, int count, size_t size, int most) {
+    uint64_t all = (uint64_t)(uintptr_t)p / size;
+    for (int i = 0; i < count; i++) all |= (uint64_t)strides[i];
+    int n = most;
+    while (n > 1 && all % n) n >>= 1;
+    return n;
+}
+
+int check_rotation(const pcr_heads* q, const pcr_heads* k, const pcr_rotation* R, int dtype, bool back) {
+    if (!q || !k || !R || !known_type(dtype)) return PCR_E_ARG;
+    if (R->dim < 1 || R->dim > 512 || R->pairs < 0 || R->pairs > R->dim / 2 || R->axes < 1 || R->axes > 4) return PCR_E_RANGE;
+    if (R->batch < 0 || R->tokens < 0 || R->tokens > kMaxGrid || R->batch > kMaxGrid) return PCR_E_RANGE;
+    const pcr_heads* side[2] = {q, k};
+    for (const pcr_heads* s : side) {
+        if (s->heads < 0 || s->heads > 65536) return PCR_E_RANGE;
+        if (s->heads && R->batch && R->tokens && (!s->in || !s->out || (back && !s->grad))) return PCR_E_ARG;
+    }
+    if (R->pairs && R->batch && R->tokens && (!R->position || !R->frequency || !R->axis)) return PCR_E_ARG;
+    return PCR_OK;
+}
+
+template <typename T, int N, bool ADJ, int MODE> void launch_axes(const AxesArgs& A, int groups, hipStream_t s) {
+    if constexpr (N <= 2) {
+        if (A.slots > 64) {
+            hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 4>), dim3(groups), dim3(256), 0, s, A);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 1>), dim3(groups), dim3(256), 0, s, A);
+}
+
+constexpr int kBackGroups = 1024;                              // workgroups of a gradient: each leaves one sum of the weights' gradient a side
+
+int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* R, float eps, int inverse, int dtype, int weight_dtype, int mode,
+             void* d_work, size_t work_bytes, hipStream_t s) {
+    int rc = check_rotation(q, k, R, dtype, mode == kNormBack);
+    if (rc) return rc;
+    if (mode != kRotate && !known_type(weight_dtype)) return PCR_E_ARG;
+    if (mode != kRotate && weight_dtype != PCR_FLOAT && weight_dtype != dtype) return PCR_E_ARG;
+    const pcr_heads* side[2] = {q, k};
+    const bool sums = mode == kNormBack && (q->weight_grad || k->weight_grad);
+    AxesArgs A = {};
+    A.batch_tokens = R->batch * R->tokens;
+    if (A.batch_tokens > kMaxGrid) return PCR_E_RANGE;
+    int groups = 0;
+    const size_t size = type_size(dtype);
+    int N = (int)(16 / size);
+    for (int z = 0; z < 2; z++) {
+        const pcr_heads& H = *side[z];
+        HeadSide& S = A.side[z];
+        S.in = H.in; S.grad = H.grad; S.out = H.out; S.weight = H.weight; S.heads = (int)H.heads;
+        S.in_b = H.in_batch; S.in_t = H.in_token; S.in_h = H.in_head;
+        S.out_b = H.out_batch; S.out_t = H.out_token; S.out_h = H.out_head;
+        S.grad_b = H.grad_batch; S.grad_t = H.grad_token; S.grad_h = H.grad_head;
+        if (!S.heads) continue;
+        const int64_t strides[9] = {S.in_b, S.in_t, S.in_h, S.out_b, S.out_t, S.out_h, S.grad_b, S.grad_t, S.grad_h};
+        N = std::min(N, run_of(H.in, strides, 6, size, N));
+        N = std::min(N, run_of(H.out, strides, 0, size, N));
+        if (mode == kNormBack) N = std::min(N, run_of(H.grad, strides + 6, 3, size, N));
+    }
+    while (N > 1 && (R->dim % N || (!R->adjacent && R->pairs % N))) N >>= 1;
+    A.position = R->position; A.frequency = R->frequency; A.axis = R->axis;
+    A.pos_a = R->axis_stride; A.pos_b = R->batch_stride; A.pos_t = R->token_stride;
+    A.tokens = R->tokens; A.wide = R->wide; A.axes = R->axes; A.dim = R->dim; A.pairs = R->pairs;
+    A.inverse = inverse; A.weight_float = weight_dtype == PCR_FLOAT; A.eps = eps;
+    const int turned = 2 * R->pairs;
+    A.slots = R->adjacent ? (R->dim + 2 * N - 1) / (2 * N) : R->pairs / N + (R->dim - turned + 2 * N - 1) / (2 * N);
+    A.per_wave = std::max(1, 64 / A.slots);
+    // Tokens of a workgroup: some 128 rows, as many as the table of sines holds, and no more than leave 1024 workgroups.
+    const int64_t heads = std::max<int64_t>(1, q->heads + k->heads);
+    int64_t chunk = std::max<int64_t>(1, 128 / heads);
+    if (R->pairs) chunk = std::min<int64_t>(chunk, kAxesTable / R->pairs);
+    chunk = std::max<int64_t>(1, std::min(chunk, A.batch_tokens / 1024));
+    A.chunk = (int)chunk;
+    A.chunks = (A.batch_tokens + chunk - 1) / chunk;
+    groups = (int)(mode == kNormBack ? std::min<int64_t>(A.chunks, kBackGroups) : A.chunks);
+    if (sums) {
+        size_t need = 0;
+        pcr_norm_rotate_workspace(A.batch_tokens, R->dim, &need);
+        if (A.batch_tokens && (!d_work || work_bytes < need)) return d_work ? PCR_E_RANGE : PCR_E_ARG;
+        for (int z = 0; z < 2; z++) if (side[z]->weight_grad) A.side[z].part = (float*)d_work + (size_t)z * groups * R->dim;
+    }
+    HIP_TRY(hipSetDevice(device));
+    if (q->heads + k->heads == 0) groups = 0;
+    if (groups) {
+        with_type(dtype, [&](auto t) {
+            typedef decltype(t) T;
+            auto by_mode = [&](auto n, auto adj) {
+                constexpr int M = decltype(n)::value;
+                constexpr bool ADJ = decltype(adj)::value;
+                if (mode == kRotate) launch_axes<T, M, ADJ, kRotate>(A, groups, s);
+                else if (mode == kNorm) launch_axes<T, M, ADJ, kNorm>(A, groups, s);
+                else launch_axes<T, M, ADJ, kNormBack>(A, groups, s);
+            };
+            auto by_pairs = [&](auto n) {
+                if (R->adjacent) by_mode(n, std::true_type());
+                else by_mode(n, std::false_type());
+            };
+            if (N == 8) { if constexpr (sizeof(T) == 2) by_pairs(std::integral_constant<int, 8>()); }
+            else if (N == 4) by_pairs(std::integral_constant<int, 4>());
+            else if (N == 2) by_pairs(std::integral_constant<int, 2>());
+            else by_pairs(std::integral_constant<int, 1>());
+        });
+    }
+    if (sums) {
+        WeightSums W = {};
+        for (int z = 0; z < 2; z++) { W.part[z] = A.side[z].part; W.out[z] = side[z]->weight_grad; }
+        W.parts = groups; W.dim = R->dim;
+        hipLaunchKernelGGL(k_weight_sums, dim3((R->dim + 15) / 16, 2), dim3(256), 0, s, W);
+    }
+    return launched();
+}
+
+// ---- distillation ----
+
+// Shares of a row: with few rows, as many as fill the chip with some 2048 workgroups, none below 8192 classes.
+int64_t shares_of(int64_t rows, int64_t V) {
+    if (rows <= 0 || rows >= 512) return 1;
+    return std::max<int64_t>(1, std::min<int64_t>(2048 / rows, V / 8192));
+}
+
+int check_distill(const pcr_distill* d) {
+    if (!d || !known_type(d->dtype) || !known_type(d->top_dtype)) return PCR_E_ARG;
+    if (d->rows < 0 || d->rows > kMaxGrid || d->classes < 1 || d->classes > kMaxGrid || d->top < 1 || d->top > 1024) return PCR_E_RANGE;
+    if (!(d->temperature > 0.f) || !isfinite(d->temperature) || !isfinite(d->distill_part) || !isfinite(d->label_part)) return PCR_E_RANGE;
+    if (d->rows && (!d->logits || !d->top_index || !d->top_logits)) return PCR_E_ARG;
+    return PCR_OK;
+}
+
+DistillArgs distill_args(const pcr_distill* d) {
+    DistillArgs A = {};
+    A.logits = d->logits; A.top_index = d->top_index; A.top_logits = d->top_logits; A.labels = d->labels;
+    A.row_stride = d->row_stride; A.rows = d->rows; A.V = d->classes; A.chunk = d->classes; A.chunks = 1;
+    A.K = d->top; A.top_dtype = d->top_dtype; A.wide = d->index_wide;
+    A.T = d->temperature; A.inv_T = 1.f / d->temperature; A.a = d->distill_part; A.b = d->label_part;
+    A.two = d->labels && d->label_part != 0.f;
+    return A;
+}
+
+template <typename T, int TEAM, int MODE> void launch_team(const DistillArgs& A, hipStream_t s) {
+    const int teams = TEAM < 256 ? 256 / TEAM : 1, threads = TEAM < 256 ? 256 : TEAM;
+    const unsigned groups = (unsigned)((A.rows * A.chunks + teams - 1) / teams);
+    const size_t lds = (size_t)teams * (16 + 3 * (A.K + 1)) * sizeof(float);
+    if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(threads), lds, s, A);
+    else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(threads), lds, s, A);
+}
+template <int MODE> void launch_distill(const DistillArgs& A, int dtype, hipStream_t s) {
+    with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        const int64_t bytes = std::min(A.chunk, A.V) * (int64_t)sizeof(T);
+        if (bytes <= 8192) launch_team<T, 64, MODE>(A, s);
+        else if (bytes <= 65536) launch_team<T, 256, MODE>(A, s);
+        else launch_team<T, 1024, MODE>(A, s);
+    });
+}
+// The sums of rows in shares, and the loss.
+void launch_shares(DistillArgs A, int64_t shares, int dtype, hipStream_t s) {
+    A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
+    A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+    with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        const unsigned groups = (unsigned)(A.rows * A.chunks);
+        if (A.two && A.T != 1.f) {
+            hipLaunchKernelGGL((k_distill_part<T, true>), dim3(groups), dim3(256), 0, s, A);
+            hipLaunchKernelGGL((k_distill_join<T, true>), dim3((unsigned)A.rows), dim3(64), 0, s, A);
+        } else {
+            hipLaunchKernelGGL((k_distill_part<T, false>), dim3(groups), dim3(256), 0, s, A);
+            hipLaunchKernelGGL((k_distill_join<T, false>), dim3((unsigned)A.rows), dim3(64), 0, s, A);
+        }
+    });
+}
+
+int check_work(int64_t rows, int64_t V, void* d_work, size_t work_bytes) {
+    size_t need = 0;
+    pcr_distill_workspace(rows, V, &need);
+    if (!need) return PCR_OK;
+    return !d_work ? PCR_E_ARG : work_bytes < need ? PCR_E_RANGE : PCR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, const int32_t* d_shape, const int64_t* d_offset, const int64_t* d_first, int64_t n,
+                   int64_t rows, int patch, int merge, int frames, int channels, const float* mean, const float* inv_std, int dtype,
+                   void* d_out, int32_t* d_positions, void* hip_stream) {
+    if (!mean || !inv_std || !known_type(dtype)) return PCR_E_ARG;
+    if (n < 0 || rows < 0 || patch < 1 || patch > 128 || merge < 1 || merge > 16 || frames < 1 || (channels != 1 && channels != 3)) return PCR_E_RANGE;
+    if (rows > 4 * kMaxGrid) return PCR_E_RANGE;
+    if (!d_offset || !d_first || (rows && !d_out) || (rows && n && (!d_pixels || !d_shape))) return PCR_E_ARG;
+    if (!rows) return PCR_OK;
+    PatchArgs A = {};
+    A.pixels = d_pixels; A.shape = d_shape; A.offset = d_offset; A.first = d_first; A.n = n; A.rows = rows;
+    A.pixel_bytes = (int64_t)std::min<size_t>(pixel_bytes, INT64_MAX);
+    A.patch = patch; A.merge = merge; A.frames = frames; A.channels = channels; A.out = d_out; A.positions = d_positions;
+    for (int c = 0; c < channels; c++) {
+        A.scale[c] = (float)((double)inv_std[c] / 255.0);
+        A.shift[c] = (float)(-(double)mean[c] * inv_std[c]);
+    }
+    HIP_TRY(hipSetDevice(device_id));
+    with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        hipLaunchKernelGGL(k_patch_rows<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, A);
+    });
+    return launched();
+}
+
+int pcr_rotate_axes(int device_id, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* rotation, int inverse, int dtype, void* hip_stream) {
+    return run_axes(device_id, q, k, rotation, 0.f, inverse != 0, dtype, dtype, kRotate, nullptr, 0, (hipStream_t)hip_stream);
+}
+
+int pcr_norm_rotate(int device_id, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* rotation, float eps, int dtype, int weight_dtype,
+                    void* hip_stream) {
+    return run_axes(device_id, q, k, rotation, eps, 0, dtype, weight_dtype, kNorm, nullptr, 0, (hipStream_t)hip_stream);
+}
+
+int pcr_norm_rotate_workspace(int64_t tokens, int dim, size_t* nbytes) {
+    if (!nbytes) return PCR_E_ARG;
+    if (tokens < 0 || dim < 1 || dim > 512) return PCR_E_RANGE;
+    *nbytes = (size_t)2 * std::min<int64_t>(tokens, kBackGroups) * dim * sizeof(float);
+    return PCR_OK;
+}
+
+int pcr_norm_rotate_backward(int device_id, const pcr_heads* q, const pcr_heads* k, const pcr_rotation* rotation, float eps, int dtype,
+                             int weight_dtype, void* d_work, size_t work_bytes, void* hip_stream) {
+    return run_axes(device_id, q, k, rotation, eps, 1, dtype, weight_dtype, kNormBack, d_work, work_bytes, (hipStream_t)hip_stream);
+}
+
+int pcr_distill_workspace(int64_t rows, int64_t classes, size_t* nbytes) {
+    if (!nbytes) return PCR_E_ARG;
+    if (rows < 0 || classes < 1) return PCR_E_RANGE;
+    const int64_t shares = shares_of(rows, classes);
+    *nbytes = shares > 1 ? (size_t)rows * (3 * shares + 2) * sizeof(float) : 0;
+    return PCR_OK;
+}
+
+int pcr_distill_forward(int device_id, const pcr_distill* d, float* loss, float* sums, void* d_work, size_t work_bytes, void* hip_stream) {
+    int rc = check_distill(d);
+    if (!rc && d->rows && (!loss || !sums)) rc = PCR_E_ARG;
+    if (!rc) rc = check_work(d->rows, d->classes, d_work, work_bytes);
+    if (rc || !d->rows) return rc;
+    DistillArgs A = distill_args(d);
+    A.loss = loss; A.sums = sums; A.part = (float*)d_work;
+    HIP_TRY(hipSetDevice(device_id));
+    const int64_t shares = shares_of(A.rows, A.V);
+    if (shares > 1) launch_shares(A, shares, d->dtype, (hipStream_t)hip_stream);
+    else launch_distill<kLoss>(A, d->dtype, (hipStream_t)hip_stream);
+    return launched();
+}
+
+int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums, const float* row_grad, void* out, int64_t out_stride, void* hip_stream) {
+    int rc = check_distill(d);
+    if (!rc && d->rows && (!sums || !row_grad || !out)) rc = PCR_E_ARG;
+    if (rc || !d->rows) return rc;
+    DistillArgs A = distill_args(d);
+    A.sums_in = sums; A.row_grad = row_grad; A.out = out; A.out_stride = out_stride;
+    const int64_t shares = shares_of(A.rows, A.V);
+    A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
+    A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+    HIP_TRY(hipSetDevice(device_id));
+    launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
+    return launched();
+}
+
+int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weight, float* loss, void* out, int64_t out_stride, void* d_work,
+                     size_t work_bytes, void* hip_stream) {
+    int rc = check_distill(d);
+    if (!rc && d->rows && (!row_weight || !loss || !out)) rc = PCR_E_ARG;
+    if (!rc) rc = check_work(d->rows, d->classes, d_work, work_bytes);
+    if (rc || !d->rows) return rc;
+    DistillArgs A = distill_args(d);
+    A.row_grad = row_weight; A.loss = loss; A.out = out; A.out_stride = out_stride;
+    HIP_TRY(hipSetDevice(device_id));
+    const int64_t shares = shares_of(A.rows, A.V);
+    if (shares > 1) {
+        A.part = (float*)d_work;
+        A.sums = A.part + 3 * A.rows * shares;
+        launch_shares(A, shares, d->dtype, (hipStream_t)hip_stream);
+        A.sums_in = A.sums;
+        A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
+        A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+        launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
+    } else launch_distill<kStep>(A, d->dtype, (hipStream_t)hip_stream);
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,296 @@
+"""Distillation from a teacher's top logits, forward, backward and both in one pass, against the formulas in 64 bits.
+
+Tolerances, u the half unit of the output's type: a lane adds at most V / 64 / (elements of a run) exponentials after each other, here at most 2^11, each
+off by some units of 2^-24 for the hardware's exponential and |x - maximum| 2^-23 for its argument (32 at most where it counts), so a sum is off by less
+than 2^-12 of itself in the worst case and 2^-17 where errors do not all have one sign, which is what is asked; its logarithm by 2^-17, and the sums
+themselves by 2^-23 of |L|.  The loss's terms p (log p - z / T + L) are off by 2^-22 of |z / T| + |L| + |t / T|.
+A dense gradient is g (a T P softmax(z / T) + b softmax(z)): off by 2^-16 of these (2^-17 of the sums, the same again for arguments), one by an entry's delta by
+2^-16 of it, too."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1911_00472_amd as pkg
+
+pytestmark = pytest.mark.gpu
+HALF_UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -125, torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -125}
+
+
+def reference(z, index, t, labels, T, a, b, weight=None):
+    """float64 on the host, row by row: (loss, sums, gradient of sum(weight * loss), magnitude of the gradient's terms, magnitude of the loss's)."""
+    z, t = z.double().cpu().numpy(), t.double().cpu().numpy()
+    index = index.cpu().numpy()
+    N, V = z.shape
+    loss, sums, grad, size, terms = np.zeros(N), np.zeros((N, 2)), np.zeros((N, V)), np.zeros((N, V)), np.zeros(N)
+    for n in range(N):
+        w = 1.0 if weight is None else float(weight[n])
+        with np.errstate(all="ignore"):
+            m = z[n].max()
+            L = m / T + math.log(np.exp((z[n] - m) / T).sum()) if np.isfinite(m) else math.nan
+            L1 = m + math.log(np.exp(z[n] - m).sum()) if np.isfinite(m) else math.nan
+        sums[n] = L, L1 if labels is not None and b else 0.0
+        keep = [k for k in range(index.shape[1]) if 0 <= index[n, k] < V and t[n, k] > -math.inf] if a else []
+        label = int(labels[n]) if labels is not None and b and 0 <= int(labels[n]) < V else None
+        if keep:
+            v = t[n, keep] / T
+            e = np.exp(v - v.max())
+            p = e / e.sum()
+            logp = v - v.max() - math.log(e.sum())
+            for k, pk, lk in zip(keep, p, logp):
+                if pk > 0:
+                    loss[n] += a * T * T * pk * (lk - z[n, index[n, k]] / T + L)
+                    terms[n] += abs(a) * T * T * pk * (1 + abs(lk) + abs(t[n, k]) / T + abs(z[n, index[n, k]]) / T + abs(L))
+                grad[n, index[n, k]] -= a * T * pk
+                size[n, index[n, k]] += abs(a) * T * pk
+            q = np.exp(z[n] / T - L)
+            grad[n] += a * T * q
+            size[n] += abs(a) * T * q
+        if label is not None:
+            loss[n] += b * (L1 - z[n, label])
+            terms[n] += abs(b) * (1 + abs(L1) + abs(z[n, label]))
+            q = np.exp(z[n] - L1)
+            grad[n] += b * q
+            grad[n, label] -= b
+            size[n] += abs(b) * q
+            size[n, label] += abs(b)
+        loss[n] *= w
+        grad[n] *= w
+        size[n] *= abs(w)
+        terms[n] *= abs(w)
+        if w == 0 or (not keep and label is None):
+            loss[n], grad[n], size[n], terms[n] = 0.0, 0.0, 0.0, 0.0
+    return loss, sums, grad, size, terms
+
+
+def near(got, want, tol):
+    got = got.double().cpu().numpy()
+    off = np.abs(got - want)
+    assert got.shape == want.shape and (off <= tol).all(), float((off - tol).max())
+
+
+def check_all(z, index, t, labels=None, T=1.0, a=1.0, b=0.0, weight=None):
+    """All three calls, and the gradient written over the logits."""
+    N, V = z.shape
+    if weight is None:
+        weight = torch.linspace(-0.5, 1.5, N, device="cuda") + 0.01
+    how = dict(labels=labels, temperature=T, distill_part=a, label_part=b)
+    plain = reference(z, index, t, labels, T, a, b)
+    loss, sums = pkg.distill_forward(z, index, t, **how)
+    near(loss, plain[0], 2.0 ** -17 * (abs(a) * T * T + abs(b)) + 2.0 ** -22 * plain[4])
+    near(sums, plain[1], 2.0 ** -17 + 2.0 ** -23 * np.abs(plain[1]))
+    want, _, grad, size, terms = reference(z, index, t, labels, T, a, b, weight.cpu())
+    tol = HALF_UNIT[z.dtype] * np.abs(grad) + TINY[z.dtype] + 2.0 ** -16 * size
+    back = pkg.distill_backward(weight, z, index, t, sums, **how)
+    near(back, grad, tol)
+    got, step = pkg.distill_step(z, index, t, weight, **how)
+    near(got, want, 2.0 ** -17 * np.abs(weight.cpu().numpy()) * (abs(a) * T * T + abs(b)) + 2.0 ** -22 * terms)
+    near(step, grad, tol)
+    over = z.clone()
+    assert pkg.distill_backward(weight, over, index, t, sums, out=over, **how) is over and torch.equal(over, back)
+    over = z.clone()
+    got2, _ = pkg.distill_step(over, index, t, weight, out=over, **how)
+    assert torch.equal(over, step) and torch.equal(got, got2)
+    return loss, sums, back, step
+
+
+def make(N, V, K, dtype, seed, kind=torch.int32, top_dtype=None, scale=2.0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    z = (torch.randn((N, V), generator=gen, device="cuda") * scale).to(dtype)
+    index = torch.rand((N, V), generator=gen, device="cuda").argsort(1)[:, :K] if K <= V else torch.randint(0, V, (N, K), generator=gen, device="cuda")
+    t = (torch.randn((N, K), generator=gen, device="cuda") * 3).to(top_dtype or dtype)
+    labels = torch.randint(0, V, (N,), generator=gen, device="cuda")
+    labels[::5] = -100
+    return z, index.to(kind).contiguous(), t, labels
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,V,K", [(1, 1, 1), (3, 2, 2), (9, 63, 5), (5, 64, 64), (70, 1000, 10), (6, 4097, 33), (3, 8193, 128), (600, 300, 3), (5, 33001, 50), (2, 70001, 7), (520, 9001, 20),
+                                   (513, 40003, 16), (1, 5, 1024)])
+def test_sizes_and_types(N, V, K, dtype):
+    z, index, t, labels = make(N, V, K, dtype, N + V)
+    check_all(z, index, t)
+    check_all(z, index, t, labels, 2.0, 0.7, 0.3)
+    check_all(z, index, t, labels, 1.0, 0.5, 0.5)
+    if N < 100:
+        check_all(z, index, t, labels, 3.5, 1.0, 0.0)
+        check_all(z, index, t, labels, 0.5, 0.0, 1.0)
+        check_all(z, index, t, None, 1.5, 2.0, 1.0)
+
+
+@pytest.mark.parametrize("V", [200, 5000, 40000])
+def test_entries_that_do_not_count_classes_kept_twice_and_other_types(V):
+    for kind, top_dtype, dtype in ((torch.int64, torch.float32, torch.bfloat16), (torch.int32, torch.bfloat16, torch.float32), (torch.int64, torch.float16, torch.float16)):
+        z, index, t, labels = make(12, V, 40, dtype, V, kind, top_dtype)
+        index[:, 3] = index[:, 30]                             # twice
+        index[2] = index[2, 0]                                 # all the same class
+        index[4, 7], index[4, 8], index[4, 9] = -1, V, 2 ** 31 - 1
+        if kind == torch.int64:
+            index[4, 10], index[4, 11] = 2 ** 33 + 5, -2 ** 40
+        index[6] = -1                                          # nothing kept
+        t[8, 1:] = -math.inf
+        t[9] = -math.inf
+        index[10, 0] = labels[10] = 17                         # the label is kept, too
+        labels[11] = V
+        check_all(z, index, t, labels, 2.0, 0.6, 0.4)
+        check_all(z, index, t, None, 1.0, 1.0, 0.0)
+
+
+@pytest.mark.parametrize("V", [100, 30000, 100000])
+def test_masked_classes_lowest_values_and_rows_that_are_left_out(V):
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        z, index, t, labels = make(10, V, 20, dtype, 3)
+        low = torch.finfo(dtype).min
+        masked = torch.arange(V, device="cuda") % 3 == 1
+        index = torch.where(masked[index.long()], (index + 1) % V, index)
+        index = torch.where(masked[index.long()], -1, index).to(torch.int32).contiguous()
+        labels = torch.where((labels >= 0) & masked[labels.clamp(min=0)], -100, labels)
+        z[:5, masked] = -math.inf
+        z[5:8, masked] = low
+        z[8] = low                                             # a row all of the lowest value: every class is as likely
+        loss, sums, back, step = check_rows(z, index, t, labels, [8])
+        assert not back[:5, masked].any() and not step[:8, masked].any()
+        z[3], z[4, 5] = math.nan, math.inf
+        weight = torch.ones(10, device="cuda")
+        weight[3] = weight[4] = 0
+        loss, step = pkg.distill_step(z, index, t, weight, labels, 2.0, 0.5, 0.5)
+        assert not step[3].any() and not step[4].any() and not loss[3] and not loss[4] and torch.isfinite(loss).all()
+        assert not pkg.distill_backward(weight, z, index, t, sums, labels, 2.0, 0.5, 0.5)[3:5].any()
+        index[3], labels[3] = -1, -100                         # no term: left out with a weight as well
+        weight[3] = 1
+        loss, step = pkg.distill_step(z, index, t, weight, labels, 2.0, 0.5, 0.5)
+        assert not step[3].any() and not loss[3]
+        loss, sums = pkg.distill_forward(z, index, t, labels, 2.0, 0.5, 0.5)
+        assert not loss[3] and torch.isnan(loss[4])
+        assert not pkg.distill_backward(weight, z, index, t, sums, labels, 2.0, 0.5, 0.5)[3].any()
+
+
+def check_rows(z, index, t, labels, uniform):
+    """check_all without the rows `uniform`, all of whose logits are the same: for these every class is as likely, and the logarithm is lost beside the
+    logits in the sums that are saved (and in 64 bits): the loss is held to log V."""
+    rest = [n for n in range(z.shape[0]) if n not in uniform]
+    check_all(z[rest].contiguous(), index[rest].contiguous(), t[rest].contiguous(), labels[rest].contiguous(), 2.0, 0.5, 0.5)
+    how = dict(labels=labels, temperature=2.0, distill_part=0.5, label_part=0.5)
+    loss, sums = pkg.distill_forward(z, index, t, **how)
+    weight = torch.ones(z.shape[0], device="cuda")
+    back = pkg.distill_backward(weight, z, index, t, sums, **how)
+    got, step = pkg.distill_step(z, index, t, weight, **how)
+    V = z.shape[1]
+    for n in uniform:
+        keep = index[n] >= 0
+        p = torch.softmax(t[n][keep].double() / 2.0, 0)
+        want = 0.5 * 4.0 * float((p * (p.log() + math.log(V))).sum()) + (0.5 * math.log(V) if 0 <= int(labels[n]) < V else 0.0)
+        assert abs(float(loss[n]) - want) <= 2.0 ** -14 * abs(want) and abs(float(got[n]) - want) <= 2.0 ** -14 * abs(want)
+    return loss, sums, back, step
+
+
+def test_views_of_wider_rows_and_other_strides():
+    for dtype in (torch.float32, torch.bfloat16):
+        z, index, t, labels = make(7, 5003, 12, dtype, 8)
+        wide = torch.full((7, 6001), math.nan, dtype=dtype, device="cuda")
+        for shift in (0, 1, 3, 6):
+            view = wide[:, shift:shift + 5003]
+            view.copy_(z)
+            weight = torch.rand(7, device="cuda")
+            how = dict(labels=labels, temperature=2.0, distill_part=0.5, label_part=0.5)
+            loss, sums = pkg.distill_forward(view, index, t, **how)
+            want = reference(z, index, t, labels, 2.0, 0.5, 0.5, weight.cpu())
+            tol = HALF_UNIT[dtype] * np.abs(want[2]) + TINY[dtype] + 2.0 ** -16 * want[3]
+            held = torch.full((7, 5100), 5.0, dtype=dtype, device="cuda")
+            out = held[:, 2:5005]
+            pkg.distill_backward(weight, view, index, t, sums, out=out, **how)
+            near(out, want[2], tol)
+            pkg.distill_step(view, index, t, weight, out=out, **how)
+            near(out, want[2], tol)
+            assert (held[:, :2] == 5).all() and (held[:, 5005:] == 5).all()
+
+
+def test_rows_past_32_bits():
+    """The second row begins more than 2^31 elements behind the first."""
+    z, index, t, labels = make(2, 20011, 9, torch.bfloat16, 4)
+    far = 2 ** 31 + 72
+    view = torch.empty(far + 20011, dtype=torch.bfloat16, device="cuda").as_strided((2, 20011), (far, 1))
+    view.copy_(z)
+    weight = torch.ones(2, device="cuda")
+    loss, step = pkg.distill_step(z, index, t, weight, labels, 2.0, 0.5, 0.5)
+    got, out = pkg.distill_step(view, index, t, weight, labels, 2.0, 0.5, 0.5, out=view)
+    assert torch.equal(out, step) and torch.equal(got, loss)
+
+
+def test_no_rows():
+    z, index, t, labels = make(4, 50, 3, torch.float32, 1)
+    loss, sums = pkg.distill_forward(z[:0], index[:0], t[:0], labels[:0], label_part=1.0)
+    assert loss.shape == (0,) and sums.shape == (0, 2)
+    assert pkg.distill_backward(loss, z[:0], index[:0], t[:0], sums).shape == (0, 50)
+    assert pkg.distill_step(z[:0], index[:0], t[:0], loss)[1].shape == (0, 50)
+
+
+def test_differentiation_and_differences():
+    """Through autograd: along a random direction the loss changes as the gradient says.  Differences over 2 h, h = 2^-6, leave h^2 / 6 of the third
+    derivative, which is at most a few times the gradient's terms (2^-12 of their sum), and 2^-18 of the losses over h."""
+    z, index, t, labels = make(16, 700, 12, torch.float32, 21)
+    z.requires_grad_()
+    weight = torch.rand(16, device="cuda")
+    (pkg.distill_loss(z, index, t, labels, 2.0, 0.6, 0.4) * weight).sum().backward()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    d = torch.randn(z.shape, generator=gen, device="cuda")
+    h = 2.0 ** -6
+    with torch.no_grad():
+        up, down = ((pkg.distill_loss(z + s * h * d, index, t, labels, 2.0, 0.6, 0.4) * weight).double().sum() for s in (1, -1))
+        size = torch.from_numpy(reference(z, index, t, labels, 2.0, 0.6, 0.4, weight.cpu())[3])
+        slack = 2.0 ** -10 * (size * d.abs().double().cpu()).sum() + 2.0 ** -16 / h
+    along = float((z.grad.double() * d.double()).sum())
+    assert abs(float(up - down) / (2 * h) - along) <= float(slack), (along, float(up - down) / (2 * h))
+
+
+@pytest.mark.parametrize("N,V", [(5, 40001), (600, 501)])
+def test_streams_and_graphs(N, V):
+    z, index, t, labels = make(N, V, 17, torch.bfloat16, 31)
+    weight = torch.rand(N, device="cuda")
+
+    def all_of():
+        loss, sums = pkg.distill_forward(z, index, t, labels, 2.0, 0.6, 0.4)
+        return (loss, sums, pkg.distill_backward(weight, z, index, t, sums, labels, 2.0, 0.6, 0.4)) + pkg.distill_step(z, index, t, weight, labels, 2.0, 0.6, 0.4)
+    want = all_of()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = all_of()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = all_of()
+    for turn in range(4):
+        z.copy_(torch.randn(z.shape, device="cuda"))
+        graph.replay()
+        want = all_of()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, held)), turn
+
+
+def test_refusals():
+    z, index, t, labels = make(6, 50, 4, torch.float32, 2)
+    weight = torch.ones(6, device="cuda")
+
+    def call(**more):
+        a = dict(logits=z, top_index=index, top_logits=t, row_weight=weight, labels=labels)
+        a.update(more)
+        return pkg.distill_step(**a)
+    call()
+    for bad in (dict(logits=z.cpu()), dict(logits=z.double()), dict(logits=z[0]), dict(logits=z.t()), dict(top_index=index.float()), dict(top_index=index[:5]), dict(top_index=index.cpu()),
+                dict(top_logits=t[:, :3]), dict(top_logits=t.double()), dict(labels=labels.int()), dict(labels=labels[:5]), dict(row_weight=weight.double()), dict(row_weight=weight[:5]),
+                dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.inf), dict(temperature=math.nan), dict(out=z.half()), dict(out=z[:5]), dict(out=z.t())):
+        with pytest.raises(ValueError):
+            call(**bad)
+    for bad in (dict(top_index=torch.zeros((6, 1025), dtype=torch.int32, device="cuda"), top_logits=torch.zeros((6, 1025), device="cuda")), dict(distill_part=math.nan), dict(label_part=math.inf),
+                dict(top_index=index[:, :0].contiguous(), top_logits=t[:, :0].contiguous())):
+        with pytest.raises(pkg.PcrError) as e:
+            call(**bad)
+        assert e.value.code == pkg.E_RANGE
+    with pytest.raises(ValueError):
+        pkg.distill_backward(weight, z, index, t, torch.zeros((6, 1), device="cuda"))
