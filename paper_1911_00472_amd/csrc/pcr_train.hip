@@ -11,11 +11,21 @@
 
 using namespace pcr;
 
-#define HIP_TRY(expr) do { if ((expr) != hipSuccess) { (void)hipGetLastError(); return PCR_E_DEVICE; } } while (0)
-
 namespace {
 
 constexpr int64_t kMaxGrid = 2147483647;
+
+// The calling thread's device while a call enqueues its work, and the one it had behind it.
+struct OnDevice {
+    int before = -1;
+    bool ok;
+    explicit OnDevice(int device) {
+        ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess);
+        if (!ok) (void)hipGetLastError();
+        if (before == device) before = -1;
+    }
+    ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
 
 int launched() { return hipGetLastError() == hipSuccess ? PCR_OK : PCR_E_DEVICE; }
 
@@ -111,7 +121,8 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         if (A.batch_tokens && (!d_work || work_bytes < need)) return d_work ? PCR_E_RANGE : PCR_E_ARG;
         for (int z = 0; z < 2; z++) if (side[z]->weight_grad) A.side[z].part = (float*)d_work + (size_t)z * groups * R->dim;
     }
-    HIP_TRY(hipSetDevice(device));
+    const OnDevice on(device);
+    if (!on.ok) return PCR_E_DEVICE;
     if (q->heads + k->heads == 0) groups = 0;
     if (groups) {
         with_type(dtype, [&](auto t) {
@@ -228,7 +239,8 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
         A.scale[c] = (float)((double)inv_std[c] / 255.0);
         A.shift[c] = (float)(-(double)mean[c] * inv_std[c]);
     }
-    HIP_TRY(hipSetDevice(device_id));
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         hipLaunchKernelGGL(k_patch_rows<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, A);
@@ -272,7 +284,8 @@ int pcr_distill_forward(int device_id, const pcr_distill* d, float* loss, float*
     if (rc || !d->rows) return rc;
     DistillArgs A = distill_args(d);
     A.loss = loss; A.sums = sums; A.part = (float*)d_work;
-    HIP_TRY(hipSetDevice(device_id));
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
     const int64_t shares = shares_of(A.rows, A.V);
     if (shares > 1) launch_shares(A, shares, d->dtype, (hipStream_t)hip_stream);
     else launch_distill<kLoss>(A, d->dtype, (hipStream_t)hip_stream);
@@ -288,7 +301,8 @@ int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums,
     const int64_t shares = shares_of(A.rows, A.V);
     A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
     A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
-    HIP_TRY(hipSetDevice(device_id));
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
     launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
     return launched();
 }
@@ -301,7 +315,8 @@ int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weigh
     if (rc || !d->rows) return rc;
     DistillArgs A = distill_args(d);
     A.row_grad = row_weight; A.loss = loss; A.out = out; A.out_stride = out_stride;
-    HIP_TRY(hipSetDevice(device_id));
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
     const int64_t shares = shares_of(A.rows, A.V);
     if (shares > 1) {
         A.part = (float*)d_work;

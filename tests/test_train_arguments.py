@@ -4,7 +4,23 @@ import os
 import subprocess
 
 import paper_1911_00472_amd as pkg
-from paper_1911_00472_amd import train
+
+_i64, _i32, _vp, _f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
+
+
+class Heads(ctypes.Structure):                             # pcr_heads
+    _fields_ = [("in_", _vp), ("in_batch", _i64), ("in_token", _i64), ("in_head", _i64), ("out", _vp), ("out_batch", _i64), ("out_token", _i64), ("out_head", _i64),
+                ("grad", _vp), ("grad_batch", _i64), ("grad_token", _i64), ("grad_head", _i64), ("weight", _vp), ("weight_grad", _vp), ("heads", _i64)]
+
+
+class Rotation(ctypes.Structure):                          # pcr_rotation
+    _fields_ = [("position", _vp), ("axis_stride", _i64), ("batch_stride", _i64), ("token_stride", _i64), ("frequency", _vp), ("axis", _vp), ("batch", _i64), ("tokens", _i64),
+                ("wide", _i32), ("axes", _i32), ("dim", _i32), ("pairs", _i32), ("adjacent", _i32), ("reserved", _i32)]
+
+
+class Distill(ctypes.Structure):                           # pcr_distill
+    _fields_ = [("logits", _vp), ("row_stride", _i64), ("top_index", _vp), ("top_logits", _vp), ("labels", _vp), ("rows", _i64), ("classes", _i64), ("top", _i32), ("dtype", _i32),
+                ("top_dtype", _i32), ("index_wide", _i32), ("temperature", _f32), ("distill_part", _f32), ("label_part", _f32), ("reserved", _f32)]
 
 
 def test_null_pointers_and_sizes_out_of_range():
@@ -22,13 +38,13 @@ def test_null_pointers_and_sizes_out_of_range():
     assert L.pcr_patch_rows(*with_(patch, a7=0)) == pkg.OK                      # no rows: nothing to do
 
     def rotation(**changed):
-        r = train._Rotation(at, 1, 1, 1, at, at, 1, 1, 0, 1, 8, 4, 0, 0)
+        r = Rotation(at, 1, 1, 1, at, at, 1, 1, 0, 1, 8, 4, 0, 0)
         for k, v in changed.items():
             setattr(r, k, v)
         return r
 
     def heads(**changed):
-        h = train._Heads(at, 0, 0, 0, at, 0, 0, 0, at, 0, 0, 0, None, None, 1)
+        h = Heads(at, 0, 0, 0, at, 0, 0, 0, at, 0, 0, 0, None, None, 1)
         for k, v in changed.items():
             setattr(h, k, v)
         return h
@@ -54,7 +70,7 @@ def test_null_pointers_and_sizes_out_of_range():
     assert L.pcr_norm_rotate_backward(0, by(asks), by(heads()), by(rotation()), 1e-6, 0, 0, at, 8, None) == pkg.E_RANGE
 
     def distill(**changed):
-        d = train._Distill(at, 10, at, at, None, 2, 10, 3, 0, 0, 0, 1.0, 1.0, 0.0, 0.0)
+        d = Distill(at, 10, at, at, None, 2, 10, 3, 0, 0, 0, 1.0, 1.0, 0.0, 0.0)
         for k, v in changed.items():
             setattr(d, k, v)
         return d
