@@ -234,16 +234,34 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
     PatchArgs A = {};
     A.pixels = d_pixels; A.shape = d_shape; A.offset = d_offset; A.first = d_first; A.n = n; A.rows = rows;
     A.pixel_bytes = (int64_t)std::min<size_t>(pixel_bytes, INT64_MAX);
-    A.patch = patch; A.merge = merge; A.frames = frames; A.channels = channels; A.out = d_out; A.positions = d_positions;
+    A.patch = patch; A.merge = merge; A.frames = frames; A.out = d_out; A.positions = d_positions;
     for (int c = 0; c < channels; c++) {
         A.scale[c] = (float)((double)inv_std[c] / 255.0);
         A.shift[c] = (float)(-(double)mean[c] * inv_std[c]);
     }
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
+    const uint32_t runs = (patch + 7) / 8, each = runs * patch;
+    A.by_runs = (uint32_t)(((1ull << 32) + runs - 1) / runs);  // (of 1: 0)
+    A.by_each = (uint32_t)(((1ull << 32) + each - 1) / each);
+    // Rows of a workgroup: some 512 runs of eight pixels (256 where elements have 32 bits).  Stores go through LDS where lines are not of whole runs and a row fits there.
+    const size_t row_bytes = (size_t)channels * patch * patch * type_size(dtype);
+    const bool staged = patch % 8 && row_bytes <= 65536;
+    int64_t group = (dtype == PCR_FLOAT ? 256 : 512) / each;
+    if (staged) group = std::min<int64_t>(group, 20480 / row_bytes);
+    A.group = (int)std::max<int64_t>(1, std::min<int64_t>(group, kPatchGroup));
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL(k_patch_rows<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, A);
+        auto launch = [&](auto c, auto s) {
+            hipLaunchKernelGGL((k_patch_rows<T, decltype(c)::value, decltype(s)::value>), dim3((unsigned)((rows + A.group - 1) / A.group)), dim3(256), staged ? A.group * row_bytes : 0,
+                               (hipStream_t)hip_stream, A);
+        };
+        auto by_channels = [&](auto s) {
+            if (channels == 3) launch(std::integral_constant<int, 3>(), s);
+            else launch(std::integral_constant<int, 1>(), s);
+        };
+        if (staged) by_channels(std::true_type());
+        else by_channels(std::false_type());
     });
     return launched();
 }
