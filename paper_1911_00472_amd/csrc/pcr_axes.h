@@ -19,17 +19,18 @@ namespace pcr {
 struct HeadSide {
     const void* in; const void* grad; void* out; const void* weight; float* part;    // part: [workgroup][dim] sums of the weight's gradient
     int64_t in_b, in_t, in_h, out_b, out_t, out_h, grad_b, grad_t, grad_h;
-    int heads;
+    int heads, step_tokens, step_heads;                        // a wavefront's step to its next rows, as tokens and heads
+    uint32_t by_heads;                                         // 2^32 / heads, rounded up
 };
 struct AxesArgs {
     HeadSide side[2];
     const void* position; const float* frequency; const int32_t* axis;
-    int64_t pos_a, pos_b, pos_t, batch_tokens, chunks;
-    int64_t tokens;
+    int64_t pos_a, pos_b, pos_t, tokens, shares, chunks;       // shares: chunks of a sequence
     int wide, axes, dim, pairs, inverse, weight_float;
+    int far;                                                   // a stride of tokens or heads is outside 32 bits
     int slots, per_wave;                                       // slots of a row; rows of a wavefront (64 / slots, at least 1)
     int chunk;                                                 // tokens of a workgroup at a time
-    float eps;
+    float eps, inv_dim;
 };
 
 enum { kRotate = 0, kNorm = 1, kNormBack = 2 };
@@ -50,27 +51,32 @@ __device__ __forceinline__ uint64_t turns_of(float f) {
     return bits >> 31 ? 0 - v : v;
 }
 
-// A token: its sequence and its place there.  The token `more` places on, of sequences of `tokens`, which may be several on.
-struct Place {
-    int64_t b; uint32_t t;
-    __device__ __forceinline__ Place of(int more, int64_t tokens) const {
-        const uint32_t n = (uint32_t)tokens, at = t + (uint32_t)more;
-        if (at < n) return {b, at};
-        return {b + at / n, at % n};
-    }
-};
-
-__device__ __forceinline__ void turn_of(const AxesArgs& A, Place place, int pair, float& c, float& s) {
+__device__ __forceinline__ float2 turn_of(const AxesArgs& A, int64_t b, int64_t t, int pair) {
     const int a = min(max(A.axis[pair], 0), A.axes - 1);
-    const int64_t at = a * A.pos_a + place.b * A.pos_b + place.t * A.pos_t;
+    const int64_t at = a * A.pos_a + b * A.pos_b + t * A.pos_t;
     const int64_t pos = A.wide ? ((const int64_t*)A.position)[at] : (int64_t)((const int32_t*)A.position)[at];
     const int32_t phase = (int32_t)(turns_of((float)pos * A.frequency[pair]) >> 32);
+    float c, s;
     sincospif((float)phase * 4.656612873077392578125e-10f, &s, &c);              // 2^-31: in halves of a turn
-    if (A.inverse) s = -s;
+    return make_float2(c, A.inverse ? -s : s);
 }
 
-// Sum over a row's group of lanes (`slots` neighbouring ones from `head` on), the same in all of them; `width`: a power of two that is not below it.
-__device__ __forceinline__ float group_sum(float v, int head, int member, int slots, int width) {
+template <int CONTROL> __device__ __forceinline__ float across(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
+}
+// Sum over a row's group of lanes (`slots` neighbouring ones from `head` on), the same bits in all of them.
+__device__ __forceinline__ float group_sum(float v, int head, int member, int slots) {
+    if ((slots & (slots - 1)) == 0) {                          // (the same for all lanes, as what follows)
+        if (slots > 1) v += across<0xb1>(v);                   // the neighbour, the other pair of four, the other four of eight (mirrored), the other eight
+        if (slots > 2) v += across<0x4e>(v);
+        if (slots > 4) v += across<0x141>(v);
+        if (slots > 8) v += across<0x140>(v);
+        if (slots > 16) v += __shfl_xor(v, 16);
+        if (slots > 32) v += __shfl_xor(v, 32);
+        return v;
+    }
+    int width = 1;
+    while (width < slots) width <<= 1;
     for (int d = width >> 1; d; d >>= 1) {
         const float o = __shfl(v, head + member + d);
         if (member + d < slots) v += o;
@@ -86,18 +92,75 @@ template <typename T, int N> __device__ __forceinline__ void load_weight(const A
     else load_run<T, N>((const T*)w + at, x);
 }
 
+// A lane's slot of a row as it lies in memory: two runs, which are one in memory where a pair's elements are neighbours.
+template <typename T, int N, bool ADJ> struct Slot {
+    typename Run<T, N>::Vec run[2];
+    static constexpr bool kOne = ADJ && 2 * N * sizeof(T) <= 16;
+    __device__ __forceinline__ void load(const T* row, int first, int second, int dim) {
+        if constexpr (kOne && N > 1) {                         // (there always is a second run then)
+            if (first < dim) {
+                const typename Run<T, 2 * N>::Vec v = reinterpret_cast<const typename Run<T, 2 * N>::Loose*>(row + first)->v;
+#pragma unroll
+                for (int i = 0; i < N; i++) { run[0][i] = v[i]; run[1][i] = v[N + i]; }
+            }
+        } else {
+            if (first < dim) run[0] = reinterpret_cast<const typename Run<T, N>::Loose*>(row + first)->v;
+            if (second < dim) run[1] = reinterpret_cast<const typename Run<T, N>::Loose*>(row + second)->v;
+        }
+    }
+    __device__ __forceinline__ void clear() { run[0] = run[1] = {}; }
+    __device__ __forceinline__ void take(float (&x)[2 * N]) const {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if constexpr (N == 1) { x[0] = (float)run[0]; x[1] = (float)run[1]; }
+            else { x[i] = (float)run[0][i]; x[N + i] = (float)run[1][i]; }
+        }
+    }
+    static __device__ __forceinline__ void store(T* row, int first, int second, int dim, const float (&x)[2 * N]) {
+        if constexpr (kOne && N > 1) {
+            if (first < dim) store_run<T, 2 * N>(row + first, x);
+        } else {
+            float v[N], u[N];
+#pragma unroll
+            for (int i = 0; i < N; i++) { v[i] = x[i]; u[i] = x[N + i]; }
+            if (first < dim) store_run<T, N>(row + first, v);
+            if (second < dim) store_run<T, N>(row + second, u);
+        }
+    }
+};
+
+__device__ __forceinline__ int64_t row_offset(int tl, int h, int64_t per_token, int64_t per_head, int far) {
+    if (far) return tl * per_token + h * per_head;
+    return (int64_t)tl * (int32_t)per_token + (int64_t)h * (int32_t)per_head;
+}
+
+// Turns the pairs of a lane's slots by the row's sines and cosines.
+template <int N, bool ADJ, int K> __device__ __forceinline__ void turn(float (&y)[K][2 * N], const float2* turns, const AxesArgs& A, int member, bool on) {
+#pragma unroll
+    for (int j = 0; j < K; j++) {
+        const int p = (member + 64 * j) * N;
+        if (on && p < A.pairs) {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int ia = ADJ ? 2 * i : i, ib = ADJ ? 2 * i + 1 : N + i;
+                const float2 cs = turns[p + i];
+                const float u = y[j][ia], v = y[j][ib];
+                y[j][ia] = __builtin_fmaf(u, cs.x, -(v * cs.y));
+                y[j][ib] = __builtin_fmaf(u, cs.y, v * cs.x);
+            }
+        }
+    }
+}
+
 // T: elements; N: elements of a run; ADJ: a pair's elements are neighbours (a slot is two runs behind each other) or half the rotated part apart;
-// K: slots of a lane (more than one where a row has more than 64).
+// K: slots of a lane (more than one where a row has more than 64).  Every slot is turned whole or not at all.
 template <typename T, int N, bool ADJ, int MODE, int K>
 __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
-    __shared__ float2 table[kAxesTable];
+    __shared__ __attribute__((aligned(16))) float2 table[kAxesTable];
     __shared__ float joined[MODE == kNormBack ? 4 * 512 : 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int slots = A.slots, width_slots = K > 1 ? 64 : slots;
-    const int head = K > 1 ? 0 : lane / width_slots * width_slots, member = lane - head;
-    const bool works = K > 1 || lane / width_slots < A.per_wave;
-    int width = 1;
-    while (width < width_slots) width <<= 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = A.dim;
+    const int group = K > 1 ? 64 : A.slots, place = lane / group, head = place * group, member = lane - head;
+    const bool works = place < A.per_wave;
     const int R = 2 * A.pairs;
 
     int first[K], second[K];                                   // where the lane's runs begin; dim: there is none
@@ -107,166 +170,169 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
         if (ADJ) { first[j] = 2 * N * s; second[j] = first[j] + N; }
         else if (s * N < A.pairs) { first[j] = s * N; second[j] = A.pairs + s * N; }
         else { first[j] = R + 2 * (s * N - A.pairs); second[j] = first[j] + N; }
-        if (s >= slots || first[j] >= A.dim) first[j] = A.dim;
-        if (s >= slots || second[j] >= A.dim) second[j] = A.dim;
+        if (s >= A.slots || first[j] >= dim) first[j] = dim;
+        if (s >= A.slots || second[j] >= dim) second[j] = dim;
     }
-    float dw[2][K][2 * N];
+    // A gradient takes one side after the other, so that the sums of one weight's gradient are held at a time.
+#pragma unroll 1
+    for (int side = 0; side < (MODE == kNormBack ? 2 : 1); side++) {
+    float dw[K][2 * N];
     if (MODE == kNormBack) {
+        if (!A.side[side].heads && !A.side[side].part) continue;
 #pragma unroll
-        for (int e = 0; e < 2 * K * 2 * N; e++) (&dw[0][0][0])[e] = 0.f;
+        for (int j = 0; j < K; j++)
+#pragma unroll
+            for (int i = 0; i < 2 * N; i++) dw[j][i] = 0.f;
     }
-
     for (int64_t chunk = blockIdx.x; chunk < A.chunks; chunk += gridDim.x) {
-        const int64_t t0 = chunk * A.chunk;
-        const Place base = {t0 / A.tokens, (uint32_t)(t0 % A.tokens)};
-        const int here = (int)min((int64_t)A.chunk, A.batch_tokens - t0);
+        const int64_t b = chunk / A.shares, t0 = (chunk - b * A.shares) * A.chunk;
+        const int here = (int)min((int64_t)A.chunk, A.tokens - t0);
         for (int e = threadIdx.x; e < here * A.pairs; e += 256) {
-            float c, s;
-            turn_of(A, base.of(e / A.pairs, A.tokens), e % A.pairs, c, s);
-            table[e] = make_float2(c, s);
+            const int t = e / A.pairs;
+            table[e] = turn_of(A, b, t0 + t, e - t * A.pairs);
         }
         __syncthreads();
-#pragma unroll
-        for (int z = 0; z < 2; z++) {
+#pragma unroll 1
+        for (int z = MODE == kNormBack ? side : 0; z < (MODE == kNormBack ? side + 1 : 2); z++) {
             const HeadSide& S = A.side[z];
+            const int rows = here * S.heads;
+            if (!rows) continue;
             float w[K][2 * N];
-            if (MODE != kRotate && works && S.heads) {
+            if (MODE != kRotate) {
 #pragma unroll
                 for (int j = 0; j < K; j++) {
-                    float x[N];
-                    if (first[j] < A.dim) { load_weight<T, N>(A, S.weight, first[j], x); for (int i = 0; i < N; i++) w[j][i] = x[i]; }
-                    if (second[j] < A.dim) { load_weight<T, N>(A, S.weight, second[j], x); for (int i = 0; i < N; i++) w[j][N + i] = x[i]; }
+                    float x[N], y[N];
+#pragma unroll
+                    for (int i = 0; i < N; i++) x[i] = y[i] = 0.f;
+                    if (first[j] < dim) load_weight<T, N>(A, S.weight, first[j], x);
+                    if (second[j] < dim) load_weight<T, N>(A, S.weight, second[j], y);
+#pragma unroll
+                    for (int i = 0; i < N; i++) { w[j][i] = x[i]; w[j][N + i] = y[i]; }
                 }
             }
-            const int rows = here * S.heads;
-            for (int r0 = wave * A.per_wave; r0 < rows; r0 += 4 * A.per_wave) {
-                const int r = r0 + (K > 1 ? 0 : lane / width_slots);
-                const bool on = works && r < rows;
-                const int tl = on ? r / S.heads : 0, h = on ? r - tl * S.heads : 0;
-                const Place at = base.of(tl, A.tokens);
-                const int64_t b = at.b, t = at.t;
-                const T* in = (const T*)S.in + b * S.in_b + t * S.in_t + h * S.in_h;
-                const T* gin = (const T*)S.grad + b * S.grad_b + t * S.grad_t + h * S.grad_h;
-                T* out = (T*)S.out + b * S.out_b + t * S.out_t + h * S.out_h;
-                float x[K][2 * N], g[K][2 * N];
-                float sum = 0.f;
+            const T* in = (const T*)S.in + b * S.in_b + t0 * S.in_t;
+            const T* gin = (const T*)S.grad + b * S.grad_b + t0 * S.grad_t;
+            T* out = (T*)S.out + b * S.out_b + t0 * S.out_t;
+            // A wavefront's rows are per_wave ones side by side, then those 4 per_wave further on.  The next row is loaded before the last one is done.
+            int r = wave * A.per_wave + place, tl = (int)__umulhi((uint32_t)r, S.by_heads), h = r - tl * S.heads;
+            if (S.heads == 1) { tl = r; h = 0; }
+            Slot<T, N, ADJ> X[K], G[K];
+            auto fetch = [&]() {
+                if (works && r < rows) {
+                    const T* row = in + row_offset(tl, h, S.in_t, S.in_h, A.far);
+                    const T* grow = gin + row_offset(tl, h, S.grad_t, S.grad_h, A.far);
 #pragma unroll
-                for (int j = 0; j < K; j++) {
-#pragma unroll
-                    for (int half = 0; half < 2; half++) {
-                        const int at = half ? second[j] : first[j];
-                        float v[N] = {};
-                        if (on && at < A.dim) load_run<T, N>(in + at, v);
-#pragma unroll
-                        for (int i = 0; i < N; i++) x[j][half * N + i] = v[i];
-                        if (MODE == kNormBack) {
-                            float u[N] = {};
-                            if (on && at < A.dim) load_run<T, N>(gin + at, u);
-#pragma unroll
-                            for (int i = 0; i < N; i++) g[j][half * N + i] = u[i];
-                        }
+                    for (int j = 0; j < K; j++) {
+                        X[j].load(row, first[j], second[j], dim);
+                        if (MODE == kNormBack) G[j].load(grow, first[j], second[j], dim);
                     }
                 }
-                float rms = 1.f;
+            };
+#pragma unroll
+            for (int j = 0; j < K; j++) { X[j].clear(); G[j].clear(); }
+            fetch();
+            for (int r0 = wave * A.per_wave; r0 < rows; r0 += 4 * A.per_wave) {
+                const bool on = works && r < rows;
+                const float2* turns = table + tl * A.pairs;
+                T* orow = out + row_offset(tl, h, S.out_t, S.out_h, A.far);
+                float x[K][2 * N], g[K][2 * N];
+#pragma unroll
+                for (int j = 0; j < K; j++) {
+                    X[j].take(x[j]);
+                    if (MODE == kNormBack) G[j].take(g[j]);
+                }
+                r += 4 * A.per_wave;
+                tl += S.step_tokens;
+                h += S.step_heads;
+                if (h >= S.heads) { h -= S.heads; tl++; }
+                fetch();
                 if (MODE != kRotate) {
+                    float sum = 0.f;
 #pragma unroll
                     for (int j = 0; j < K; j++)
 #pragma unroll
                         for (int i = 0; i < 2 * N; i++) sum = __builtin_fmaf(x[j][i], x[j][i], sum);
-                    sum = group_sum(sum, head, member, width_slots, width);
-                    rms = 1.f / __builtin_sqrtf(sum / (float)A.dim + A.eps);
-                }
-                if (MODE == kNorm) {
-#pragma unroll
-                    for (int j = 0; j < K; j++)
-#pragma unroll
-                        for (int i = 0; i < 2 * N; i++) x[j][i] = x[j][i] * rms * w[j][i];
-                }
-                float (&y)[K][2 * N] = MODE == kNormBack ? g : x;   // what is turned
-#pragma unroll
-                for (int j = 0; j < K; j++)
-#pragma unroll
-                    for (int i = 0; i < N; i++) {
-                        const int p = (member + 64 * j) * N + i, ia = ADJ ? 2 * i : i, ib = ADJ ? 2 * i + 1 : N + i;
-                        if (p < A.pairs) {
-                            const float2 cs = table[tl * A.pairs + p];
-                            const float u = y[j][ia], v = y[j][ib];
-                            y[j][ia] = __builtin_fmaf(u, cs.x, -(v * cs.y));
-                            y[j][ib] = __builtin_fmaf(u, cs.y, v * cs.x);
-                        }
-                    }
-                if (MODE == kNormBack) {
-                    float dot = 0.f;
+                    sum = group_sum(sum, head, member, group);
+                    const float rms = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, A.inv_dim, A.eps));
 #pragma unroll
                     for (int j = 0; j < K; j++)
 #pragma unroll
                         for (int i = 0; i < 2 * N; i++) {
-                            if (on) dw[z][j][i] = __builtin_fmaf(g[j][i], x[j][i] * rms, dw[z][j][i]);
-                            const int at = i < N ? first[j] : second[j];
-                            g[j][i] = at < A.dim ? g[j][i] * w[j][i] : 0.f;
-                            dot = __builtin_fmaf(g[j][i], x[j][i], dot);
+                            x[j][i] *= rms;
+                            if (MODE == kNorm) x[j][i] *= w[j][i];
                         }
-                    dot = group_sum(dot, head, member, width_slots, width);
-                    const float back = dot / (float)A.dim * rms * rms;
+                    if (MODE == kNormBack) {
+                        turn<N, ADJ, K>(g, turns, A, member, on);
+                        float dot = 0.f;
 #pragma unroll
-                    for (int j = 0; j < K; j++)
+                        for (int j = 0; j < K; j++)
 #pragma unroll
-                        for (int i = 0; i < 2 * N; i++) x[j][i] = rms * (g[j][i] - x[j][i] * back);
-                }
+                            for (int i = 0; i < 2 * N; i++) {
+                                if (on) dw[j][i] = __builtin_fmaf(g[j][i], x[j][i], dw[j][i]);
+                                g[j][i] *= w[j][i];
+                                dot = __builtin_fmaf(g[j][i], x[j][i], dot);
+                            }
+                        dot = group_sum(dot, head, member, group) * A.inv_dim;
 #pragma unroll
-                for (int j = 0; j < K; j++)
+                        for (int j = 0; j < K; j++)
 #pragma unroll
-                    for (int half = 0; half < 2; half++) {
-                        const int at = half ? second[j] : first[j];
-                        float v[N];
-#pragma unroll
-                        for (int i = 0; i < N; i++) v[i] = x[j][half * N + i];
-                        if (on && at < A.dim) store_run<T, N>(out + at, v);
+                            for (int i = 0; i < 2 * N; i++) x[j][i] = rms * __builtin_fmaf(-x[j][i], dot, g[j][i]);
                     }
+                }
+                if (MODE != kNormBack) turn<N, ADJ, K>(x, turns, A, member, on);
+                if (on) {
+#pragma unroll
+                    for (int j = 0; j < K; j++) Slot<T, N, ADJ>::store(orow, first[j], second[j], dim, x[j]);
+                }
             }
         }
         __syncthreads();                                       // the table is made anew
     }
 
-    // The weights' gradients: a lane's sums over its rows, then over the groups of a wavefront and the wavefronts in their order.
-    if (MODE == kNormBack) {
+    // The weight's gradient: a lane's sums over its rows, then over the groups of a wavefront and the wavefronts in their order.
+    if (MODE == kNormBack && A.side[side].part) {              // (the same for all)
+        float* part = A.side[side].part;
 #pragma unroll
-        for (int z = 0; z < 2; z++) {
-            float* part = A.side[z].part;
-            if (!part) continue;                               // (the same for all)
+        for (int j = 0; j < K; j++)
 #pragma unroll
-            for (int j = 0; j < K; j++)
-#pragma unroll
-                for (int i = 0; i < 2 * N; i++) {
-                    float v = works ? dw[z][j][i] : 0.f;
-                    if (K == 1) {
-                        float all = 0.f;
-                        for (int q = 0; q < A.per_wave; q++) all += __shfl(v, q * width_slots + member);
-                        v = all;
-                    }
-                    const int at = i < N ? first[j] : second[j];
-                    if (head == 0 && at < A.dim) joined[wave * 512 + at + (i < N ? i : i - N)] = v;
+            for (int i = 0; i < 2 * N; i++) {
+                float v = works ? dw[j][i] : 0.f;
+                if (K == 1) {
+                    float all = 0.f;
+                    for (int q = 0; q < A.per_wave; q++) all += __shfl(v, q * group + member);
+                    v = all;
                 }
-            __syncthreads();
-            for (int e = threadIdx.x; e < A.dim; e += 256)
-                part[(int64_t)blockIdx.x * A.dim + e] = ((joined[e] + joined[512 + e]) + joined[1024 + e]) + joined[1536 + e];
-            __syncthreads();
-        }
+                const int at = i < N ? first[j] : second[j];
+                if (place == 0 && at < dim) joined[wave * 512 + at + (i < N ? i : i - N)] = v;
+            }
+        __syncthreads();
+        for (int e = threadIdx.x; e < dim; e += 256)
+            part[(int64_t)blockIdx.x * dim + e] = ((joined[e] + joined[512 + e]) + joined[1024 + e]) + joined[1536 + e];
+        __syncthreads();
+    }
     }
 }
 
-// Sums [parts][dim] over the parts: a workgroup takes 16 columns of one side, 16 threads to a column, in a fixed order.
+// Sums [parts][dim] over the parts: a workgroup takes 16 columns of one side, 64 threads to a column, in a fixed order.
 struct WeightSums { const float* part[2]; float* out[2]; int parts, dim; };
-__global__ __launch_bounds__(256) void k_weight_sums(WeightSums A) {
-    __shared__ float joined[256];
+__global__ __launch_bounds__(1024) void k_weight_sums(WeightSums A) {
+    __shared__ float joined[1024];
     const int column = threadIdx.x & 15, share = threadIdx.x >> 4, z = blockIdx.y, e = blockIdx.x * 16 + column;
     if (!A.out[z]) return;
     float sum = 0.f;
-    if (e < A.dim)
-        for (int p = share; p < A.parts; p += 16) sum += A.part[z][(int64_t)p * A.dim + e];
+    if (e < A.dim) {
+#pragma unroll 8
+        for (int p = share; p < A.parts; p += 64) sum += A.part[z][(int64_t)p * A.dim + e];
+    }
     joined[threadIdx.x] = sum;
     __syncthreads();
+    if (threadIdx.x < 256) {
+        sum = (sum + joined[threadIdx.x + 256]) + (joined[threadIdx.x + 512] + joined[threadIdx.x + 768]);
+        joined[threadIdx.x] = sum;
+    }
+    __syncthreads();
     if (share == 0 && e < A.dim) {
+#pragma unroll
         for (int q = 1; q < 16; q++) sum += joined[q * 16 + column];
         A.out[z][e] = sum;
     }

@@ -38,14 +38,11 @@ template <typename F> void with_type(int dtype, F f) {
 
 // ---- rotation ----
 
-// Largest run of elements (at most 16 bytes) that every place of a side is a multiple of.
-int run_of(const void* p, const int64_t* strides, int count, size_t size, int most) {
-    uint64_t all = (uint64_t)(uintptr_t)p / size;
-    for (int i = 0; i < count; i++) all |= (uint64_t)strides[i];
-    int n = most;
-    while (n > 1 && all % n) n >>= 1;
-    return n;
+// Whether every place of a side is a multiple of `unit` elements.
+bool aligned(const void* p, int64_t b, int64_t t, int64_t h, size_t size, int unit) {
+    return ((uint64_t)(uintptr_t)p / size | (uint64_t)b | (uint64_t)t | (uint64_t)h) % unit == 0;
 }
+bool within_32(int64_t stride) { return stride >= INT32_MIN && stride <= INT32_MAX; }
 
 int check_rotation(const pcr_heads* q, const pcr_heads* k, const pcr_rotation* R, int dtype, bool back) {
     if (!q || !k || !R || !known_type(dtype)) return PCR_E_ARG;
@@ -81,44 +78,69 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     const pcr_heads* side[2] = {q, k};
     const bool sums = mode == kNormBack && (q->weight_grad || k->weight_grad);
     AxesArgs A = {};
-    A.batch_tokens = R->batch * R->tokens;
-    if (A.batch_tokens > kMaxGrid) return PCR_E_RANGE;
-    int groups = 0;
+    if (R->batch * R->tokens > kMaxGrid) return PCR_E_RANGE;
     const size_t size = type_size(dtype);
-    int N = (int)(16 / size);
+    const bool back = mode == kNormBack;
+    int64_t batch = R->batch, tokens = R->tokens;
+    A.pos_a = R->axis_stride; A.pos_b = R->batch_stride; A.pos_t = R->token_stride;
+    // Sequences whose tokens follow each other at one stride everywhere (always, if they are of one token) are one long sequence.
+    bool one = tokens == 1 || A.pos_b == tokens * A.pos_t;
+    for (const pcr_heads* H : side)
+        if (H->heads && tokens != 1)
+            one = one && H->in_batch == tokens * H->in_token && H->out_batch == tokens * H->out_token && (!back || H->grad_batch == tokens * H->grad_token);
+    one = one && batch > 1;
+    const bool single = one && tokens == 1;                    // the step from token to token is that from sequence to sequence
+    if (single) A.pos_t = A.pos_b;
+    if (one) { tokens *= batch; batch = 1; }
     for (int z = 0; z < 2; z++) {
         const pcr_heads& H = *side[z];
         HeadSide& S = A.side[z];
         S.in = H.in; S.grad = H.grad; S.out = H.out; S.weight = H.weight; S.heads = (int)H.heads;
-        S.in_b = H.in_batch; S.in_t = H.in_token; S.in_h = H.in_head;
-        S.out_b = H.out_batch; S.out_t = H.out_token; S.out_h = H.out_head;
-        S.grad_b = H.grad_batch; S.grad_t = H.grad_token; S.grad_h = H.grad_head;
+        S.in_b = H.in_batch; S.in_t = single ? H.in_batch : H.in_token; S.in_h = H.in_head;
+        S.out_b = H.out_batch; S.out_t = single ? H.out_batch : H.out_token; S.out_h = H.out_head;
+        S.grad_b = H.grad_batch; S.grad_t = single ? H.grad_batch : H.grad_token; S.grad_h = H.grad_head;
         if (!S.heads) continue;
-        const int64_t strides[9] = {S.in_b, S.in_t, S.in_h, S.out_b, S.out_t, S.out_h, S.grad_b, S.grad_t, S.grad_h};
-        N = std::min(N, run_of(H.in, strides, 6, size, N));
-        N = std::min(N, run_of(H.out, strides, 0, size, N));
-        if (mode == kNormBack) N = std::min(N, run_of(H.grad, strides + 6, 3, size, N));
+        A.far |= !within_32(S.in_t) || !within_32(S.in_h) || !within_32(S.out_t) || !within_32(S.out_h) || (back && (!within_32(S.grad_t) || !within_32(S.grad_h)));
     }
-    while (N > 1 && (R->dim % N || (!R->adjacent && R->pairs % N))) N >>= 1;
+    // Runs of up to 16 bytes, as long as heads, pairs and alignment are multiples of them (of two, where those are one in memory).
+    int N = (int)(16 / size);
+    for (; N > 1; N >>= 1) {
+        bool fits = R->pairs % N == 0 && R->dim % (R->adjacent ? 2 * N : N) == 0;
+        const int unit = R->adjacent ? std::min<int>(2 * N, (int)(16 / size)) : N;
+        for (int z = 0; z < 2 && fits; z++) {
+            const HeadSide& S = A.side[z];
+            if (!S.heads) continue;
+            fits = aligned(S.in, S.in_b, S.in_t, S.in_h, size, unit) && aligned(S.out, S.out_b, S.out_t, S.out_h, size, unit) &&
+                   (!back || aligned(S.grad, S.grad_b, S.grad_t, S.grad_h, size, unit));
+        }
+        if (fits) break;
+    }
     A.position = R->position; A.frequency = R->frequency; A.axis = R->axis;
-    A.pos_a = R->axis_stride; A.pos_b = R->batch_stride; A.pos_t = R->token_stride;
-    A.tokens = R->tokens; A.wide = R->wide; A.axes = R->axes; A.dim = R->dim; A.pairs = R->pairs;
-    A.inverse = inverse; A.weight_float = weight_dtype == PCR_FLOAT; A.eps = eps;
+    A.tokens = tokens; A.wide = R->wide; A.axes = R->axes; A.dim = R->dim; A.pairs = R->pairs;
+    A.inverse = inverse; A.weight_float = weight_dtype == PCR_FLOAT; A.eps = eps; A.inv_dim = 1.f / R->dim;
     const int turned = 2 * R->pairs;
     A.slots = R->adjacent ? (R->dim + 2 * N - 1) / (2 * N) : R->pairs / N + (R->dim - turned + 2 * N - 1) / (2 * N);
     A.per_wave = std::max(1, 64 / A.slots);
-    // Tokens of a workgroup: some 128 rows, as many as the table of sines holds, and no more than leave 1024 workgroups.
-    const int64_t heads = std::max<int64_t>(1, q->heads + k->heads);
-    int64_t chunk = std::max<int64_t>(1, 128 / heads);
+    for (HeadSide& S : A.side) {
+        if (!S.heads) continue;
+        S.step_tokens = 4 * A.per_wave / S.heads; S.step_heads = 4 * A.per_wave % S.heads;
+        S.by_heads = (uint32_t)(((1ull << 32) + S.heads - 1) / S.heads);
+    }
+    // Tokens of a workgroup at a time: some 128 rows (a gradient: what its workgroups come to), as many as the table of sines holds, and no more than
+    // leave 1024 workgroups.
+    const int64_t heads = std::max<int64_t>(1, q->heads + k->heads), all = batch * tokens;
+    int64_t chunk = back ? (all + kBackGroups - 1) / kBackGroups : std::min<int64_t>(128 / heads, all / 1024);
     if (R->pairs) chunk = std::min<int64_t>(chunk, kAxesTable / R->pairs);
-    chunk = std::max<int64_t>(1, std::min(chunk, A.batch_tokens / 1024));
+    chunk = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunk, 4096), tokens));
     A.chunk = (int)chunk;
-    A.chunks = (A.batch_tokens + chunk - 1) / chunk;
-    groups = (int)(mode == kNormBack ? std::min<int64_t>(A.chunks, kBackGroups) : A.chunks);
+    A.shares = tokens ? (tokens + chunk - 1) / chunk : 0;
+    A.chunks = batch * A.shares;
+    if (!A.shares) A.shares = 1;
+    int groups = (int)(back ? std::min<int64_t>(A.chunks, kBackGroups) : A.chunks);
     if (sums) {
         size_t need = 0;
-        pcr_norm_rotate_workspace(A.batch_tokens, R->dim, &need);
-        if (A.batch_tokens && (!d_work || work_bytes < need)) return d_work ? PCR_E_RANGE : PCR_E_ARG;
+        pcr_norm_rotate_workspace(all, R->dim, &need);
+        if (all && (!d_work || work_bytes < need)) return d_work ? PCR_E_RANGE : PCR_E_ARG;
         for (int z = 0; z < 2; z++) if (side[z]->weight_grad) A.side[z].part = (float*)d_work + (size_t)z * groups * R->dim;
     }
     const OnDevice on(device);
@@ -148,7 +170,7 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         WeightSums W = {};
         for (int z = 0; z < 2; z++) { W.part[z] = A.side[z].part; W.out[z] = side[z]->weight_grad; }
         W.parts = groups; W.dim = R->dim;
-        hipLaunchKernelGGL(k_weight_sums, dim3((R->dim + 15) / 16, 2), dim3(256), 0, s, W);
+        hipLaunchKernelGGL(k_weight_sums, dim3((R->dim + 15) / 16, 2), dim3(1024), 0, s, W);
     }
     return launched();
 }
