@@ -6,7 +6,8 @@
 //
 // The angle is the 32-bit product of the position and the frequency, each a 32-bit float: what a program gets that multiplies a table of frequencies by
 // positions as tensors, and what weights were trained with, 2^-24 of itself off (0.002 radians at position 32768 in the fastest pair).  From there on
-// nothing is lost: the float becomes a fraction of a turn in 64-bit fixed point, whose upper 32 bits go to sine and cosine of a half-turn's multiple.
+// nothing is lost: the float becomes a fraction of a turn in double precision, or, from 2^20 on, in 64-bit fixed point (all floats so: a rotation of one head
+// of queries and keys, which shares an angle between two rows, took 511 us instead of 386 for 2 million tokens).
 //
 // Bound by memory: every element is read once and written once.  A workgroup takes a few tokens: its lanes make the tokens' sines and cosines once,
 // in LDS, for all heads of both sides; then a row (a head of a token) goes to a group of lanes, a lane holding one slot: a run of pairs, that is
@@ -29,7 +30,7 @@ struct AxesArgs {
     int wide, axes, dim, pairs, inverse, weight_float;
     int far;                                                   // a stride of tokens or heads is outside 32 bits
     int slots, per_wave;                                       // slots of a row; rows of a wavefront (64 / slots, at least 1)
-    int chunk;                                                 // tokens of a workgroup at a time
+    int chunk, table_tokens;                                   // tokens of a workgroup at a time; tokens whose angles it makes at a time (256 / pairs)
     float eps, inv_dim;
 };
 
@@ -51,14 +52,16 @@ __device__ __forceinline__ uint64_t turns_of(float f) {
     return bits >> 31 ? 0 - v : v;
 }
 
-__device__ __forceinline__ float2 turn_of(const AxesArgs& A, int64_t b, int64_t t, int pair) {
-    const int a = min(max(A.axis[pair], 0), A.axes - 1);
-    const int64_t at = a * A.pos_a + b * A.pos_b + t * A.pos_t;
-    const int64_t pos = A.wide ? ((const int64_t*)A.position)[at] : (int64_t)((const int32_t*)A.position)[at];
-    const int32_t phase = (int32_t)(turns_of((float)pos * A.frequency[pair]) >> 32);
+__device__ __forceinline__ float2 turn_of(float angle, int inverse) {
+    float halves;                                              // of a turn, -1 .. 1
+    if (__builtin_fabsf(angle) < 1048576.f) {                  // double precision's 2^-53 of 2^18 turns are below 2^-34 of one
+        double turns = (double)angle * 0.15915494309189533577;
+        turns -= __builtin_rint(turns);
+        halves = 2.f * (float)turns;
+    } else halves = (float)(int32_t)(turns_of(angle) >> 32) * 4.656612873077392578125e-10f;      // 2^-31
     float c, s;
-    sincospif((float)phase * 4.656612873077392578125e-10f, &s, &c);              // 2^-31: in halves of a turn
-    return make_float2(c, A.inverse ? -s : s);
+    sincospif(halves, &s, &c);
+    return make_float2(c, inverse ? -s : s);
 }
 
 template <int CONTROL> __device__ __forceinline__ float across(float v) {
@@ -173,6 +176,18 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
         if (s >= A.slots || first[j] >= dim) first[j] = dim;
         if (s >= A.slots || second[j] >= dim) second[j] = dim;
     }
+    int mine = A.pairs, mine_token = 0;
+    float frequency = 0.f;
+    int64_t mine_position = 0;
+    if (A.pairs) {
+        mine_token = threadIdx.x / A.pairs;
+        if (mine_token < A.table_tokens) {
+            mine = threadIdx.x - mine_token * A.pairs;
+            frequency = A.frequency[mine];
+            mine_position = min(max(A.axis[mine], 0), A.axes - 1) * A.pos_a;
+        }
+    }
+
     // A gradient takes one side after the other, so that the sums of one weight's gradient are held at a time.
 #pragma unroll 1
     for (int side = 0; side < (MODE == kNormBack ? 2 : 1); side++) {
@@ -185,12 +200,14 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
             for (int i = 0; i < 2 * N; i++) dw[j][i] = 0.f;
     }
     for (int64_t chunk = blockIdx.x; chunk < A.chunks; chunk += gridDim.x) {
-        const int64_t b = chunk / A.shares, t0 = (chunk - b * A.shares) * A.chunk;
+        const int64_t b = A.shares == A.chunks ? 0 : chunk / A.shares, t0 = (chunk - b * A.shares) * A.chunk;
         const int here = (int)min((int64_t)A.chunk, A.tokens - t0);
-        for (int e = threadIdx.x; e < here * A.pairs; e += 256) {
-            const int t = e / A.pairs;
-            table[e] = turn_of(A, b, t0 + t, e - t * A.pairs);
-        }
+        if (mine < A.pairs)                                    // a thread makes one pair's angles, of every few tokens
+            for (int t = mine_token; t < here; t += A.table_tokens) {
+                const int64_t at = mine_position + b * A.pos_b + (t0 + t) * A.pos_t;
+                const float position = A.wide ? (float)((const int64_t*)A.position)[at] : (float)((const int32_t*)A.position)[at];
+                table[t * A.pairs + mine] = turn_of(position * frequency, A.inverse);
+            }
         __syncthreads();
 #pragma unroll 1
         for (int z = MODE == kNormBack ? side : 0; z < (MODE == kNormBack ? side + 1 : 2); z++) {

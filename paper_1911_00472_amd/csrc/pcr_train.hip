@@ -102,8 +102,9 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         if (!S.heads) continue;
         A.far |= !within_32(S.in_t) || !within_32(S.in_h) || !within_32(S.out_t) || !within_32(S.out_h) || (back && (!within_32(S.grad_t) || !within_32(S.grad_h)));
     }
-    // Runs of up to 16 bytes, as long as heads, pairs and alignment are multiples of them (of two, where those are one in memory).
-    int N = (int)(16 / size);
+    // Runs of up to 16 bytes, as long as heads, pairs and alignment are multiples of them (of two, where those are one in memory).  A gradient's are of
+    // four elements at most: with eight it has 140 registers, three wavefronts a SIMD (32768 tokens of 40 heads of 128, bfloat: 224 us, and 217).
+    int N = back ? 4 : (int)(16 / size);
     for (; N > 1; N >>= 1) {
         bool fits = R->pairs % N == 0 && R->dim % (R->adjacent ? 2 * N : N) == 0;
         const int unit = R->adjacent ? std::min<int>(2 * N, (int)(16 / size)) : N;
@@ -126,13 +127,14 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         S.step_tokens = 4 * A.per_wave / S.heads; S.step_heads = 4 * A.per_wave % S.heads;
         S.by_heads = (uint32_t)(((1ull << 32) + S.heads - 1) / S.heads);
     }
-    // Tokens of a workgroup at a time: some 128 rows (a gradient: what its workgroups come to), as many as the table of sines holds, and no more than
-    // leave 1024 workgroups.
+    // Tokens of a workgroup at a time: rows of some 32 KB, 128 at least (a gradient: half of what its workgroups come to), as many as the table of sines holds,
+    // and no more than leave 1024 workgroups.  (us with 64 / 128 / 256 / 512 rows: rows of 256 bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)
     const int64_t heads = std::max<int64_t>(1, q->heads + k->heads), all = batch * tokens;
-    int64_t chunk = back ? (all + kBackGroups - 1) / kBackGroups : std::min<int64_t>(128 / heads, all / 1024);
+    int64_t chunk = back ? (all + 2 * kBackGroups - 1) / (2 * kBackGroups) : std::min<int64_t>(std::max<int64_t>(128, 32768 / (R->dim * size)) / heads, all / 1024);
     if (R->pairs) chunk = std::min<int64_t>(chunk, kAxesTable / R->pairs);
     chunk = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunk, 4096), tokens));
     A.chunk = (int)chunk;
+    A.table_tokens = R->pairs ? 256 / R->pairs : 0;
     A.shares = tokens ? (tokens + chunk - 1) / chunk : 0;
     A.chunks = batch * A.shares;
     if (!A.shares) A.shares = 1;
@@ -154,7 +156,7 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
                 constexpr bool ADJ = decltype(adj)::value;
                 if (mode == kRotate) launch_axes<T, M, ADJ, kRotate>(A, groups, s);
                 else if (mode == kNorm) launch_axes<T, M, ADJ, kNorm>(A, groups, s);
-                else launch_axes<T, M, ADJ, kNormBack>(A, groups, s);
+                else if constexpr (M <= 4) launch_axes<T, M, ADJ, kNormBack>(A, groups, s);
             };
             auto by_pairs = [&](auto n) {
                 if (R->adjacent) by_mode(n, std::true_type());
