@@ -64,16 +64,13 @@ __device__ __forceinline__ float2 turn_of(float angle, int inverse) {
     return make_float2(c, inverse ? -s : s);
 }
 
-template <int CONTROL> __device__ __forceinline__ float across(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
-}
 // Sum over a row's group of lanes (`slots` neighbouring ones from `head` on), the same bits in all of them.
 __device__ __forceinline__ float group_sum(float v, int head, int member, int slots) {
     if ((slots & (slots - 1)) == 0) {                          // (the same for all lanes, as what follows)
-        if (slots > 1) v += across<0xb1>(v);                   // the neighbour, the other pair of four, the other four of eight (mirrored), the other eight
-        if (slots > 2) v += across<0x4e>(v);
-        if (slots > 4) v += across<0x141>(v);
-        if (slots > 8) v += across<0x140>(v);
+        if (slots > 1) v += across<kNeighbour>(v);
+        if (slots > 2) v += across<kPairOfFour>(v);
+        if (slots > 4) v += across<kFourOfEight>(v);
+        if (slots > 8) v += across<kEightOfSixteen>(v);
         if (slots > 16) v += __shfl_xor(v, 16);
         if (slots > 32) v += __shfl_xor(v, 32);
         return v;

@@ -6,8 +6,11 @@
 // with delta = -g a T p_k for a kept logit and -g b for the label: the dense part is written first and the few classes with a delta again
 // behind it, every one with the deltas of all entries at its class, in their order.
 //
-// Both sums over a row are made in one pass with a running maximum, in 32 bits, relative to it.  Bound by memory: a row is read once for the
-// loss, and read and written once for the gradient.
+// Sums over a row are made in 32 bits relative to its maximum.  Bound by memory: a row is read once for the loss, and read and written once for loss and
+// gradient: a team of threads holds it in its registers, packed as it came, and makes its exponentials where they are used (k_distill_rows).  Rows too
+// long for that are read with a running maximum and again for the gradient (k_distill), a few long ones in shares (k_distill_part, k_distill_join).
+// us (floor at a large copy's 5.0 TB/s): loss and gradient of 4096 rows of 50001 bfloat logits with labels, T = 2: 178 (164), read twice 323; of 2048 of
+// 131071: 254 (215); of 4096 of 32000: 111 (105); of 8192 of 10000: 69 (66); loss of 8192 rows of 50001: 181 (164), with a running maximum 262.
 #pragma once
 #include "pcr_vec.h"
 
@@ -35,11 +38,7 @@ template <int TEAM> __device__ __forceinline__ void team_sync() {
 }
 // Maximum and sum over a team, the same bits in all of it.  `lds`: a float for every wavefront of the team.
 template <int TEAM, bool MAX> __device__ __forceinline__ float team_join(float v, float* lds) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        const float o = __shfl_xor(v, d);
-        v = MAX ? fmaxf(v, o) : v + o;
-    }
+    v = wave_join<MAX>(v);
     if (TEAM == 64) return v;
     const int wave = threadIdx.x >> 6;
     __syncthreads();
@@ -243,6 +242,188 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
         for (int k = 0; k < E; k++) more += at[k] == (int)v ? delta[k] : 0.f;
         x[0] += more;
         store_run<T, 1>(out + (v - v0), x);
+    }
+}
+
+// Several values at a time, with one barrier: `lds` holds C floats for every wavefront of the team and is used by no other join.
+template <int TEAM, int C, bool MAX> __device__ __forceinline__ void team_join_all(float (&v)[C], float* lds) {
+    constexpr int W = TEAM / 64;
+#pragma unroll
+    for (int i = 0; i < C; i++) v[i] = wave_join<MAX>(v[i]);
+    if (W == 1) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < C; i++) lds[wave * C + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+        float x = lds[lane % W * C + i];
+        if (W > 1) x = both<MAX>(x, across<kNeighbour>(x));
+        if (W > 2) x = both<MAX>(x, across<kPairOfFour>(x));
+        if (W > 4) x = both<MAX>(x, across<kFourOfEight>(x));
+        if (W > 8) x = both<MAX>(x, across<kEightOfSixteen>(x));
+        v[i] = x;
+    }
+}
+
+// exp((x - m) / T) and, where BY is not kOneSum, exp(x - m): by an exponential of its own, or as the second or fourth power of the first (T = 2, 4).
+enum { kOneSum = 1, kTwoSums = 0, kSquare = 2, kFourth = 4 };
+template <int BY> __device__ __forceinline__ void exps(float x, float m, float c, float T, float& e, float& e1) {
+    const float y = (x - m) * c;
+    e = __builtin_amdgcn_exp2f(y);
+    if (BY == kTwoSums) e1 = __builtin_amdgcn_exp2f(y * T);
+    if (BY == kSquare) e1 = e * e;
+    if (BY == kFourth) e1 = (e * e) * (e * e);
+}
+
+// A run's elements, in a way that keeps the compiler from carrying what it made of them before (32 bits an element, their exponentials: twice to four times
+// the registers) to this use.
+template <typename T, typename V, int N> __device__ __forceinline__ void take_again(V& raw, float (&x)[N]) {
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    Words w = __builtin_bit_cast(Words, raw);
+    asm volatile("" : "+v"(w));
+    raw = __builtin_bit_cast(V, w);
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = (float)raw[i];
+}
+
+// Loss (MODE kLoss) or loss and gradient (kStep) of rows that a team of TEAM threads holds in its registers, R runs of 16 bytes a thread: read once, written once.
+template <typename T, int TEAM, int R, int BY, int MODE>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(DistillArgs A) {
+    extern __shared__ float lds[];                             // a team's: joins [6 a wavefront], and of entry e: class, delta, logit
+    constexpr int N = 16 / sizeof(T), W = TEAM / 64;
+    typedef typename Run<T, N>::Vec Vec;
+    const int tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM, E = A.K + 1;
+    const int64_t n = (int64_t)blockIdx.x * (TEAM < 256 ? 256 / TEAM : 1) + team;
+    if (n >= A.rows) return;                                   // (a whole wavefront, or nobody of a workgroup that shares a row)
+    float* join = lds + team * (6 * W + 3 * E);
+    int* at = (int*)(join + 6 * W);
+    float* delta = join + 6 * W + E;
+    float* logit = delta + E;
+    const T* z = (const T*)A.logits + n * A.row_stride;
+    T* out = MODE == kStep ? (T*)A.out + n * A.out_stride : nullptr;
+    const float g = MODE == kStep ? A.row_grad[n] : 1.f, c = A.inv_T * kLog2e;
+    if (MODE == kStep && g == 0.f) {
+        write_zeros<T, TEAM>(out, A.V, tid);
+        if (tid == 0) A.loss[n] = 0.f;
+        return;
+    }
+    const int V = (int)A.V, lead = min(V, (int)((-(uintptr_t)z & 15) / sizeof(T))), runs = (V - lead) / N, tail = lead + runs * N;
+    Vec raw[R];
+    Vec least;
+#pragma unroll
+    for (int i = 0; i < N; i++) least[i] = (T)-INFINITY;
+    const T* body = z + lead;
+#pragma unroll
+    for (int u = 0; u < R; u++) raw[u] = tid + u * TEAM < runs ? reinterpret_cast<const Vec*>(body)[tid + u * TEAM] : least;
+    const int edge = tid < lead ? tid : tail + tid - lead;     // the elements in front of and behind the runs: one of some threads
+    const bool edged = edge < V;
+    const float x_edge = edged ? (float)z[edge] : -INFINITY;
+    const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
+    const bool labelled = label >= 0 && label < A.V;
+    const float zl = labelled ? (float)z[label] : 0.f;
+
+    float most[2] = {x_edge, -INFINITY};                       // of the logits, of the kept teacher's logits
+    for (int k = tid; k < A.K; k += TEAM) {
+        const int64_t v = A.a != 0.f ? top_class(A, n * A.K + k) : -1;
+        const float t = v >= 0 ? top_logit(A, n * A.K + k) * A.inv_T : -INFINITY;
+        at[k] = t == -INFINITY ? -1 : (int)v;
+        delta[k] = t;
+        logit[k] = t == -INFINITY ? 0.f : (float)z[v];
+        most[1] = fmaxf(most[1], t == t ? t : INFINITY);       // (of a NaN all that follows is one)
+    }
+#pragma unroll
+    for (int u = 0; u < R; u++)
+#pragma unroll
+        for (int i = 0; i < N; i++) most[0] = fmaxf(most[0], (float)raw[u][i]);
+    team_join_all<TEAM, 2, true>(most, join);
+    const float m = most[0];
+    const bool kept = most[1] != -INFINITY;
+    if (MODE == kStep && !kept && !labelled) {
+        write_zeros<T, TEAM>(out, A.V, tid);
+        if (tid == 0) A.loss[n] = 0.f;
+        return;
+    }
+    float sum[3] = {0.f, 0.f, 0.f};                            // of exp((z - m) / T), of exp(z - m), of the teacher's
+    auto add = [&](float x) {
+        float e, e1 = 0.f;
+        exps<BY>(x, m, c, A.T, e, e1);
+        sum[0] += e;
+        sum[1] += e1;
+    };
+#pragma unroll
+    for (int u = 0; u < R; u++) {
+        if (u * TEAM < runs) {                                 // (the same for the team)
+            float x[N];
+            take_again<T>(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < N; i++) add(x[i]);
+        }
+    }
+    if (edged) add(x_edge);
+    for (int k = tid; k < A.K; k += TEAM) if (at[k] >= 0) sum[2] += __builtin_amdgcn_exp2f((delta[k] - most[1]) * kLog2e);
+    team_join_all<TEAM, 3, false>(sum, join + 2 * W);
+    if (BY == kOneSum) sum[1] = sum[0];
+    const float total = sum[2], L = m * A.inv_T, log_s = logf(sum[0]), log_s1 = logf(sum[1]), log_total = logf(total);
+    const float unit = -g * A.a * A.T;
+    const float ca = kept ? -unit / sum[0] : 0.f, cb = labelled ? g * A.b / sum[1] : 0.f;
+
+    // entries: their share of the loss, and what each adds to the dense part of its class
+    auto finish = [&](float entries) {                         // the row's loss, from the sum of the entries' shares
+        float all = kept ? A.a * A.T * A.T * (entries / total) : 0.f;
+        if (labelled) all += A.b * (log_s1 - (zl - m));
+        A.loss[n] = g * all;
+    };
+    float loss[1] = {0.f};
+    for (int k = tid; k < A.K; k += TEAM) {
+        float d = 0.f;
+        if (at[k] >= 0) {
+            const float t = delta[k] - most[1], e = __builtin_amdgcn_exp2f(t * kLog2e);
+            if (e > 0.f || t != t) loss[0] += e * ((t - log_total) - ((logit[k] * A.inv_T - L) - log_s));
+            d = unit * (e / total);
+        }
+        delta[k] = d;
+    }
+    if (MODE == kLoss) {
+        team_join_all<TEAM, 1, false>(loss, join + 5 * W);
+        if (tid == 0) {
+            finish(loss[0]);
+            A.sums[2 * n] = L + log_s;
+            A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f;
+        }
+        return;
+    }
+    if (tid == 0) { at[A.K] = labelled ? (int)label : -1; delta[A.K] = -g * A.b; logit[A.K] = zl; }
+
+    auto dense = [&](float x) {
+        float e, e1 = 0.f;
+        exps<BY>(x, m, c, A.T, e, e1);
+        if (BY == kOneSum) return (ca + cb) * e;
+        if (BY == kSquare) return e * __builtin_fmaf(cb, e, ca);
+        return __builtin_fmaf(cb, e1, ca * e);
+    };
+    T* to = out + lead;
+#pragma unroll
+    for (int u = 0; u < R; u++)
+        if (tid + u * TEAM < runs) {
+            float x[N];
+            take_again<T>(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = dense(x[i]);
+            store_run<T, N>(to + (tid + u * TEAM) * N, x);
+        }
+    if (edged) out[edge] = (T)dense(x_edge);
+    team_join_all<TEAM, 1, false>(loss, join + 5 * W);         // (the dense part and the entries are behind this barrier, too)
+    team_sync<TEAM>();
+    if (tid == 0) finish(loss[0]);
+    for (int e = tid; e < E; e += TEAM) {
+        const int v = at[e];
+        if (v < 0) continue;
+        float more = 0.f;
+        for (int k = 0; k < E; k++) more += at[k] == v ? delta[k] : 0.f;
+        out[v] = (T)(dense(logit[e]) + more);
     }
 }
 

@@ -179,10 +179,21 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
 
 // ---- distillation ----
 
-// Shares of a row: with few rows, as many as fill the chip with some 2048 workgroups, none below 8192 classes.
-int64_t shares_of(int64_t rows, int64_t V) {
+// Shares that a few rows are cut into: as many as fill the chip with some 2048 workgroups, none below 8192 classes.
+int64_t parts_of(int64_t rows, int64_t V) {
     if (rows <= 0 || rows >= 512) return 1;
     return std::max<int64_t>(1, std::min<int64_t>(2048 / rows, V / 8192));
+}
+// Classes of a row that a team of 1024 threads holds in its registers.
+constexpr int kMostRuns = 19;
+int64_t most_held(size_t size) { return 1024 * kMostRuns * (int64_t)(16 / size); }
+// Whether a loss (or a loss with its gradient) over few rows is made of shares of a row.  us, held / in shares, of rows of bfloat logits:
+//                        1 row       24 rows      64 rows     128 rows
+//   loss  65000      7.3/ 9.1     7.9/ 9.1     8.3/ 9.0     9.3/ 9.9      131071  10.5/ 8.8    10.8/ 8.8    12.0/10.3    14.6/13.1  (256 of 100000: 16.6/17.8)
+//   step  65000     12.0/12.3    12.6/13.7    13.8/16.3    15.2/19.9      131071  18.1/12.4    19.1/15.9    21.5/20.6    24.2/28.0
+bool in_shares(int64_t rows, int64_t V, size_t size, bool step) {
+    if (parts_of(rows, V) == 1) return false;
+    return V > most_held(size) || (V * (int64_t)size > 131072 && rows <= (step ? 64 : 128));
 }
 
 int check_distill(const pcr_distill* d) {
@@ -203,6 +214,11 @@ DistillArgs distill_args(const pcr_distill* d) {
     return A;
 }
 
+void cut(DistillArgs& A, int64_t parts) {
+    A.chunk = ((A.V + parts - 1) / parts + 63) / 64 * 64;
+    A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+}
+
 template <typename T, int TEAM, int MODE> void launch_team(const DistillArgs& A, hipStream_t s) {
     const int teams = TEAM < 256 ? 256 / TEAM : 1, threads = TEAM < 256 ? 256 : TEAM;
     const unsigned groups = (unsigned)((A.rows * A.chunks + teams - 1) / teams);
@@ -210,19 +226,43 @@ template <typename T, int TEAM, int MODE> void launch_team(const DistillArgs& A,
     if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(threads), lds, s, A);
     else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(threads), lds, s, A);
 }
+// The gradient from saved sums, and (MODE kLoss, kStep) rows too long for a team's registers, read twice.
 template <int MODE> void launch_distill(const DistillArgs& A, int dtype, hipStream_t s) {
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const int64_t bytes = std::min(A.chunk, A.V) * (int64_t)sizeof(T);
-        if (bytes <= 8192) launch_team<T, 64, MODE>(A, s);
-        else if (bytes <= 65536) launch_team<T, 256, MODE>(A, s);
-        else launch_team<T, 1024, MODE>(A, s);
+        if constexpr (MODE == kGrad) {
+            if (bytes <= 8192) return launch_team<T, 64, MODE>(A, s);
+            if (bytes <= 65536) return launch_team<T, 256, MODE>(A, s);
+        }
+        launch_team<T, 1024, MODE>(A, s);
     });
 }
+// A team that holds a row in its registers, the smallest there is: false if there is none.
+template <typename T, int TEAM, int R, int MODE> bool launch_rows(const DistillArgs& A, hipStream_t s) {
+    constexpr int N = 16 / sizeof(T);
+    if (A.V > (int64_t)TEAM * R * N) return false;             // (elements in front of and behind the runs are held beside them)
+    const int teams = TEAM < 256 ? 256 / TEAM : 1, threads = TEAM < 256 ? 256 : TEAM;
+    const dim3 groups((unsigned)((A.rows + teams - 1) / teams));
+    const size_t lds = (size_t)teams * (6 * (TEAM / 64) + 3 * (A.K + 1)) * sizeof(float);
+    if (!A.two || A.T == 1.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kOneSum, MODE>), groups, dim3(threads), lds, s, A);
+    else if (A.T == 2.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kSquare, MODE>), groups, dim3(threads), lds, s, A);
+    else if (A.T == 4.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kFourth, MODE>), groups, dim3(threads), lds, s, A);
+    else hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kTwoSums, MODE>), groups, dim3(threads), lds, s, A);
+    return true;
+}
+template <int MODE> bool launch_resident(const DistillArgs& A, int dtype, hipStream_t s) {
+    bool held = false;
+    with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        held = launch_rows<T, 64, 4, MODE>(A, s) || launch_rows<T, 64, 8, MODE>(A, s) || launch_rows<T, 256, 4, MODE>(A, s) || launch_rows<T, 256, 8, MODE>(A, s) ||
+               launch_rows<T, 512, 8, MODE>(A, s) || launch_rows<T, 512, 16, MODE>(A, s) || launch_rows<T, 1024, 16, MODE>(A, s) || launch_rows<T, 1024, kMostRuns, MODE>(A, s);
+    });
+    return held;
+}
 // The sums of rows in shares, and the loss.
-void launch_shares(DistillArgs A, int64_t shares, int dtype, hipStream_t s) {
-    A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
-    A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+void launch_shares(DistillArgs A, int64_t parts, int dtype, hipStream_t s) {
+    cut(A, parts);
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const unsigned groups = (unsigned)(A.rows * A.chunks);
@@ -236,10 +276,10 @@ void launch_shares(DistillArgs A, int64_t shares, int dtype, hipStream_t s) {
     });
 }
 
-int check_work(int64_t rows, int64_t V, void* d_work, size_t work_bytes) {
+int check_work(bool shares, int64_t rows, int64_t V, void* d_work, size_t work_bytes) {
+    if (!shares) return PCR_OK;
     size_t need = 0;
     pcr_distill_workspace(rows, V, &need);
-    if (!need) return PCR_OK;
     return !d_work ? PCR_E_ARG : work_bytes < need ? PCR_E_RANGE : PCR_OK;
 }
 
@@ -314,23 +354,24 @@ int pcr_norm_rotate_backward(int device_id, const pcr_heads* q, const pcr_heads*
 int pcr_distill_workspace(int64_t rows, int64_t classes, size_t* nbytes) {
     if (!nbytes) return PCR_E_ARG;
     if (rows < 0 || classes < 1) return PCR_E_RANGE;
-    const int64_t shares = shares_of(rows, classes);
-    *nbytes = shares > 1 ? (size_t)rows * (3 * shares + 2) * sizeof(float) : 0;
+    const bool shares = in_shares(rows, classes, 2, false) || in_shares(rows, classes, 4, false);     // (of a step as well: its rows are fewer)
+    *nbytes = shares ? (size_t)rows * (3 * parts_of(rows, classes) + 2) * sizeof(float) : 0;
     return PCR_OK;
 }
 
 int pcr_distill_forward(int device_id, const pcr_distill* d, float* loss, float* sums, void* d_work, size_t work_bytes, void* hip_stream) {
     int rc = check_distill(d);
-    if (!rc && d->rows && (!loss || !sums)) rc = PCR_E_ARG;
-    if (!rc) rc = check_work(d->rows, d->classes, d_work, work_bytes);
+    if (rc) return rc;
+    if (d->rows && (!loss || !sums)) return PCR_E_ARG;
+    const bool shares = in_shares(d->rows, d->classes, type_size(d->dtype), false);
+    rc = check_work(shares, d->rows, d->classes, d_work, work_bytes);
     if (rc || !d->rows) return rc;
     DistillArgs A = distill_args(d);
     A.loss = loss; A.sums = sums; A.part = (float*)d_work;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
-    const int64_t shares = shares_of(A.rows, A.V);
-    if (shares > 1) launch_shares(A, shares, d->dtype, (hipStream_t)hip_stream);
-    else launch_distill<kLoss>(A, d->dtype, (hipStream_t)hip_stream);
+    if (shares) launch_shares(A, parts_of(A.rows, A.V), d->dtype, (hipStream_t)hip_stream);
+    else if (!launch_resident<kLoss>(A, d->dtype, (hipStream_t)hip_stream)) launch_distill<kLoss>(A, d->dtype, (hipStream_t)hip_stream);
     return launched();
 }
 
@@ -340,9 +381,7 @@ int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums,
     if (rc || !d->rows) return rc;
     DistillArgs A = distill_args(d);
     A.sums_in = sums; A.row_grad = row_grad; A.out = out; A.out_stride = out_stride;
-    const int64_t shares = shares_of(A.rows, A.V);
-    A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
-    A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+    cut(A, parts_of(A.rows, A.V));
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
     launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
@@ -352,23 +391,24 @@ int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums,
 int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weight, float* loss, void* out, int64_t out_stride, void* d_work,
                      size_t work_bytes, void* hip_stream) {
     int rc = check_distill(d);
-    if (!rc && d->rows && (!row_weight || !loss || !out)) rc = PCR_E_ARG;
-    if (!rc) rc = check_work(d->rows, d->classes, d_work, work_bytes);
+    if (rc) return rc;
+    if (d->rows && (!row_weight || !loss || !out)) return PCR_E_ARG;
+    const bool shares = in_shares(d->rows, d->classes, type_size(d->dtype), true);
+    rc = check_work(shares, d->rows, d->classes, d_work, work_bytes);
     if (rc || !d->rows) return rc;
     DistillArgs A = distill_args(d);
     A.row_grad = row_weight; A.loss = loss; A.out = out; A.out_stride = out_stride;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
-    const int64_t shares = shares_of(A.rows, A.V);
-    if (shares > 1) {
+    if (shares) {
+        const int64_t parts = parts_of(A.rows, A.V);
         A.part = (float*)d_work;
-        A.sums = A.part + 3 * A.rows * shares;
-        launch_shares(A, shares, d->dtype, (hipStream_t)hip_stream);
+        A.sums = A.part + 3 * A.rows * parts;
+        launch_shares(A, parts, d->dtype, (hipStream_t)hip_stream);
         A.sums_in = A.sums;
-        A.chunk = ((A.V + shares - 1) / shares + 63) / 64 * 64;
-        A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
+        cut(A, parts);
         launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
-    } else launch_distill<kStep>(A, d->dtype, (hipStream_t)hip_stream);
+    } else if (!launch_resident<kStep>(A, d->dtype, (hipStream_t)hip_stream)) launch_distill<kStep>(A, d->dtype, (hipStream_t)hip_stream);
     return launched();
 }
 

@@ -36,6 +36,22 @@ template <typename T, int N> __device__ __forceinline__ void store_run(T* p, con
     reinterpret_cast<typename Run<T, N>::Loose*>(p)->v = v;
 }
 
+// v of another lane: the neighbour's, one of the other pair of four lanes, of the other four of eight, of the other eight of sixteen (the last two mirrored).
+enum { kNeighbour = 0xb1, kPairOfFour = 0x4e, kFourOfEight = 0x141, kEightOfSixteen = 0x140 };
+template <int FROM> __device__ __forceinline__ float across(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), FROM, 0xf, 0xf, true));
+}
+// Maximum or sum over a wavefront, the same bits in all lanes.
+template <bool MAX> __device__ __forceinline__ float both(float a, float b) { return MAX ? fmaxf(a, b) : a + b; }
+template <bool MAX> __device__ __forceinline__ float wave_join(float v) {
+    v = both<MAX>(v, across<kNeighbour>(v));
+    v = both<MAX>(v, across<kPairOfFour>(v));
+    v = both<MAX>(v, across<kFourOfEight>(v));
+    v = both<MAX>(v, across<kEightOfSixteen>(v));
+    v = both<MAX>(v, __shfl_xor(v, 16));
+    return both<MAX>(v, __shfl_xor(v, 32));
+}
+
 inline bool known_type(int dtype) { return dtype >= 0 && dtype <= 2; }
 inline size_t type_size(int dtype) { return dtype == 0 ? 4 : 2; }
 
