@@ -75,6 +75,7 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     if (rc) return rc;
     if (mode != kRotate && !known_type(weight_dtype)) return PCR_E_ARG;
     if (mode != kRotate && weight_dtype != PCR_FLOAT && weight_dtype != dtype) return PCR_E_ARG;
+    if (mode != kRotate && !(eps >= 0.f && isfinite(eps))) return PCR_E_RANGE;
     const pcr_heads* side[2] = {q, k};
     const bool sums = mode == kNormBack && (q->weight_grad || k->weight_grad);
     AxesArgs A = {};
@@ -100,6 +101,9 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         S.out_b = H.out_batch; S.out_t = single ? H.out_batch : H.out_token; S.out_h = H.out_head;
         S.grad_b = H.grad_batch; S.grad_t = single ? H.grad_batch : H.grad_token; S.grad_h = H.grad_head;
         if (!S.heads) continue;
+        if (batch == 1) S.in_b = S.out_b = S.grad_b = 0;       // (steps that are never taken neither move nor misalign anything)
+        if (tokens == 1) S.in_t = S.out_t = S.grad_t = 0;
+        if (S.heads == 1) S.in_h = S.out_h = S.grad_h = 0;
         A.far |= !within_32(S.in_t) || !within_32(S.in_h) || !within_32(S.out_t) || !within_32(S.out_h) || (back && (!within_32(S.grad_t) || !within_32(S.grad_h)));
     }
     // Runs of up to 16 bytes, as long as heads, pairs and alignment are multiples of them (of two, where those are one in memory).  A gradient's are of
@@ -310,7 +314,7 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
     A.by_each = (uint32_t)(((1ull << 32) + each - 1) / each);
     // Rows of a workgroup: some 512 runs of eight pixels (256 where elements have 32 bits).  Stores go through LDS where lines are not of whole runs and a row fits there.
     const size_t row_bytes = (size_t)channels * patch * patch * type_size(dtype);
-    const bool staged = patch % 8 && row_bytes <= 65536;
+    const bool staged = patch % 8 && row_bytes <= 61440;
     int64_t group = (dtype == PCR_FLOAT ? 256 : 512) / each;
     if (staged) group = std::min<int64_t>(group, 20480 / row_bytes);
     A.group = (int)std::max<int64_t>(1, std::min<int64_t>(group, kPatchGroup));

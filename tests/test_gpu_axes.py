@@ -191,6 +191,38 @@ def test_in_place_and_broadcast_gradients():
     assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
+def test_a_stream_that_is_named():
+    gen = generator(15)
+    positions, frequency, axis = setting(32, 3, 4, 64, gen)
+    q, k = make(4, 64, 8, 2, 64, torch.bfloat16, "split", gen)
+    gq, gk = make(4, 64, 8, 2, 64, torch.bfloat16, "split", gen)
+    w = torch.randn(64, generator=gen, device="cuda")
+    want = pkg.norm_rotate_backward(gq, gk, q, k, w, w, positions, frequency, axis)
+    side = torch.cuda.Stream()
+    for stream in (side.cuda_stream, 0):
+        side.wait_stream(torch.cuda.current_stream())
+        got = pkg.norm_rotate_backward(gq, gk, q, k, w, w, positions, frequency, axis, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_sequences_that_are_one_and_sequences_that_are_not():
+    """Sequences whose tokens follow each other at one stride are taken as one; with another order of memory, shared positions or a gap between
+    sequences they are not: the results are the same."""
+    gen = generator(16)
+    for T in (1, 37):
+        positions, frequency, axis = setting(24, 2, 9, T, gen)
+        q, k = make(9, T, 3, 1, 48, torch.float16, "split", gen)
+        want = pkg.norm_rotate(q, k, None, None, positions, frequency, axis)
+        wide = torch.zeros((9, T + 5, 3, 48), dtype=torch.float16, device="cuda")
+        wide[:, 2:2 + T] = q
+        assert torch.equal(pkg.norm_rotate(wide[:, 2:2 + T], k, None, None, positions, frequency, axis)[0], want[0])
+        across = q.transpose(0, 1).contiguous().transpose(0, 1)
+        assert torch.equal(pkg.norm_rotate(across, k, None, None, positions.transpose(1, 2).contiguous().transpose(1, 2), frequency, axis)[0], want[0])
+        shared = positions[:, :1].expand(2, 9, T)
+        assert torch.equal(pkg.norm_rotate(q, k, None, None, shared[:, 0], frequency, axis)[1], pkg.norm_rotate(q, k, None, None, shared.contiguous(), frequency, axis)[1])
+
+
 def test_no_tokens_and_no_heads():
     positions, frequency, axis = setting(8, 2, 1, 0, generator(9))
     w = torch.ones(16, device="cuda")

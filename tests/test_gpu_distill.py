@@ -121,6 +121,25 @@ def test_sizes_and_types(N, V, K, dtype):
         check_all(z, index, t, None, 1.5, 2.0, 1.0)
 
 
+@pytest.mark.parametrize("N,V,dtype", [(3, 156001, torch.bfloat16), (514, 78003, torch.float32), (514, 156001, torch.float16), (130, 155648, torch.bfloat16), (129, 66001, torch.float16),
+                                       (70, 33000, torch.float32), (64, 40001, torch.float32), (1, 300007, torch.bfloat16)])
+def test_long_rows(N, V, dtype):
+    """Rows around what a team of threads holds, few (made in shares) and many."""
+    z, index, t, labels = make(N, V, 9, dtype, N + V)
+    check_all(z, index, t, labels, 2.0, 0.7, 0.3)
+    if N < 10:
+        check_all(z, index, t, None, 3.0, 1.0, 0.0)
+        check_all(z, index, t, labels, 4.0, 0.5, 0.5)
+
+
+@pytest.mark.parametrize("V,top", [(999, 1024), (5000, 600), (70000, 300), (200, 1)])
+def test_many_entries_and_powers_of_the_exponential(V, top):
+    """T = 2 and T = 4, where exp(z - m) is a power of exp((z - m) / T), beside T close to them; more entries than threads of a team."""
+    z, index, t, labels = make(6, V, top, torch.bfloat16, V)
+    for T in (2.0, 4.0, 1.9999, 4.0001, 1.0):
+        check_all(z, index, t, labels, T, 0.5, 0.5)
+
+
 @pytest.mark.parametrize("V", [200, 5000, 40000])
 def test_entries_that_do_not_count_classes_kept_twice_and_other_types(V):
     for kind, top_dtype, dtype in ((torch.int64, torch.float32, torch.bfloat16), (torch.int32, torch.bfloat16, torch.float32), (torch.int64, torch.float16, torch.float16)):

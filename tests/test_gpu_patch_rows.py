@@ -45,7 +45,8 @@ def check(got, positions, want, places):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
-@pytest.mark.parametrize("C,P,m,frames", [(3, 14, 1, 1), (3, 16, 2, 4), (1, 8, 1, 3), (3, 7, 3, 1), (1, 5, 2, 2), (3, 1, 1, 1), (3, 28, 1, 1), (3, 128, 1, 1), (1, 16, 16, 1)])
+@pytest.mark.parametrize("C,P,m,frames", [(3, 14, 1, 1), (3, 16, 2, 4), (1, 8, 1, 3), (3, 7, 3, 1), (1, 5, 2, 2), (3, 1, 1, 1), (3, 28, 1, 1), (3, 128, 1, 1), (1, 16, 16, 1), (3, 100, 1, 1), (3, 101, 1, 1),
+                                          (1, 127, 1, 1), (3, 24, 2, 1), (3, 9, 1, 7), (1, 2, 1, 1)])
 def test_rows_and_positions(C, P, m, frames, dtype):
     rng = np.random.default_rng(P * 10 + m)
     total = sum(h * w * C for h, w in SIZES)
