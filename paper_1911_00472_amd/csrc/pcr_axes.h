@@ -6,8 +6,9 @@
 //
 // The angle is the 32-bit product of the position and the frequency, each a 32-bit float: what a program gets that multiplies a table of frequencies by
 // positions as tensors, and what weights were trained with, 2^-24 of itself off (0.002 radians at position 32768 in the fastest pair).  From there on
-// nothing is lost: the float becomes a fraction of a turn in double precision, or, from 2^20 on, in 64-bit fixed point (all floats so: a rotation of one head
-// of queries and keys, which shares an angle between two rows, took 511 us instead of 386 for 2 million tokens).
+// nothing is lost: the float is reduced to an eighth of a turn with a constant of 48 bits, or, from 2^20 on, in 64-bit fixed point.  (Fixed point for all
+// of them and the compiler's sine and cosine took 511 us for 2 million tokens of one head of queries and keys, which share an angle between two rows;
+// double precision and that 386, this 367.)
 //
 // Bound by memory: every element is read once and written once.  A workgroup takes a few tokens: its lanes make the tokens' sines and cosines once,
 // in LDS, for all heads of both sides; then a row (a head of a token) goes to a group of lanes, a lane holding one slot: a run of pairs, that is
@@ -52,16 +53,26 @@ __device__ __forceinline__ uint64_t turns_of(float f) {
     return bits >> 31 ? 0 - v : v;
 }
 
+// Cosine and sine of an angle, the sine's sign turned over for an inverse.  The angle becomes quarter turns and r, the rest as half-turns (-1/4 .. 1/4): the
+// constant 1 / (2 pi) in two floats (2^-48 of it is missing, 2^-30 turns at 2^20 radians), the products in fused operations, the rest off by 2^-27 turns;
+// sin(pi r) / r and (cos(pi r) - 1) / r^2 are polynomials of third degree in r^2, fitted to least maximal error over that range (10^-9).
 __device__ __forceinline__ float2 turn_of(float angle, int inverse) {
-    float halves;                                              // of a turn, -1 .. 1
-    if (__builtin_fabsf(angle) < 1048576.f) {                  // double precision's 2^-53 of 2^18 turns are below 2^-34 of one
-        double turns = (double)angle * 0.15915494309189533577;
-        turns -= __builtin_rint(turns);
-        halves = 2.f * (float)turns;
-    } else halves = (float)(int32_t)(turns_of(angle) >> 32) * 4.656612873077392578125e-10f;      // 2^-31
-    float c, s;
-    sincospif(halves, &s, &c);
-    return make_float2(c, inverse ? -s : s);
+    float rest, quarters;
+    if (__builtin_fabsf(angle) < 1048576.f) {
+        quarters = __builtin_rintf(angle * 0.63661974668502807617f);
+        rest = __builtin_fmaf(angle, 6.4206382432985265e-9f, __builtin_fmaf(angle, 0.15915493667125701904f, -0.25f * quarters));
+    } else {
+        const uint64_t turns = turns_of(angle);
+        quarters = (float)(uint32_t)((turns + (1ull << 61)) >> 62);
+        rest = (float)((int64_t)(turns - ((uint64_t)(uint32_t)quarters << 62)) >> 32) * 2.3283064365386962891e-10f;      // 2^-32
+    }
+    const float r = rest + rest, u = r * r;
+    const float sine = r * __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(-0.5876994729042053f, u, 2.5496182441711426f), u, -5.167703151702881f), u, 3.141592502593994f);
+    const float cosine = __builtin_fmaf(u, __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(0.2313908338546753f, u, -1.3350543975830078f), u, 4.0587077140808105f), u, -4.934802055358887f), 1.f);
+    const uint32_t q = (uint32_t)(int32_t)quarters;
+    const uint32_t s = __float_as_uint(q & 1 ? cosine : sine) ^ ((q & 2) << 30) ^ (inverse ? 0x80000000u : 0);
+    const uint32_t c = __float_as_uint(q & 1 ? sine : cosine) ^ (((q + 1) & 2) << 30);
+    return make_float2(__uint_as_float(c), __uint_as_float(s));
 }
 
 // Sum over a row's group of lanes (`slots` neighbouring ones from `head` on), the same bits in all of them.
