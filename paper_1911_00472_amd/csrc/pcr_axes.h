@@ -29,6 +29,7 @@ struct AxesArgs {
     const void* position; const float* frequency; const int32_t* axis;
     int64_t pos_a, pos_b, pos_t, tokens, shares, chunks;       // shares: chunks of a sequence
     int wide, axes, dim, pairs, inverse, weight_float;
+    int apart;                                                 // the sides have workgroups of their own (blockIdx.y)
     int far;                                                   // a stride of tokens or heads is outside 32 bits
     int slots, per_wave;                                       // slots of a row; rows of a wavefront (64 / slots, at least 1)
     int chunk, table_tokens;                                   // tokens of a workgroup at a time; tokens whose angles it makes at a time (256 / pairs)
@@ -196,9 +197,10 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
         }
     }
 
-    // A gradient takes one side after the other, so that the sums of one weight's gradient are held at a time.
+    // Few tokens: a workgroup takes one side.  A gradient takes one side after the other, so that the sums of one weight's gradient are held at a time.
+    const int from = A.apart ? blockIdx.y : 0, to = A.apart ? from + 1 : 2;
 #pragma unroll 1
-    for (int side = 0; side < (MODE == kNormBack ? 2 : 1); side++) {
+    for (int side = from; side < (MODE == kNormBack ? to : from + 1); side++) {
     float dw[K][2 * N];
     if (MODE == kNormBack) {
         if (!A.side[side].heads && !A.side[side].part) continue;
@@ -210,20 +212,30 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
     for (int64_t chunk = blockIdx.x; chunk < A.chunks; chunk += gridDim.x) {
         const int64_t b = A.shares == A.chunks ? 0 : chunk / A.shares, t0 = (chunk - b * A.shares) * A.chunk;
         const int here = (int)min((int64_t)A.chunk, A.tokens - t0);
-        if (mine < A.pairs)                                    // a thread makes one pair's angles, of every few tokens
-            for (int t = mine_token; t < here; t += A.table_tokens) {
-                const int64_t at = mine_position + b * A.pos_b + (t0 + t) * A.pos_t;
-                const float position = A.wide ? (float)((const int64_t*)A.position)[at] : (float)((const int32_t*)A.position)[at];
-                table[t * A.pairs + mine] = turn_of(position * frequency, A.inverse);
+        float w[K][2 * N];
+        Slot<T, N, ADJ> X[K], G[K];
+        int rows, r, tl, h;
+        auto fetch = [&](const HeadSide& S) {
+            if (works && r < rows) {
+                const T* row = (const T*)S.in + b * S.in_b + t0 * S.in_t + row_offset(tl, h, S.in_t, S.in_h, A.far);
+                const T* grow = (const T*)S.grad + b * S.grad_b + t0 * S.grad_t + row_offset(tl, h, S.grad_t, S.grad_h, A.far);
+#pragma unroll
+                for (int j = 0; j < K; j++) {
+                    X[j].load(row, first[j], second[j], dim);
+                    if (MODE == kNormBack) G[j].load(grow, first[j], second[j], dim);
+                }
             }
-        __syncthreads();
-#pragma unroll 1
-        for (int z = MODE == kNormBack ? side : 0; z < (MODE == kNormBack ? side + 1 : 2); z++) {
-            const HeadSide& S = A.side[z];
-            const int rows = here * S.heads;
-            if (!rows) continue;
-            float w[K][2 * N];
-            if (MODE != kRotate) {
+        };
+        // A side's weights and its first rows.  A wavefront's rows are per_wave ones side by side, then those 4 per_wave further on.
+        auto begin = [&](const HeadSide& S) {
+            rows = here * S.heads;
+            r = wave * A.per_wave + place;
+            tl = S.heads == 1 ? r : (int)__umulhi((uint32_t)r, S.by_heads);
+            h = r - tl * S.heads;
+#pragma unroll
+            for (int j = 0; j < K; j++) { X[j].clear(); G[j].clear(); }
+            fetch(S);
+            if (MODE != kRotate && S.heads) {
 #pragma unroll
                 for (int j = 0; j < K; j++) {
                     float x[N], y[N];
@@ -235,27 +247,20 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
                     for (int i = 0; i < N; i++) { w[j][i] = x[i]; w[j][N + i] = y[i]; }
                 }
             }
-            const T* in = (const T*)S.in + b * S.in_b + t0 * S.in_t;
-            const T* gin = (const T*)S.grad + b * S.grad_b + t0 * S.grad_t;
+        };
+        begin(A.side[side]);
+        if (mine < A.pairs)                                    // a thread makes one pair's angles, of every few tokens
+            for (int t = mine_token; t < here; t += A.table_tokens) {
+                const int64_t at = mine_position + b * A.pos_b + (t0 + t) * A.pos_t;
+                const float position = A.wide ? (float)((const int64_t*)A.position)[at] : (float)((const int32_t*)A.position)[at];
+                table[t * A.pairs + mine] = turn_of(position * frequency, A.inverse);
+            }
+        __syncthreads();
+#pragma unroll 1
+        for (int z = side; z < (MODE == kNormBack ? side + 1 : to); z++) {
+            const HeadSide& S = A.side[z];
+            if (z != side) begin(S);
             T* out = (T*)S.out + b * S.out_b + t0 * S.out_t;
-            // A wavefront's rows are per_wave ones side by side, then those 4 per_wave further on.  The next row is loaded before the last one is done.
-            int r = wave * A.per_wave + place, tl = (int)__umulhi((uint32_t)r, S.by_heads), h = r - tl * S.heads;
-            if (S.heads == 1) { tl = r; h = 0; }
-            Slot<T, N, ADJ> X[K], G[K];
-            auto fetch = [&]() {
-                if (works && r < rows) {
-                    const T* row = in + row_offset(tl, h, S.in_t, S.in_h, A.far);
-                    const T* grow = gin + row_offset(tl, h, S.grad_t, S.grad_h, A.far);
-#pragma unroll
-                    for (int j = 0; j < K; j++) {
-                        X[j].load(row, first[j], second[j], dim);
-                        if (MODE == kNormBack) G[j].load(grow, first[j], second[j], dim);
-                    }
-                }
-            };
-#pragma unroll
-            for (int j = 0; j < K; j++) { X[j].clear(); G[j].clear(); }
-            fetch();
             for (int r0 = wave * A.per_wave; r0 < rows; r0 += 4 * A.per_wave) {
                 const bool on = works && r < rows;
                 const float2* turns = table + tl * A.pairs;
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
                 tl += S.step_tokens;
                 h += S.step_heads;
                 if (h >= S.heads) { h -= S.heads; tl++; }
-                fetch();
+                fetch(S);                                      // (the next row is loaded before this one is done)
                 if (MODE != kRotate) {
                     float sum = 0.f;
 #pragma unroll

@@ -60,11 +60,11 @@ int check_rotation(const pcr_heads* q, const pcr_heads* k, const pcr_rotation* R
 template <typename T, int N, bool ADJ, int MODE> void launch_axes(const AxesArgs& A, int groups, hipStream_t s) {
     if constexpr (N <= 2) {
         if (A.slots > 64) {
-            hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 4>), dim3(groups), dim3(256), 0, s, A);
+            hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 4>), dim3(groups, A.apart ? 2 : 1), dim3(256), 0, s, A);
             return;
         }
     }
-    hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 1>), dim3(groups), dim3(256), 0, s, A);
+    hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 1>), dim3(groups, A.apart ? 2 : 1), dim3(256), 0, s, A);
 }
 
 constexpr int kBackGroups = 1024;                              // workgroups of a gradient: each leaves one sum of the weights' gradient a side
@@ -143,6 +143,8 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     A.chunks = batch * A.shares;
     if (!A.shares) A.shares = 1;
     int groups = (int)(back ? std::min<int64_t>(A.chunks, kBackGroups) : A.chunks);
+    // (us, one after the other / apart: norm and rotation of 256 tokens of 40 heads 6.7 / 6.2, gradient of 64 tokens 14.4 / 10.4; of 1000 tokens 9.2 / 10.5)
+    A.apart = q->heads && k->heads && groups <= 512;
     if (sums) {
         size_t need = 0;
         pcr_norm_rotate_workspace(all, R->dim, &need);
