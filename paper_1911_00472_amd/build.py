@@ -6,6 +6,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "pcr_lib.hip")                # the decoder, the loader, records
 SRC_TRAIN = os.path.join(HERE, "csrc", "pcr_train.hip")        # the operators behind the decode
+SRC_DISTILL = os.path.join(HERE, "csrc", "pcr_distill.hip")
 SRC_BIND = os.path.join(HERE, "csrc", "pcr_bind.cpp")          # their arguments, as a Python module
 LIB = os.path.join(HERE, "libpcr.so")
 MODULE = os.path.join(HERE, "_train.so")
@@ -26,7 +27,7 @@ def build():
     """Compile csrc/ into libpcr.so and _train.so (always recompiles)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     compile_only = [hipcc, "-c"] + [f for f in HIPCC_FLAGS if f != "-shared"]
-    sources = (SRC, SRC_TRAIN)
+    sources = (SRC, SRC_TRAIN, SRC_DISTILL)
     objects = [s[:-len(".hip")] + ".o" for s in sources]
     module, torch_lib = _module_command()
     running = [subprocess.Popen(c) for c in [compile_only + ["-o", o, s] for s, o in zip(sources, objects)] + [module]]

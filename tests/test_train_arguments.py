@@ -3,6 +3,8 @@ import ctypes
 import os
 import subprocess
 
+import pytest
+
 import paper_1911_00472_amd as pkg
 
 _i64, _i32, _vp, _f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
@@ -92,11 +94,12 @@ def test_null_pointers_and_sizes_out_of_range():
     assert L.pcr_distill_workspace(-1, 10, by(need)) == pkg.E_RANGE and L.pcr_distill_workspace(1, 10, None) == pkg.E_ARG
 
 
-def test_no_kernel_spills_to_scratch_memory(tmp_path):
+@pytest.mark.parametrize("source", ["SRC_TRAIN", "SRC_DISTILL"])
+def test_no_kernel_spills_to_scratch_memory(tmp_path, source):
     from paper_1911_00472_amd import build
-    asm = tmp_path / "train.s"
+    asm = tmp_path / "kernels.s"
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
-    subprocess.check_call([hipcc] + flags + ["-S", "--cuda-device-only", "-o", str(asm), build.SRC_TRAIN], stderr=subprocess.DEVNULL)
+    subprocess.check_call([hipcc] + flags + ["-S", "--cuda-device-only", "-o", str(asm), getattr(build, source)], stderr=subprocess.DEVNULL)
     sizes = [line.split()[-1] for line in asm.read_text().splitlines() if ".amdhsa_private_segment_fixed_size" in line]
     assert len(sizes) > 30 and all(s == "0" for s in sizes), sizes
