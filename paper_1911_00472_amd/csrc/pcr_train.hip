@@ -110,9 +110,9 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         S.by_heads = (uint32_t)(((1ull << 32) + S.heads - 1) / S.heads);
     }
     // Tokens of a workgroup at a time: rows of some 32 KB, 128 at least (a gradient: half of what its workgroups come to), as many as the table of sines holds,
-    // and no more than leave 1024 workgroups.  (us with 64 / 128 / 256 / 512 rows: rows of 256 bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)
+    // and as many as come to 1024 workgroups, which fit side by side (2909 tokens of 26 heads, norm and rotation: 15.6 us with some more than that, 12.4).  (us with 64 / 128 / 256 / 512 rows: rows of 256 bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)
     const int64_t heads = std::max<int64_t>(1, q->heads + k->heads), all = batch * tokens;
-    int64_t chunk = back ? (all + 2 * kBackGroups - 1) / (2 * kBackGroups) : std::min<int64_t>(std::max<int64_t>(128, 32768 / (R->dim * size)) / heads, all / 1024);
+    int64_t chunk = back ? (all + 2 * kBackGroups - 1) / (2 * kBackGroups) : std::min<int64_t>(std::max<int64_t>(128, 32768 / (R->dim * size)) / heads, (all + 1023) / 1024);
     if (R->pairs) chunk = std::min<int64_t>(chunk, kAxesTable / R->pairs);
     chunk = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunk, 4096), tokens));
     A.chunk = (int)chunk;
