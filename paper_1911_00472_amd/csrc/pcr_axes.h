@@ -37,7 +37,7 @@ struct AxesArgs {
 };
 
 enum { kRotate = 0, kNorm = 1, kNormBack = 2 };
-constexpr int kAxesTable = 2048;                               // pairs of sine and cosine that a workgroup keeps (16 KB)
+constexpr int kAxesTable = 4096;                               // pairs of sine and cosine that a workgroup keeps at most (32 KB)
 
 // f radians as a fraction of a turn, in 64 bits behind the point: f's 24 bits times 1 / (2 pi) to 128 bits, moved by f's exponent and cut.
 // (What is infinite or NaN gives some angle.)
@@ -168,7 +168,7 @@ template <int N, bool ADJ, int K> __device__ __forceinline__ void turn(float (&y
 // K: slots of a lane (more than one where a row has more than 64).  Every slot is turned whole or not at all.
 template <typename T, int N, bool ADJ, int MODE, int K>
 __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
-    __shared__ __attribute__((aligned(16))) float2 table[kAxesTable];
+    extern __shared__ __attribute__((aligned(16))) float2 table[];
     __shared__ float joined[MODE == kNormBack ? 4 * 512 : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = A.dim;
     const int group = K > 1 ? 64 : A.slots, place = lane / group, head = place * group, member = lane - head;

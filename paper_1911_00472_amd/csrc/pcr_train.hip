@@ -38,11 +38,11 @@ int check_rotation(const pcr_heads* q, const pcr_heads* k, const pcr_rotation* R
 template <typename T, int N, bool ADJ, int MODE> void launch_axes(const AxesArgs& A, int groups, hipStream_t s) {
     if constexpr (N <= 2) {
         if (A.slots > 64) {
-            hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 4>), dim3(groups, A.apart ? 2 : 1), dim3(256), 0, s, A);
+            hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 4>), dim3(groups, A.apart ? 2 : 1), dim3(256), (size_t)A.chunk * A.pairs * sizeof(float2), s, A);
             return;
         }
     }
-    hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 1>), dim3(groups, A.apart ? 2 : 1), dim3(256), 0, s, A);
+    hipLaunchKernelGGL((k_axes<T, N, ADJ, MODE, 1>), dim3(groups, A.apart ? 2 : 1), dim3(256), (size_t)A.chunk * A.pairs * sizeof(float2), s, A);
 }
 
 constexpr int kBackGroups = 1024;                              // workgroups of a gradient: each leaves one sum of the weights' gradient a side
@@ -113,7 +113,12 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     // and as many as come to 1024 workgroups, which fit side by side (2909 tokens of 26 heads, norm and rotation: 15.6 us with some more than that, 12.4).  (us with 64 / 128 / 256 / 512 rows: rows of 256 bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)
     const int64_t heads = std::max<int64_t>(1, q->heads + k->heads), all = batch * tokens;
     int64_t chunk = back ? (all + 2 * kBackGroups - 1) / (2 * kBackGroups) : std::min<int64_t>(std::max<int64_t>(128, 32768 / (R->dim * size)) / heads, (all + 1023) / 1024);
-    if (R->pairs) chunk = std::min<int64_t>(chunk, kAxesTable / R->pairs);
+    if (R->pairs) {
+        // 32 KB of sines in gradients, and where 1024 workgroups come to it; 16 otherwise.  (Few heads: gradient of 2045759 tokens of one head of queries and keys 751
+        // us with 32, 875 with 16, norm and rotation of 41828 tokens 16.1 and 18.9; rotation of 2 million, whose workgroups come and go, 396 and 357.)
+        const bool all_at_once = back || (all + 1023) / 1024 * R->pairs <= kAxesTable;
+        chunk = std::min<int64_t>(chunk, (all_at_once ? kAxesTable : kAxesTable / 2) / R->pairs);
+    }
     chunk = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunk, 4096), tokens));
     A.chunk = (int)chunk;
     A.table_tokens = R->pairs ? 256 / R->pairs : 0;
