@@ -327,7 +327,9 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
 #pragma unroll
             for (int i = 0; i < 2 * N; i++) {
                 float v = works ? dw[j][i] : 0.f;
-                if (K == 1) {
+                if (K == 1 && (group & (group - 1)) == 0) {
+                    for (int d = group; d < 64; d <<= 1) v += __shfl_xor(v, d);
+                } else if (K == 1) {
                     float all = 0.f;
                     for (int q = 0; q < A.per_wave; q++) all += __shfl(v, q * group + member);
                     v = all;

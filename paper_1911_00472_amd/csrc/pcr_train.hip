@@ -109,10 +109,14 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         S.step_tokens = 4 * A.per_wave / S.heads; S.step_heads = 4 * A.per_wave % S.heads;
         S.by_heads = (uint32_t)(((1ull << 32) + S.heads - 1) / S.heads);
     }
-    // Tokens of a workgroup at a time: rows of some 32 KB, 128 at least (a gradient: half of what its workgroups come to), as many as the table of sines holds,
-    // and as many as come to 1024 workgroups, which fit side by side (2909 tokens of 26 heads, norm and rotation: 15.6 us with some more than that, 12.4).  (us with 64 / 128 / 256 / 512 rows: rows of 256 bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)
+    // Tokens of a workgroup at a time: rows of some 32 KB, 128 at least, as many as the table of sines holds, and as many as come to 1024 workgroups, which
+    // fit side by side (2909 tokens of 26 heads, norm and rotation: 15.6 us with some more than that, 12.4).  (us with 64 / 128 / 256 / 512 rows: rows of 256
+    // bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)  A gradient has 1024 workgroups at most, which leave sums: fewer of rows of 32 KB, down
+    // to 128, where there are few tokens (us with rows of 8 / 32 KB: 3552 tokens of 19 heads of 64 21.4 / 18.7, 3160 of 18 of 128 23.1 / 18.3).
     const int64_t heads = std::max<int64_t>(1, q->heads + k->heads), all = batch * tokens;
-    int64_t chunk = back ? (all + 2 * kBackGroups - 1) / (2 * kBackGroups) : std::min<int64_t>(std::max<int64_t>(128, 32768 / (R->dim * size)) / heads, (all + 1023) / 1024);
+    const int64_t row = (int64_t)(R->dim * size);
+    const int64_t few = std::max<int64_t>(1, std::min<int64_t>(32768 / (row * heads), (all + 127) / 128));
+    int64_t chunk = back ? std::max<int64_t>(few, (all + kBackGroups - 1) / kBackGroups) : std::min<int64_t>(std::max<int64_t>(128, 32768 / row) / heads, (all + 1023) / 1024);
     if (R->pairs) {
         // 32 KB of sines in gradients, and where 1024 workgroups come to it; 16 otherwise.  (Few heads: gradient of 2045759 tokens of one head of queries and keys 751
         // us with 32, 875 with 16, norm and rotation of 41828 tokens 16.1 and 18.9; rotation of 2 million, whose workgroups come and go, 396 and 357.)
