@@ -93,25 +93,27 @@ struct Entries {
         return all;
     }
 };
-// Reads a row's entries, four of a thread's at a time, and returns the largest of the thread's logits.
+// Reads a row's entries and returns the largest of the thread's logits.  A wavefront reads four of a lane's at a time; larger teams one, as their threads
+// have one mostly and registers are short (with four 4096 rows of 50001 took 261 us, for 136 registers; 175).
 template <typename T, int TEAM> __device__ __forceinline__ float load_entries(const DistillArgs& A, int64_t n, const T* z, const Entries& E, int tid) {
+    constexpr int B = TEAM > 64 ? 1 : 4;
     float most = -INFINITY;
-    for (int k0 = tid; k0 < A.K; k0 += 4 * TEAM) {
-        int64_t v[4];
-        float t[4], x[4];
+    for (int k0 = tid; k0 < A.K; k0 += B * TEAM) {
+        int64_t v[B];
+        float t[B], x[B];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < B; j++) {
             const int k = k0 + j * TEAM;
             v[j] = k < A.K && A.a != 0.f ? top_class(A, n * A.K + k) : -1;
             t[j] = k < A.K ? top_logit(A, n * A.K + k) * A.inv_T : -INFINITY;
         }
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < B; j++) {
             if (v[j] < 0 || t[j] == -INFINITY) { v[j] = -1; t[j] = -INFINITY; }
             x[j] = v[j] >= 0 ? (float)z[v[j]] : 0.f;
         }
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < B; j++) {
             const int k = k0 + j * TEAM;
             if (k >= A.K) break;
             E.at[k] = (int)v[j];
