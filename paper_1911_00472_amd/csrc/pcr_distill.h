@@ -349,7 +349,8 @@ template <typename T, typename V, int N> __device__ __forceinline__ void take_ag
     for (int i = 0; i < N; i++) x[i] = (float)raw[i];
 }
 
-// Loss (MODE kLoss) or loss and gradient (kStep) of rows that a team of TEAM threads holds in its registers, R runs of 16 bytes a thread: read once, written once.
+// Loss (MODE kLoss), loss and gradient (kStep) or the gradient from saved sums (kGrad) of rows that a team of TEAM threads holds in its registers, R runs of 16
+// bytes a thread: read once, written once.
 template <typename T, int TEAM, int R, int BY, int MODE>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(DistillArgs A) {
     extern __shared__ float lds[];                             // a team's: joins [6 a wavefront], entries
@@ -361,15 +362,19 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     float* join = lds + team * (6 * W + entry_floats(A.K, A.V));
     Entries E(join + 6 * W, A.K, A.V);
     const T* z = (const T*)A.logits + n * A.row_stride;
-    T* out = MODE == kStep ? (T*)A.out + n * A.out_stride : nullptr;
-    const float g = MODE == kStep ? A.row_grad[n] : 1.f, c = A.inv_T * kLog2e;
-    if (MODE == kStep && g == 0.f) {
+    constexpr bool WRITES = MODE != kLoss, SUMS = MODE != kGrad;
+    T* out = WRITES ? (T*)A.out + n * A.out_stride : nullptr;
+    const float g = WRITES ? A.row_grad[n] : 1.f, c = A.inv_T * kLog2e;
+    auto left_out = [&]() {
         write_zeros<T, TEAM>(out, A.V, tid);
-        if (tid == 0) A.loss[n] = 0.f;
-        return;
-    }
+        if (SUMS && tid == 0) A.loss[n] = 0.f;
+    };
+    // A wavefront asks for its row before it knows whether it counts (a trip to memory less, of three); larger teams leave the row's bytes where they are.
+    if (TEAM > 64 && WRITES && g == 0.f) return left_out();
+    const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
+    const float saved = SUMS ? 0.f : A.sums_in[2 * n], saved1 = SUMS ? 0.f : A.sums_in[2 * n + 1];
     const int V = (int)A.V, lead = min(V, (int)((-(uintptr_t)z & 15) / sizeof(T))), runs = (V - lead) / N, tail = lead + runs * N;
-    if (MODE == kStep) E.clear<TEAM>(tid);
+    if (WRITES) E.clear<TEAM>(tid);
     Vec raw[R];
     Vec least;
 #pragma unroll
@@ -380,23 +385,21 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     const int edge = tid < lead ? tid : tail + tid - lead;     // the elements in front of and behind the runs: one of some threads
     const bool edged = edge < V;
     const float x_edge = edged ? (float)z[edge] : -INFINITY;
-    const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
-    const bool labelled = label >= 0 && label < A.V;
-    const float zl = labelled ? (float)z[label] : 0.f;
+    if (TEAM == 64 && WRITES && g == 0.f) return left_out();
 
     float most[2] = {x_edge, load_entries<T, TEAM>(A, n, z, E, tid)};            // of the logits, of the kept teacher's logits
+    const bool labelled = label >= 0 && label < A.V;
+    const float zl = labelled ? (float)z[label] : 0.f;
+    if (SUMS) {
 #pragma unroll
-    for (int u = 0; u < R; u++)
+        for (int u = 0; u < R; u++)
 #pragma unroll
-        for (int i = 0; i < N; i++) most[0] = fmaxf(most[0], (float)raw[u][i]);
+            for (int i = 0; i < N; i++) most[0] = fmaxf(most[0], (float)raw[u][i]);
+    }
     team_join_all<TEAM, 2, true>(most, join);
     const float m = most[0];
     const bool kept = most[1] != -INFINITY;
-    if (MODE == kStep && !kept && !labelled) {
-        write_zeros<T, TEAM>(out, A.V, tid);
-        if (tid == 0) A.loss[n] = 0.f;
-        return;
-    }
+    if (WRITES && !kept && !labelled) return left_out();
     float sum[3] = {0.f, 0.f, 0.f};                            // of exp((z - m) / T), of exp(z - m), of the teacher's
     auto add = [&](float x) {
         float e, e1 = 0.f;
@@ -404,22 +407,24 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         sum[0] += e;
         sum[1] += e1;
     };
+    if (SUMS) {
 #pragma unroll
-    for (int u = 0; u < R; u++) {
-        if (u * TEAM < runs) {                                 // (the same for the team)
-            float x[N];
-            take_again<T>(raw[u], x);
+        for (int u = 0; u < R; u++) {
+            if (u * TEAM < runs) {                             // (the same for the team)
+                float x[N];
+                take_again<T>(raw[u], x);
 #pragma unroll
-            for (int i = 0; i < N; i++) add(x[i]);
+                for (int i = 0; i < N; i++) add(x[i]);
+            }
         }
+        if (edged) add(x_edge);
     }
-    if (edged) add(x_edge);
     for (int k = tid; k < A.K; k += TEAM) if (E.at[k] >= 0) sum[2] += __builtin_amdgcn_exp2f((E.delta[k] - most[1]) * kLog2e);
     team_join_all<TEAM, 3, false>(sum, join + 2 * W);
     if (BY == kOneSum) sum[1] = sum[0];
     const float total = sum[2], L = m * A.inv_T, log_s = logf(sum[0]), log_s1 = logf(sum[1]), log_total = logf(total);
     const float unit = -g * A.a * A.T;
-    const float ca = kept ? -unit / sum[0] : 0.f, cb = labelled ? g * A.b / sum[1] : 0.f;
+    const float ca = kept ? (SUMS ? -unit / sum[0] : -unit) : 0.f, cb = labelled ? (SUMS ? g * A.b / sum[1] : g * A.b) : 0.f;
 
     // entries: their share of the loss, and what each adds to the dense part of its class
     auto finish = [&](float entries) {                         // the row's loss, from the sum of the entries' shares
@@ -428,16 +433,16 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         A.loss[n] = g * all;
     };
     float loss[1] = {0.f};
-    if (MODE == kStep) team_sync<TEAM>();                      // (the bits are cleared)
+    if (WRITES) team_sync<TEAM>();                             // (the bits are cleared)
     for (int k = tid; k < A.K; k += TEAM) {
         const int v = E.at[k];
         float d = 0.f;
         if (v >= 0) {
             const float t = E.delta[k] - most[1], e = __builtin_amdgcn_exp2f(t * kLog2e);
-            if (e > 0.f || t != t) loss[0] += e * ((t - log_total) - ((E.logit[k] * A.inv_T - L) - log_s));
+            if (SUMS && (e > 0.f || t != t)) loss[0] += e * ((t - log_total) - ((E.logit[k] * A.inv_T - L) - log_s));
             d = unit * (e / total);
-            if (MODE == kStep) E.mark((uint32_t)v);
-            if (MODE == kStep && labelled && v == label) *E.labelled = 1;
+            if (WRITES) E.mark((uint32_t)v);
+            if (WRITES && labelled && v == label) *E.labelled = 1;
         }
         E.delta[k] = d;
     }
@@ -450,7 +455,9 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         }
         return;
     }
+    const Dense D = {A.inv_T, saved, saved1, BY == kOneSum ? ca + cb : ca, cb};
     auto dense = [&](float x) {
+        if (!SUMS) return dense_of<BY == kTwoSums>(x, D);
         float e, e1 = 0.f;
         exps<BY>(x, m, c, A.T, e, e1);
         if (BY == kOneSum) return (ca + cb) * e;
@@ -470,7 +477,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     if (edged) out[edge] = (T)dense(x_edge);
     team_join_all<TEAM, 1, false>(loss, join + 5 * W);         // (the dense part and the entries are behind this barrier, too)
     team_sync<TEAM>();
-    if (tid == 0) finish(loss[0]);
+    if (SUMS && tid == 0) finish(loss[0]);
     for (int e = tid; e < A.K; e += TEAM) {
         const int v = E.at[e];
         if (v >= 0) out[v] = (T)(dense(E.logit[e]) + (E.sum(e, (uint32_t)v, A.K) - (v == label ? g * A.b : 0.f)));

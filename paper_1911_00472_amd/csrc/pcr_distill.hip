@@ -59,13 +59,12 @@ template <typename T, int TEAM, int MODE> void launch_team(const DistillArgs& A,
     if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(threads), lds, s, A);
     else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(threads), lds, s, A);
 }
-// The gradient from saved sums, and (MODE kLoss, kStep) rows too long for a team's registers, read twice.
+// The gradient from saved sums of rows for more than a wavefront, and (MODE kLoss, kStep) rows too long for a team's registers, read twice.
 template <int MODE> void launch_distill(const DistillArgs& A, int dtype, hipStream_t s) {
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const int64_t bytes = std::min(A.chunk, A.V) * (int64_t)sizeof(T);
         if constexpr (MODE == kGrad) {
-            if (bytes <= 8192) return launch_team<T, 64, MODE>(A, s);
             if (bytes <= 65536) return launch_team<T, 256, MODE>(A, s);
         }
         launch_team<T, 1024, MODE>(A, s);
@@ -79,17 +78,23 @@ template <typename T, int TEAM, int R, int MODE> bool launch_rows(const DistillA
     const dim3 groups((unsigned)((A.rows + teams - 1) / teams));
     const size_t lds = (size_t)teams * (6 * (TEAM / 64) + entry_floats(A.K, A.V)) * sizeof(float);
     if (!A.two || A.T == 1.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kOneSum, MODE>), groups, dim3(threads), lds, s, A);
-    else if (A.T == 2.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kSquare, MODE>), groups, dim3(threads), lds, s, A);
-    else if (A.T == 4.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kFourth, MODE>), groups, dim3(threads), lds, s, A);
+    else if (MODE != kGrad && A.T == 2.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, MODE == kGrad ? kTwoSums : kSquare, MODE>), groups, dim3(threads), lds, s, A);
+    else if (MODE != kGrad && A.T == 4.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, MODE == kGrad ? kTwoSums : kFourth, MODE>), groups, dim3(threads), lds, s, A);
     else hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kTwoSums, MODE>), groups, dim3(threads), lds, s, A);
     return true;
 }
+// Whether rows go to a wavefront each: short ones, unless there are so few that a workgroup each is done sooner.  (us, wavefronts / workgroups of 256, gradient
+// from saved sums over rows of 3000 classes with 256 entries: 1 row 7.9 / 5.7, 64 9.0 / 5.4, 1024 11.2 / 7.3, 4096 18.9 / 24.7; of 500 classes with 10
+// entries: 1024 5.5 / 5.5, 4096 6.8 / 16.7.)
+bool by_wavefronts(int64_t rows, int64_t V, size_t size) { return V * (int64_t)size <= 8192 && rows > (V * (int64_t)size > 4096 ? 1024 : 256); }
 template <int MODE> bool launch_resident(const DistillArgs& A, int dtype, hipStream_t s) {
     bool held = false;
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        held = launch_rows<T, 64, 4, MODE>(A, s) || launch_rows<T, 64, 8, MODE>(A, s) || launch_rows<T, 256, 4, MODE>(A, s) || launch_rows<T, 256, 8, MODE>(A, s) ||
-               launch_rows<T, 512, 8, MODE>(A, s) || launch_rows<T, 512, 16, MODE>(A, s) || launch_rows<T, 1024, 16, MODE>(A, s) || launch_rows<T, 1024, kMostRuns, MODE>(A, s);
+        if (by_wavefronts(A.rows, A.V, sizeof(T))) held = launch_rows<T, 64, 4, MODE>(A, s) || launch_rows<T, 64, 8, MODE>(A, s);
+        if constexpr (MODE != kGrad)                           // (longer rows are written as fast as they are read again)
+            held = held || launch_rows<T, 256, 4, MODE>(A, s) || launch_rows<T, 256, 8, MODE>(A, s) || launch_rows<T, 512, 8, MODE>(A, s) ||
+                   launch_rows<T, 512, 16, MODE>(A, s) || launch_rows<T, 1024, 16, MODE>(A, s) || launch_rows<T, 1024, kMostRuns, MODE>(A, s);
     });
     return held;
 }
@@ -153,7 +158,7 @@ int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums,
     cut(A, parts_of(A.rows, A.V));
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
-    launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
+    if (!launch_resident<kGrad>(A, d->dtype, (hipStream_t)hip_stream)) launch_distill<kGrad>(A, d->dtype, (hipStream_t)hip_stream);
     return launched();
 }
 
