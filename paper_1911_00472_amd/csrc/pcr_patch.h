@@ -3,8 +3,8 @@
 // Row r of picture i holds a patch as [channel][y][x], (pixel / 255 - mean) inv_std, written as one multiply-add of the pixel with
 // inv_std / 255 and -mean inv_std (its error, 2^-24 of each of the two, is far below the rounding to 16 bits and within three units of 32).
 // Bound by memory: a pixel byte in, two or four bytes out.  1024 photographs of 300 to 500 pixels a side, us (floor: the bytes at a large copy's 5.0 TB/s):
-// patches of 14, bfloat 340 (312), of 16 295 (305), of 8 313 (310), of 28 324; 512 of them in 32 bits, patches of 16 246 (253), of 14 256.
-// An element a lane and loads of bytes took 1228 with patches of 14; eight pixels a lane with stores in pieces 504.
+// patches of 14, bfloat 304, in windows of 2 x 2 319 (312), of 16 285 (305), of 8 300 (310), of 28 303; 512 of them in 32 bits, patches of 16 245 (253), of 14 247.
+// An element a lane and loads of bytes took 1228 with patches of 14; eight pixels a lane with stores in pieces 504; one load of a lane under way at a time 340.
 #pragma once
 #include "pcr_vec.h"
 
@@ -106,40 +106,53 @@ __global__ __launch_bounds__(256) void k_patch_rows(PatchArgs A) {
     }
     __syncthreads();
     const uint32_t runs = (uint32_t)(P + 7) / 8, each = (uint32_t)P * runs, all = each * here;
-    for (uint32_t e = threadIdx.x; e < all; e += 256) {
+    struct Item { uint32_t words[2 * C]; T* out; int n, there; };
+    auto fetch = [&](uint32_t e, Item& I) {
         const uint32_t t = quotient(e, A.by_each), inside = e - t * each, y = quotient(inside, A.by_runs), x = (inside - y * runs) * 8;
         const Patch p = patches[t];
         const int64_t py = (int64_t)p.row * P + y, px = (int64_t)p.column * P + x;
-        const int n = min(8, P - (int)x);
-        const int there = py < p.H ? (int)max((int64_t)0, min((int64_t)n, p.W - px)) : 0;     // pixels that the picture has
-        uint32_t words[2 * C] = {};
-        if (there) {
+        I.n = min(8, P - (int)x);
+        I.there = py < p.H ? (int)max((int64_t)0, min((int64_t)I.n, p.W - px)) : 0;           // pixels that the picture has
+        I.out = STAGED ? (T*)staged + (t * C * P + y) * P + x : (T*)A.out + ((r0 + t) * C * P + y) * P + x;
+#pragma unroll
+        for (int j = 0; j < 2 * C; j++) I.words[j] = 0;
+        if (I.there) {
             const int64_t at = p.begin + (py * p.W + px) * C;
             if (at + 8 * C <= A.pixel_bytes) {
                 struct __attribute__((packed, aligned(1))) Loose { uint32_t w[2 * C]; };
                 const Loose v = *reinterpret_cast<const Loose*>(A.pixels + at);
 #pragma unroll
-                for (int j = 0; j < 2 * C; j++) words[j] = v.w[j];
+                for (int j = 0; j < 2 * C; j++) I.words[j] = v.w[j];
             } else {                                           // the pixels' last bytes
 #pragma unroll
                 for (int j = 0; j < 8 * C; j++)
-                    if (at + j < A.pixel_bytes) words[j / 4] |= (uint32_t)A.pixels[at + j] << 8 * (j % 4);
+                    if (at + j < A.pixel_bytes) I.words[j / 4] |= (uint32_t)A.pixels[at + j] << 8 * (j % 4);
             }
         }
-        T* out = STAGED ? (T*)staged + (t * C * P + y) * P + x : (T*)A.out + ((r0 + t) * C * P + y) * P + x;
+    };
+    auto finish = [&](const Item& I) {
+        T* out = I.out;
 #pragma unroll
         for (int c = 0; c < C; c++) {
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const int j = i * C + c;
-                v[i] = i < there ? __builtin_fmaf((float)(words[j / 4] >> 8 * (j % 4) & 255), A.scale[c], A.shift[c]) : 0.f;
+                v[i] = i < I.there ? __builtin_fmaf((float)(I.words[j / 4] >> 8 * (j % 4) & 255), A.scale[c], A.shift[c]) : 0.f;
             }
-            if (STAGED && sizeof(T) == 2 && P % 2 == 0) stage_pairs<T>(out, v, n);
-            else if (!STAGED && n == 8) store_eight<T>(out, v);
-            else store_some<T>(out, v, n);
+            if (STAGED && sizeof(T) == 2 && P % 2 == 0) stage_pairs<T>(out, v, I.n);
+            else if (!STAGED && I.n == 8) store_eight<T>(out, v);
+            else store_some<T>(out, v, I.n);
             out += P * P;
         }
+    };
+    for (uint32_t e = threadIdx.x; e < all; e += 512) {        // two at a time: the loads of both are under way together
+        Item I, J;
+        fetch(e, I);
+        const bool two = e + 256 < all;
+        if (two) fetch(e + 256, J);
+        finish(I);
+        if (two) finish(J);
     }
     if (STAGED) {
         __syncthreads();

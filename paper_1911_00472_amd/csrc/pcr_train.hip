@@ -195,11 +195,14 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
     const uint32_t runs = (patch + 7) / 8, each = runs * patch;
     A.by_runs = (uint32_t)(((1ull << 32) + runs - 1) / runs);  // (of 1: 0)
     A.by_each = (uint32_t)(((1ull << 32) + each - 1) / each);
-    // Rows of a workgroup: some 512 runs of eight pixels (256 where elements have 32 bits).  Stores go through LDS where lines are not of whole runs and a row fits there.
-    const size_t row_bytes = (size_t)channels * patch * patch * type_size(dtype);
+    // Stores go through LDS where lines are not of whole runs and a row fits there.  Rows of a workgroup: some 512 runs of eight pixels, two a thread (256 where 32-bit
+    // elements are stored at once), in LDS no more than 10240 elements, eight together (16-byte stores then lie at multiples of 16).  us for 1024 photographs with 8 / 16 /
+    // 24 rows of patches of 14: 406 / 319 / 350, of 16 - / 285 / 296; 512 of them in 32 bits, 14: 268 / 247 / -, 16: 245 / 250 / -.
+    const size_t size = type_size(dtype), row_bytes = (size_t)channels * patch * patch * size;
     const bool staged = patch % 8 && row_bytes <= 61440;
-    int64_t group = (dtype == PCR_FLOAT ? 256 : 512) / each;
-    if (staged) group = std::min<int64_t>(group, 20480 / row_bytes);
+    int64_t group = (dtype == PCR_FLOAT && !staged ? 256 : 512) / each;
+    if (staged) group = std::min<int64_t>(group, 10240 * size / row_bytes);
+    if (group > 8) group -= group % 8;
     A.group = (int)std::max<int64_t>(1, std::min<int64_t>(group, kPatchGroup));
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
