@@ -112,7 +112,7 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     // Tokens of a workgroup at a time: rows of some 32 KB, 128 at least, as many as the table of sines holds, and as many as come to 1024 workgroups, which
     // fit side by side (2909 tokens of 26 heads, norm and rotation: 15.6 us with some more than that, 12.4).  (us with 64 / 128 / 256 / 512 rows: rows of 256
     // bytes 263 / 241 / 251 / 259, of 128 bytes 188 / 143 / 121 / 114.)  A gradient has 1024 workgroups at most, which leave sums: fewer of rows of 32 KB, down
-    // to 128, where there are few tokens (us with rows of 8 / 32 KB: 3552 tokens of 19 heads of 64 21.4 / 18.7, 3160 of 18 of 128 23.1 / 18.3).
+    // to 128, where there are few tokens (us with rows of 16 / 32 / 64 KB: 3552 tokens of 19 heads of 64 19.0 / 18.7 / 23.9, 3160 of 18 of 128 22.6 / 18.3 / 19.5).
     const int64_t heads = std::max<int64_t>(1, q->heads + k->heads), all = batch * tokens;
     const int64_t row = (int64_t)(R->dim * size);
     const int64_t few = std::max<int64_t>(1, std::min<int64_t>(32768 / (row * heads), (all + 127) / 128));
@@ -130,8 +130,9 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     A.chunks = batch * A.shares;
     if (!A.shares) A.shares = 1;
     int groups = (int)(back ? std::min<int64_t>(A.chunks, kBackGroups) : A.chunks);
-    // (us, one after the other / apart: norm and rotation of 256 tokens of 40 heads 6.7 / 6.2, gradient of 64 tokens 14.4 / 10.4; of 1000 tokens 9.2 / 10.5)
-    A.apart = q->heads && k->heads && groups <= 512;
+    // (us, one after the other / apart: norm and rotation of 256 tokens of 40 heads 6.7 / 6.2, of 1000 9.2 / 10.5; gradient of 64 tokens of 40 heads 14.4 / 10.4,
+    // of 5006 of 31 of 64, 626 workgroups, 25.2 / 20.8, of 3000 of 56, 1000 workgroups, 37.2 / 38.3)
+    A.apart = q->heads && k->heads && groups <= (back ? 768 : 512);
     if (sums) {
         size_t need = 0;
         pcr_norm_rotate_workspace(all, R->dim, &need);
