@@ -206,147 +206,147 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
     const int from = A.apart ? blockIdx.y : 0, to = A.apart ? from + 1 : 2;
 #pragma unroll 1
     for (int side = from; side < (MODE == kNormBack ? to : from + 1); side++) {
-    float dw[K][2 * N];
-    if (MODE == kNormBack) {
-        if (!A.side[side].heads && !A.side[side].part) continue;
+        float dw[K][2 * N];
+        if (MODE == kNormBack) {
+            if (!A.side[side].heads && !A.side[side].part) continue;
 #pragma unroll
-        for (int j = 0; j < K; j++)
+            for (int j = 0; j < K; j++)
 #pragma unroll
-            for (int i = 0; i < 2 * N; i++) dw[j][i] = 0.f;
-    }
-    for (int64_t chunk = blockIdx.x; chunk < A.chunks; chunk += gridDim.x) {
-        const int64_t b = A.shares == A.chunks ? 0 : chunk / A.shares, t0 = (chunk - b * A.shares) * A.chunk;
-        const int here = (int)min((int64_t)A.chunk, A.tokens - t0);
-        float w[K][2 * N];
-        Slot<T, N, ADJ> X[K], G[K];
-        int rows, r, tl, h;
-        auto fetch = [&](const HeadSide& S) {
-            if (works && r < rows) {
-                const T* row = (const T*)S.in + b * S.in_b + t0 * S.in_t + row_offset(tl, h, S.in_t, S.in_h, A.far);
-                const T* grow = (const T*)S.grad + b * S.grad_b + t0 * S.grad_t + row_offset(tl, h, S.grad_t, S.grad_h, A.far);
+                for (int i = 0; i < 2 * N; i++) dw[j][i] = 0.f;
+        }
+        for (int64_t chunk = blockIdx.x; chunk < A.chunks; chunk += gridDim.x) {
+            const int64_t b = A.shares == A.chunks ? 0 : chunk / A.shares, t0 = (chunk - b * A.shares) * A.chunk;
+            const int here = (int)min((int64_t)A.chunk, A.tokens - t0);
+            float w[K][2 * N];
+            Slot<T, N, ADJ> X[K], G[K];
+            int rows, r, tl, h;
+            auto fetch = [&](const HeadSide& S) {
+                if (works && r < rows) {
+                    const T* row = (const T*)S.in + b * S.in_b + t0 * S.in_t + row_offset(tl, h, S.in_t, S.in_h, A.far);
+                    const T* grow = (const T*)S.grad + b * S.grad_b + t0 * S.grad_t + row_offset(tl, h, S.grad_t, S.grad_h, A.far);
 #pragma unroll
-                for (int j = 0; j < K; j++) {
-                    X[j].load(row, first[j], second[j], dim);
-                    if (MODE == kNormBack) G[j].load(grow, first[j], second[j], dim);
+                    for (int j = 0; j < K; j++) {
+                        X[j].load(row, first[j], second[j], dim);
+                        if (MODE == kNormBack) G[j].load(grow, first[j], second[j], dim);
+                    }
                 }
-            }
-        };
-        // A side's weights and its first rows.  A wavefront's rows are per_wave ones side by side, then those 4 per_wave further on.
-        auto begin = [&](const HeadSide& S) {
-            rows = here * S.heads;
-            r = wave * A.per_wave + place;
-            tl = S.heads == 1 ? r : (int)__umulhi((uint32_t)r, S.by_heads);
-            h = r - tl * S.heads;
+            };
+            // A side's weights and its first rows.  A wavefront's rows are per_wave ones side by side, then those 4 per_wave further on.
+            auto begin = [&](const HeadSide& S) {
+                rows = here * S.heads;
+                r = wave * A.per_wave + place;
+                tl = S.heads == 1 ? r : (int)__umulhi((uint32_t)r, S.by_heads);
+                h = r - tl * S.heads;
 #pragma unroll
-            for (int j = 0; j < K; j++) { X[j].clear(); G[j].clear(); }
-            fetch(S);
-            if (MODE != kRotate && S.heads) {
+                for (int j = 0; j < K; j++) { X[j].clear(); G[j].clear(); }
+                fetch(S);
+                if (MODE != kRotate && S.heads) {
 #pragma unroll
-                for (int j = 0; j < K; j++) {
-                    float x[N], y[N];
+                    for (int j = 0; j < K; j++) {
+                        float x[N], y[N];
 #pragma unroll
-                    for (int i = 0; i < N; i++) x[i] = y[i] = 0.f;
-                    if (first[j] < dim) load_weight<T, N>(A, S.weight, first[j], x);
-                    if (second[j] < dim) load_weight<T, N>(A, S.weight, second[j], y);
+                        for (int i = 0; i < N; i++) x[i] = y[i] = 0.f;
+                        if (first[j] < dim) load_weight<T, N>(A, S.weight, first[j], x);
+                        if (second[j] < dim) load_weight<T, N>(A, S.weight, second[j], y);
 #pragma unroll
-                    for (int i = 0; i < N; i++) { w[j][i] = x[i]; w[j][N + i] = y[i]; }
+                        for (int i = 0; i < N; i++) { w[j][i] = x[i]; w[j][N + i] = y[i]; }
+                    }
                 }
-            }
-        };
-        begin(A.side[side]);
-        if (mine < A.pairs)                                    // a thread makes one pair's angles, of every few tokens
-            for (int t = mine_token; t < here; t += A.table_tokens) {
-                const int64_t at = mine_position + b * A.pos_b + (t0 + t) * A.pos_t;
-                const float position = A.wide ? (float)((const int64_t*)A.position)[at] : (float)((const int32_t*)A.position)[at];
-                table[t * A.pairs + mine] = turn_of(position * frequency, A.inverse);
-            }
-        __syncthreads();
+            };
+            begin(A.side[side]);
+            if (mine < A.pairs)                                    // a thread makes one pair's angles, of every few tokens
+                for (int t = mine_token; t < here; t += A.table_tokens) {
+                    const int64_t at = mine_position + b * A.pos_b + (t0 + t) * A.pos_t;
+                    const float position = A.wide ? (float)((const int64_t*)A.position)[at] : (float)((const int32_t*)A.position)[at];
+                    table[t * A.pairs + mine] = turn_of(position * frequency, A.inverse);
+                }
+            __syncthreads();
 #pragma unroll 1
-        for (int z = side; z < (MODE == kNormBack ? side + 1 : to); z++) {
-            const HeadSide& S = A.side[z];
-            if (z != side) begin(S);
-            T* out = (T*)S.out + b * S.out_b + t0 * S.out_t;
-            for (int r0 = wave * A.per_wave; r0 < rows; r0 += 4 * A.per_wave) {
-                const bool on = works && r < rows;
-                const float2* turns = table + tl * A.pairs;
-                T* orow = out + row_offset(tl, h, S.out_t, S.out_h, A.far);
-                float x[K][2 * N], g[K][2 * N];
+            for (int z = side; z < (MODE == kNormBack ? side + 1 : to); z++) {
+                const HeadSide& S = A.side[z];
+                if (z != side) begin(S);
+                T* out = (T*)S.out + b * S.out_b + t0 * S.out_t;
+                for (int r0 = wave * A.per_wave; r0 < rows; r0 += 4 * A.per_wave) {
+                    const bool on = works && r < rows;
+                    const float2* turns = table + tl * A.pairs;
+                    T* orow = out + row_offset(tl, h, S.out_t, S.out_h, A.far);
+                    float x[K][2 * N], g[K][2 * N];
 #pragma unroll
-                for (int j = 0; j < K; j++) {
-                    X[j].take(x[j]);
-                    if (MODE == kNormBack) G[j].take(g[j]);
-                }
-                r += 4 * A.per_wave;
-                tl += S.step_tokens;
-                h += S.step_heads;
-                if (h >= S.heads) { h -= S.heads; tl++; }
-                fetch(S);                                      // (the next row is loaded before this one is done)
-                if (MODE != kRotate) {
-                    float sum = 0.f;
+                    for (int j = 0; j < K; j++) {
+                        X[j].take(x[j]);
+                        if (MODE == kNormBack) G[j].take(g[j]);
+                    }
+                    r += 4 * A.per_wave;
+                    tl += S.step_tokens;
+                    h += S.step_heads;
+                    if (h >= S.heads) { h -= S.heads; tl++; }
+                    fetch(S);                                      // (the next row is loaded before this one is done)
+                    if (MODE != kRotate) {
+                        float sum = 0.f;
 #pragma unroll
-                    for (int j = 0; j < K; j++)
+                        for (int j = 0; j < K; j++)
 #pragma unroll
-                        for (int i = 0; i < 2 * N; i++) sum = __builtin_fmaf(x[j][i], x[j][i], sum);
-                    sum = group_sum(sum, head, member, group);
-                    const float rms = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, A.inv_dim, A.eps));
-#pragma unroll
-                    for (int j = 0; j < K; j++)
-#pragma unroll
-                        for (int i = 0; i < 2 * N; i++) {
-                            x[j][i] *= rms;
-                            if (MODE == kNorm) x[j][i] *= w[j][i];
-                        }
-                    if (MODE == kNormBack) {
-                        turn<N, ADJ, K>(g, turns, A, member, on);
-                        float dot = 0.f;
+                            for (int i = 0; i < 2 * N; i++) sum = __builtin_fmaf(x[j][i], x[j][i], sum);
+                        sum = group_sum(sum, head, member, group);
+                        const float rms = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, A.inv_dim, A.eps));
 #pragma unroll
                         for (int j = 0; j < K; j++)
 #pragma unroll
                             for (int i = 0; i < 2 * N; i++) {
-                                if (on) dw[j][i] = __builtin_fmaf(g[j][i], x[j][i], dw[j][i]);
-                                g[j][i] *= w[j][i];
-                                dot = __builtin_fmaf(g[j][i], x[j][i], dot);
+                                x[j][i] *= rms;
+                                if (MODE == kNorm) x[j][i] *= w[j][i];
                             }
-                        dot = group_sum(dot, head, member, group) * A.inv_dim;
+                        if (MODE == kNormBack) {
+                            turn<N, ADJ, K>(g, turns, A, member, on);
+                            float dot = 0.f;
 #pragma unroll
-                        for (int j = 0; j < K; j++)
+                            for (int j = 0; j < K; j++)
 #pragma unroll
-                            for (int i = 0; i < 2 * N; i++) x[j][i] = rms * __builtin_fmaf(-x[j][i], dot, g[j][i]);
+                                for (int i = 0; i < 2 * N; i++) {
+                                    if (on) dw[j][i] = __builtin_fmaf(g[j][i], x[j][i], dw[j][i]);
+                                    g[j][i] *= w[j][i];
+                                    dot = __builtin_fmaf(g[j][i], x[j][i], dot);
+                                }
+                            dot = group_sum(dot, head, member, group) * A.inv_dim;
+#pragma unroll
+                            for (int j = 0; j < K; j++)
+#pragma unroll
+                                for (int i = 0; i < 2 * N; i++) x[j][i] = rms * __builtin_fmaf(-x[j][i], dot, g[j][i]);
+                        }
+                    }
+                    if (MODE != kNormBack) turn<N, ADJ, K>(x, turns, A, member, on);
+                    if (on) {
+#pragma unroll
+                        for (int j = 0; j < K; j++) Slot<T, N, ADJ>::store(orow, first[j], second[j], dim, x[j]);
                     }
                 }
-                if (MODE != kNormBack) turn<N, ADJ, K>(x, turns, A, member, on);
-                if (on) {
-#pragma unroll
-                    for (int j = 0; j < K; j++) Slot<T, N, ADJ>::store(orow, first[j], second[j], dim, x[j]);
-                }
             }
+            __syncthreads();                                       // the table is made anew
         }
-        __syncthreads();                                       // the table is made anew
-    }
 
-    // The weight's gradient: a lane's sums over its rows, then over the groups of a wavefront and the wavefronts in their order.
-    if (MODE == kNormBack && A.side[side].part) {              // (the same for all)
-        float* part = A.side[side].part;
+        // The weight's gradient: a lane's sums over its rows, then over the groups of a wavefront and the wavefronts in their order.
+        if (MODE == kNormBack && A.side[side].part) {              // (the same for all)
+            float* part = A.side[side].part;
 #pragma unroll
-        for (int j = 0; j < K; j++)
+            for (int j = 0; j < K; j++)
 #pragma unroll
-            for (int i = 0; i < 2 * N; i++) {
-                float v = works ? dw[j][i] : 0.f;
-                if (K == 1 && (group & (group - 1)) == 0) {
-                    for (int d = group; d < 64; d <<= 1) v += __shfl_xor(v, d);
-                } else if (K == 1) {
-                    float all = 0.f;
-                    for (int q = 0; q < A.per_wave; q++) all += __shfl(v, q * group + member);
-                    v = all;
+                for (int i = 0; i < 2 * N; i++) {
+                    float v = works ? dw[j][i] : 0.f;
+                    if (K == 1 && (group & (group - 1)) == 0) {
+                        for (int d = group; d < 64; d <<= 1) v += __shfl_xor(v, d);
+                    } else if (K == 1) {
+                        float all = 0.f;
+                        for (int q = 0; q < A.per_wave; q++) all += __shfl(v, q * group + member);
+                        v = all;
+                    }
+                    const int at = i < N ? first[j] : second[j];
+                    if (place == 0 && at < dim) joined[wave * 512 + at + (i < N ? i : i - N)] = v;
                 }
-                const int at = i < N ? first[j] : second[j];
-                if (place == 0 && at < dim) joined[wave * 512 + at + (i < N ? i : i - N)] = v;
-            }
-        __syncthreads();
-        for (int e = threadIdx.x; e < dim; e += 256)
-            part[(int64_t)blockIdx.x * dim + e] = ((joined[e] + joined[512 + e]) + joined[1024 + e]) + joined[1536 + e];
-        __syncthreads();
-    }
+            __syncthreads();
+            for (int e = threadIdx.x; e < dim; e += 256)
+                part[(int64_t)blockIdx.x * dim + e] = ((joined[e] + joined[512 + e]) + joined[1024 + e]) + joined[1536 + e];
+            __syncthreads();
+        }
     }
 }
 

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/pcr.h"
 #include "pcr_axes.h"

@@ -7,7 +7,6 @@ namespace pcr {
 
 // A run of N elements as it lies in memory; aligned to an element only, so that any row may be read with it.  (The compiler makes one load of
 // up to 16 bytes of it; the hardware takes any alignment, at full speed where the address is a multiple of the run's size.)
-template <typename T, int N> struct Run;
 template <typename T, int N> struct Run {
     typedef T Vec __attribute__((ext_vector_type(N)));
     struct __attribute__((packed, aligned(sizeof(T)))) Loose { Vec v; };
