@@ -8,7 +8,7 @@
 // positions as tensors, and what weights were trained with, 2^-24 of itself off (0.002 radians at position 32768 in the fastest pair).  From there on
 // nothing is lost: the float is reduced to an eighth of a turn with a constant of 48 bits, or, from 2^20 on, in 64-bit fixed point.  (Fixed point for all
 // of them and the compiler's sine and cosine took 511 us for 2 million tokens of one head of queries and keys, which share an angle between two rows;
-// double precision and that 386, this 367.)
+// double precision and that 386, this 367, and 307 with what was gained elsewhere.)
 //
 // Bound by memory: every element is read once and written once.  A workgroup takes a few tokens: its lanes make the tokens' sines and cosines once,
 // in LDS, for all heads of both sides; then a row (a head of a token) goes to a group of lanes, a lane holding one slot: a run of pairs, that is
@@ -16,8 +16,8 @@
 // while one is worked on; a lane steps from row to row by adding (with a division a row, and 64-bit strides, there were 21 instructions an element, and 10 now).
 // us (floor at a large copy's 5.0 TB/s): inverse rotation of 65536 tokens of 40 heads of 128, bfloat 241 (269); rotation of 49999 tokens of 32 heads of 72 in
 // neighbouring pairs, half 92 (92); norm and rotation of 8204 tokens of 16 heads of 96 in 32 bits 19 (20); gradient of norm and rotation of 32768 tokens of
-// 40 heads of 128, bfloat 209 + 5 for the sums (201).  One head of queries and keys alone is not at its floor: 356 (258) for 2 million tokens of 80, its
-// gradient 751 (394); there is an angle to make for every two rows.
+// 40 heads of 128, bfloat 209 + 5 for the sums (201).  One head of queries and keys alone is not at its floor: 307 (258) for 2 million tokens of 80, its
+// gradient behind a norm 735 (394); there is an angle to make for every two rows.
 #pragma once
 #include "pcr_vec.h"
 

@@ -122,7 +122,11 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
         // 32 KB of sines in gradients, and where 1024 workgroups come to it; 16 otherwise.  (Few heads: gradient of 2045759 tokens of one head of queries and keys 751
         // us with 32, 875 with 16, norm and rotation of 41828 tokens 16.1 and 18.9; rotation of 2 million, whose workgroups come and go, 396 and 357.)
         const bool all_at_once = back || (all + 1023) / 1024 * R->pairs <= kAxesTable;
-        chunk = std::min<int64_t>(chunk, (all_at_once ? kAxesTable : kAxesTable / 2) / R->pairs);
+        const int64_t most = (all_at_once ? kAxesTable : kAxesTable / 2) / R->pairs;
+        if (chunk > most) {                                    // ... in whole steps of its wavefronts through the queries' rows (the last one 307 instead of 357)
+            const int64_t step = 4 * A.per_wave, h = std::max<int64_t>(1, q->heads);
+            chunk = most * h > step ? std::max<int64_t>(1, most * h / step * step / h) : most;
+        }
     }
     chunk = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(chunk, 4096), tokens));
     A.chunk = (int)chunk;
