@@ -540,8 +540,8 @@ int pcr_norm_rotate_backward(int device_id, const pcr_heads* q, const pcr_heads*
  *   logits       dtype [rows] with row_stride; top_index int32, or int64 where index_wide is set, [rows][top]; top_logits top_dtype [rows][top]
  *   labels       int64 [rows] or NULL (label_part then has no effect);  classes 1 .. 2^31 - 1, top 1 .. 1024, temperature > 0
  * pcr_distill_forward: loss float [rows]; sums float [rows][2]: logsumexp(z / T), and logsumexp(z) where there are labels and label_part is not 0
- *   (else 0), which the backward pass takes.  (Where all logits of a row are so far from 0 that 32 bits hold no logarithm beside them -- the type's
- *   lowest value throughout -- the sums hold none, and the backward pass misses it; pcr_distill_step of many rows does not.)
+ *   (else 0), which the backward pass takes.  (A sum of 128 or more in magnitude holds too little of the logarithm beside the row's maximum, and none
+ *   where the row is the type's lowest value throughout: the backward pass makes such a row's sums anew from its logits.)
  * pcr_distill_backward: row_grad float [rows]: the gradient of each row's loss; out: dtype, the gradient of the logits with out_stride.  A row
  *   whose row_grad is 0, or that has no term, is zeros whatever its logits hold.
  * pcr_distill_step: loss[n] = row_weight[n] * the row's loss and the gradient of the sum of these, in one pass; a row of weight 0, or without a

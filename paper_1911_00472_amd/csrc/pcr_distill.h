@@ -146,9 +146,9 @@ template <int N, bool TWO> __device__ __forceinline__ void add_run(RowSums& R, c
     }
 }
 
-// Sums over z[0 .. count) by a team: elements in front of the first 16-byte boundary, whole runs, the rest.
-template <typename T, int TEAM, bool TWO> __device__ __forceinline__ RowSums row_sums(const T* z, int64_t count, float c, int tid) {
-    constexpr int N = 16 / sizeof(T), U = 4;
+// Sums over z[0 .. count) by a team: elements in front of the first 16-byte boundary, whole runs (U of a thread's loaded together), the rest.
+template <typename T, int TEAM, bool TWO, int U = 4> __device__ __forceinline__ RowSums row_sums(const T* z, int64_t count, float c, int tid) {
+    constexpr int N = 16 / sizeof(T);
     RowSums R = {-INFINITY, 0.f, 0.f};
     const int64_t lead = min(count, (int64_t)((-(uintptr_t)z & 15) / sizeof(T)));
     const int64_t runs = (count - lead) / N, tail = lead + runs * N;
@@ -172,19 +172,33 @@ template <typename T, int TEAM, bool TWO> __device__ __forceinline__ RowSums row
 
 __device__ __forceinline__ float scaled(float s, float m, float most, float c) { return m == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f((m - most) * c); }
 
-// The dense part of the gradient of one element.
-struct Dense { float inv_T, L, L1, ca, cb; };
-template <bool TWO> __device__ __forceinline__ float dense_of(float x, const Dense& D) {
-    float v = D.ca * __builtin_amdgcn_exp2f(__builtin_fmaf(x, D.inv_T, -D.L) * kLog2e);
-    if (TWO) v = __builtin_fmaf(D.cb, __builtin_amdgcn_exp2f((x - D.L1) * kLog2e), v);
-    return v;
-}
-template <typename T, int TEAM, bool TWO> __device__ __forceinline__ void write_dense(const T* z, T* out, int64_t count, const Dense& D, int tid) {
+// The dense part of the gradient of one element: against saved sums, or against the row's maximum (ca and cb are then divided by the sums).
+template <bool TWO> struct BySaved {
+    float inv_T, L, L1, ca, cb;
+    __device__ __forceinline__ float operator()(float x) const {
+        float v = ca * __builtin_amdgcn_exp2f(__builtin_fmaf(x, inv_T, -L) * kLog2e);
+        if (TWO) v = __builtin_fmaf(cb, __builtin_amdgcn_exp2f((x - L1) * kLog2e), v);
+        return v;
+    }
+};
+template <bool TWO> struct ByMaximum {
+    float c, m, ca, cb;
+    __device__ __forceinline__ float operator()(float x) const {
+        const float v = ca * __builtin_amdgcn_exp2f((x - m) * c);
+        return TWO ? __builtin_fmaf(cb, __builtin_amdgcn_exp2f((x - m) * kLog2e), v) : v;
+    }
+};
+// Saved sums that are too far from 0: from 128 on the two roundings in one come to more than 2^-17, and every element of the gradient is off by that part of
+// itself; where a float holds nothing of the sum's logarithm beside the maximum, x / T less it is a rounding error of any size.  The maximum and the sums of
+// such a row are made anew.
+__device__ __forceinline__ bool saved_too_far(float L) { return !(__builtin_fabsf(L) < 128.f); }
+
+template <typename T, int TEAM, typename D> __device__ __forceinline__ void write_dense(const T* z, T* out, int64_t count, const D& dense, int tid) {
     constexpr int N = 16 / sizeof(T), U = 4;
     const int64_t lead = min(count, (int64_t)((-(uintptr_t)out & 15) / sizeof(T)));
     const int64_t runs = (count - lead) / N, tail = lead + runs * N;
-    if (tid < lead) { float x[1]; load_run<T, 1>(z + tid, x); x[0] = dense_of<TWO>(x[0], D); store_run<T, 1>(out + tid, x); }
-    if (tail + tid < count) { float x[1]; load_run<T, 1>(z + tail + tid, x); x[0] = dense_of<TWO>(x[0], D); store_run<T, 1>(out + tail + tid, x); }
+    if (tid < lead) { float x[1]; load_run<T, 1>(z + tid, x); x[0] = dense(x[0]); store_run<T, 1>(out + tid, x); }
+    if (tail + tid < count) { float x[1]; load_run<T, 1>(z + tail + tid, x); x[0] = dense(x[0]); store_run<T, 1>(out + tail + tid, x); }
     int64_t r = tid;
     for (; r + (U - 1) * TEAM < runs; r += U * TEAM) {
         float x[U][N];
@@ -193,7 +207,7 @@ template <typename T, int TEAM, bool TWO> __device__ __forceinline__ void write_
 #pragma unroll
         for (int u = 0; u < U; u++) {
 #pragma unroll
-            for (int i = 0; i < N; i++) x[u][i] = dense_of<TWO>(x[u][i], D);
+            for (int i = 0; i < N; i++) x[u][i] = dense(x[u][i]);
             store_run<T, N>(out + lead + (r + u * TEAM) * N, x[u]);
         }
     }
@@ -201,7 +215,7 @@ template <typename T, int TEAM, bool TWO> __device__ __forceinline__ void write_
         float x[N];
         load_run<T, N>(z + lead + r * N, x);
 #pragma unroll
-        for (int i = 0; i < N; i++) x[i] = dense_of<TWO>(x[i], D);
+        for (int i = 0; i < N; i++) x[i] = dense(x[i]);
         store_run<T, N>(out + lead + r * N, x);
     }
 }
@@ -224,7 +238,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
     if (unit >= A.rows * A.chunks) return;                     // (a whole wavefront, or nobody of a workgroup that shares a row)
     const int64_t n = unit / A.chunks;
     const int share = (int)(unit - n * A.chunks);
-    const int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
+    int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
     float* join = lds + team * (16 + entry_floats(A.K, A.chunk));
     Entries E(join + 16, A.K, A.chunk);
     const T* z = (const T*)A.logits + n * A.row_stride;
@@ -236,6 +250,15 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
         if (MODE == kStep && tid == 0) A.loss[n] = 0.f;
         return;
     }
+    // A row whose sums are made anew goes to one team whole: it is read before any of it is written, which may be in its place.
+    const float saved = MODE == kGrad ? A.sums_in[2 * n] : 0.f, saved1 = MODE == kGrad ? A.sums_in[2 * n + 1] : 0.f;
+    const bool anew = MODE != kGrad || saved_too_far(saved) || (TWO && saved_too_far(saved1));
+    if (MODE == kGrad && anew) {
+        if (share) return;
+        count = A.V;
+    }
+    // Where a class has its bit: the chunk's bits are taken again for every chunk of a whole row.
+    auto place = [&](int64_t v) { return MODE == kGrad && anew ? (uint32_t)v % (uint32_t)A.chunk : (uint32_t)(v - v0); };
     if (MODE != kLoss) E.clear<TEAM>(tid);
     // entries: softmax of the teacher's logits over those that count
     float most = load_entries<T, TEAM>(A, n, z, E, tid);
@@ -248,23 +271,22 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
     total = team_join<TEAM, false>(total, join);
     const bool kept = most != -INFINITY;
 
-    // What the dense part is taken against: the saved sums, or (exact also where the logarithm is lost beside it) the maximum and the sum's reciprocal.
-    float L, L1, over = 1.f, over1 = 1.f;
-    if (MODE == kGrad) {
-        L = A.sums_in[2 * n]; L1 = A.sums_in[2 * n + 1];
-    } else {
-        if (MODE == kStep && !kept && !labelled) {
-            write_zeros<T, TEAM>(out, count, tid);
-            if (tid == 0) A.loss[n] = 0.f;
-            return;
-        }
-        RowSums R = row_sums<T, TEAM, TWO>(z, A.V, A.inv_T * kLog2e, tid);
-        const float m = team_join<TEAM, true>(R.m, join);
-        const float s = team_join<TEAM, false>(scaled(R.s, R.m, m, A.inv_T * kLog2e), join);
-        const float s1 = TWO ? team_join<TEAM, false>(scaled(R.s1, R.m, m, kLog2e), join) : s;
-        const float log_s = logf(s), log_s1 = TWO ? logf(s1) : log_s;
-        L = m * A.inv_T; L1 = m;
-        over = 1.f / s; over1 = 1.f / s1;
+    if (MODE != kLoss && !kept && !labelled) {
+        write_zeros<T, TEAM>(out, count, tid);
+        if (MODE == kStep && tid == 0) A.loss[n] = 0.f;
+        return;
+    }
+    // What the dense part is taken against: the saved sums, or (exact also where the logarithm is lost beside it) the maximum and the sums' reciprocals.
+    const float c = A.inv_T * kLog2e;
+    float m = 0.f, s = 1.f, s1 = 1.f;
+    if (anew) {
+        RowSums R = row_sums<T, TEAM, TWO, MODE == kGrad ? 1 : 4>(z, A.V, c, tid);     // (a gradient keeps its registers, and with them two workgroups a compute unit)
+        m = team_join<TEAM, true>(R.m, join);
+        s = team_join<TEAM, false>(scaled(R.s, R.m, m, c), join);
+        s1 = TWO ? team_join<TEAM, false>(scaled(R.s1, R.m, m, kLog2e), join) : s;
+    }
+    if (MODE != kGrad) {
+        const float L = m * A.inv_T, log_s = logf(s), log_s1 = TWO ? logf(s1) : log_s;
         float sum = 0.f;
         for (int k = tid; k < A.K; k += TEAM)
             if (E.at[k] >= 0) {
@@ -280,31 +302,31 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
         }
     }
     if (MODE == kLoss) return;
-    if (!kept && !labelled) {
-        write_zeros<T, TEAM>(out, count, tid);
-        return;
-    }
-    Dense D = {A.inv_T, L, L1, kept ? g * A.a * A.T * over : 0.f, labelled ? g * A.b * over1 : 0.f};
-    if (!TWO) D.ca += D.cb;
     team_sync<TEAM>();                                         // (the bits are cleared)
     for (int k = tid; k < A.K; k += TEAM) {
         const int64_t v = E.at[k];
         E.delta[k] = v >= 0 ? -g * A.a * A.T * (__builtin_amdgcn_exp2f((E.delta[k] - most) * kLog2e) / total) : 0.f;
-        if (v >= v0 && v < v0 + count) E.mark((uint32_t)(v - v0));
+        if (v >= v0 && v < v0 + count) E.mark(place(v));
         if (labelled && v == label) *E.labelled = 1;
     }
-    write_dense<T, TEAM, TWO>(z + v0, out, count, D, tid);
-    team_sync<TEAM>();                                         // the dense part is written, the entries are marked
-    for (int e = tid; e < A.K; e += TEAM) {
-        const int64_t v = E.at[e];
-        if (v < v0 || v >= v0 + count) continue;
-        const float x[1] = {dense_of<TWO>(E.logit[e], D) + (E.sum(e, (uint32_t)(v - v0), A.K) - (v == label ? g * A.b : 0.f))};
-        store_run<T, 1>(out + (v - v0), x);
-    }
-    if (tid == 0 && labelled && !*E.labelled && label >= v0 && label < v0 + count) {
-        const float x[1] = {dense_of<TWO>(zl, D) - g * A.b};
-        store_run<T, 1>(out + (label - v0), x);
-    }
+    auto write = [&](auto dense) {
+        if (!TWO) dense.ca += dense.cb;
+        write_dense<T, TEAM>(z + v0, out, count, dense, tid);
+        team_sync<TEAM>();                                     // the dense part is written, the entries are marked
+        for (int e = tid; e < A.K; e += TEAM) {
+            const int64_t v = E.at[e];
+            if (v < v0 || v >= v0 + count) continue;
+            const float x[1] = {dense(E.logit[e]) + (E.sum(e, place(v), A.K) - (v == label ? g * A.b : 0.f))};
+            store_run<T, 1>(out + (v - v0), x);
+        }
+        if (tid == 0 && labelled && !*E.labelled && label >= v0 && label < v0 + count) {
+            const float x[1] = {dense(zl) - g * A.b};
+            store_run<T, 1>(out + (label - v0), x);
+        }
+    };
+    const float ca = kept ? g * A.a * A.T : 0.f, cb = labelled ? g * A.b : 0.f;
+    if (anew) write(ByMaximum<TWO>{c, m, ca / s, cb / s1});
+    else if (MODE == kGrad) write(BySaved<TWO>{A.inv_T, saved, saved1, ca, cb});
 }
 
 // Several values at a time, with one barrier: `lds` holds C floats for every wavefront of the team and is used by no other join.
@@ -376,6 +398,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     if (TEAM > 64 && WRITES && g == 0.f) return left_out();
     const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
     const float saved = SUMS ? 0.f : A.sums_in[2 * n], saved1 = SUMS ? 0.f : A.sums_in[2 * n + 1];
+    const bool anew = SUMS || saved_too_far(saved) || (BY != kOneSum && saved_too_far(saved1));
     const int V = (int)A.V, lead = min(V, (int)((-(uintptr_t)z & 15) / sizeof(T))), runs = (V - lead) / N, tail = lead + runs * N;
     if (WRITES) E.clear<TEAM>(tid);
     Vec raw[R];
@@ -393,7 +416,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     float most[2] = {x_edge, load_entries<T, TEAM>(A, n, z, E, tid)};            // of the logits, of the kept teacher's logits
     const bool labelled = label >= 0 && label < A.V;
     const float zl = labelled ? (float)z[label] : 0.f;
-    if (SUMS) {
+    if (anew) {
 #pragma unroll
         for (int u = 0; u < R; u++)
 #pragma unroll
@@ -410,7 +433,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         sum[0] += e;
         sum[1] += e1;
     };
-    if (SUMS) {
+    if (anew) {
 #pragma unroll
         for (int u = 0; u < R; u++) {
             if (u * TEAM < runs) {                             // (the same for the team)
@@ -427,7 +450,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     if (BY == kOneSum) sum[1] = sum[0];
     const float total = sum[2], L = m * A.inv_T, log_s = logf(sum[0]), log_s1 = logf(sum[1]), log_total = logf(total);
     const float unit = -g * A.a * A.T;
-    const float ca = kept ? (SUMS ? -unit / sum[0] : -unit) : 0.f, cb = labelled ? (SUMS ? g * A.b / sum[1] : g * A.b) : 0.f;
+    const float ca = kept ? (anew ? -unit / sum[0] : -unit) : 0.f, cb = labelled ? (anew ? g * A.b / sum[1] : g * A.b) : 0.f;
 
     // entries: their share of the loss, and what each adds to the dense part of its class
     auto finish = [&](float entries) {                         // the row's loss, from the sum of the entries' shares
@@ -458,34 +481,40 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         }
         return;
     }
-    const Dense D = {A.inv_T, saved, saved1, BY == kOneSum ? ca + cb : ca, cb};
-    auto dense = [&](float x) {
-        if (!SUMS) return dense_of<BY == kTwoSums>(x, D);
-        float e, e1 = 0.f;
-        exps<BY>(x, m, c, A.T, e, e1);
-        if (BY == kOneSum) return (ca + cb) * e;
-        if (BY == kSquare) return e * __builtin_fmaf(cb, e, ca);
-        return __builtin_fmaf(cb, e1, ca * e);
-    };
-    T* to = out + lead;
+    auto write = [&](auto dense) {
+        T* to = out + lead;
 #pragma unroll
-    for (int u = 0; u < R; u++)
-        if (tid + u * TEAM < runs) {
-            float x[N];
-            take_again<T>(raw[u], x);
+        for (int u = 0; u < R; u++)
+            if (tid + u * TEAM < runs) {
+                float x[N];
+                take_again<T>(raw[u], x);
 #pragma unroll
-            for (int i = 0; i < N; i++) x[i] = dense(x[i]);
-            store_run<T, N>(to + (tid + u * TEAM) * N, x);
+                for (int i = 0; i < N; i++) x[i] = dense(x[i]);
+                store_run<T, N>(to + (tid + u * TEAM) * N, x);
+            }
+        if (edged) out[edge] = (T)dense(x_edge);
+        team_join_all<TEAM, 1, false>(loss, join + 5 * W);     // (the dense part and the entries are behind this barrier, too)
+        team_sync<TEAM>();
+        if (SUMS && tid == 0) finish(loss[0]);
+        for (int e = tid; e < A.K; e += TEAM) {
+            const int v = E.at[e];
+            if (v >= 0) out[v] = (T)(dense(E.logit[e]) + (E.sum(e, (uint32_t)v, A.K) - (v == label ? g * A.b : 0.f)));
         }
-    if (edged) out[edge] = (T)dense(x_edge);
-    team_join_all<TEAM, 1, false>(loss, join + 5 * W);         // (the dense part and the entries are behind this barrier, too)
-    team_sync<TEAM>();
-    if (SUMS && tid == 0) finish(loss[0]);
-    for (int e = tid; e < A.K; e += TEAM) {
-        const int v = E.at[e];
-        if (v >= 0) out[v] = (T)(dense(E.logit[e]) + (E.sum(e, (uint32_t)v, A.K) - (v == label ? g * A.b : 0.f)));
+        if (tid == 0 && labelled && !*E.labelled) out[label] = (T)(dense(zl) - g * A.b);
+    };
+    if constexpr (SUMS) {
+        write([&](float x) {
+            float e, e1 = 0.f;
+            exps<BY>(x, m, c, A.T, e, e1);
+            if (BY == kOneSum) return (ca + cb) * e;
+            if (BY == kSquare) return e * __builtin_fmaf(cb, e, ca);
+            return __builtin_fmaf(cb, e1, ca * e);
+        });
+    } else {
+        constexpr bool TWO = BY != kOneSum;
+        if (anew) write(ByMaximum<TWO>{c, m, TWO ? ca : ca + cb, cb});
+        else write(BySaved<TWO>{A.inv_T, saved, saved1, TWO ? ca : ca + cb, cb});
     }
-    if (tid == 0 && labelled && !*E.labelled) out[label] = (T)(dense(zl) - g * A.b);
 }
 
 // Few rows: shares of a row are summed by workgroups of their own and joined by k_distill_join, a wavefront to a row.
