@@ -63,8 +63,8 @@ __device__ __forceinline__ int64_t top_class(const DistillArgs& A, int64_t at) {
     return v >= 0 && v < A.V ? v : -1;
 }
 
-// The kept entries of a row in LDS: class (-1: it does not count), the teacher's logit over T and later what the entry adds to its class's gradient, the
-// student's logit.  `seen` and `several`: a bit for every class (for every 65536th, of more classes) that an entry, or several, have; only the latter look for
+// The kept entries of a row in LDS: class (-1: it does not count), the teacher's logit and later what the entry adds to its class's gradient, the
+// student's logit.  (Differences are taken before they are divided by T: a mask's value over a T below 1 is infinite.)  `seen` and `several`: a bit for every class (for every 65536th, of more classes) that an entry, or several, have; only the latter look for
 // each other.  (Every entry looking at every other took 143 us for 11145 rows of 344 classes with 256 entries.)
 constexpr int64_t kEntryBits = 65536;
 __host__ __device__ inline int entry_words(int64_t classes) { return (int)((classes < kEntryBits ? classes : kEntryBits) + 31) / 32; }
@@ -107,7 +107,7 @@ template <typename T, int TEAM> __device__ __forceinline__ float load_entries(co
         for (int j = 0; j < B; j++) {
             const int k = k0 + j * TEAM;
             v[j] = k < A.K && A.a != 0.f ? top_class(A, n * A.K + k) : -1;
-            t[j] = k < A.K ? top_logit(A, n * A.K + k) * A.inv_T : -INFINITY;
+            t[j] = k < A.K ? top_logit(A, n * A.K + k) : -INFINITY;
         }
 #pragma unroll
         for (int j = 0; j < B; j++) {
@@ -266,8 +266,9 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
     const bool labelled = label >= 0 && label < A.V;
     const float zl = labelled ? (float)z[label] : 0.f;
     most = team_join<TEAM, true>(most, join);
+    const float c = A.inv_T * kLog2e;
     float total = 0.f;
-    for (int k = tid; k < A.K; k += TEAM) if (E.at[k] >= 0) total += __builtin_amdgcn_exp2f((E.delta[k] - most) * kLog2e);
+    for (int k = tid; k < A.K; k += TEAM) if (E.at[k] >= 0) total += __builtin_amdgcn_exp2f((E.delta[k] - most) * c);
     total = team_join<TEAM, false>(total, join);
     const bool kept = most != -INFINITY;
 
@@ -277,7 +278,6 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
         return;
     }
     // What the dense part is taken against: the saved sums, or (exact also where the logarithm is lost beside it) the maximum and the sums' reciprocals.
-    const float c = A.inv_T * kLog2e;
     float m = 0.f, s = 1.f, s1 = 1.f;
     if (anew) {
         RowSums R = row_sums<T, TEAM, TWO, MODE == kGrad ? 1 : 4>(z, A.V, c, tid);     // (a gradient keeps its registers, and with them two workgroups a compute unit)
@@ -286,26 +286,26 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
         s1 = TWO ? team_join<TEAM, false>(scaled(R.s1, R.m, m, kLog2e), join) : s;
     }
     if (MODE != kGrad) {
-        const float L = m * A.inv_T, log_s = logf(s), log_s1 = TWO ? logf(s1) : log_s;
+        const float log_s = logf(s), log_s1 = TWO ? logf(s1) : log_s;
         float sum = 0.f;
         for (int k = tid; k < A.K; k += TEAM)
             if (E.at[k] >= 0) {
-                const float t = E.delta[k] - most, e = __builtin_amdgcn_exp2f(t * kLog2e);
-                if (e > 0.f || t != t) sum += e * ((t - logf(total)) - ((E.logit[k] * A.inv_T - L) - log_s));
+                const float t = (E.delta[k] - most) * A.inv_T, e = __builtin_amdgcn_exp2f((E.delta[k] - most) * c);
+                if (e > 0.f || t != t) sum += e * ((t - logf(total)) - ((E.logit[k] - m) * A.inv_T - log_s));
             }
         sum = team_join<TEAM, false>(sum, join);
         if (tid == 0) {
             float loss = kept ? A.a * A.T * A.T * (sum / total) : 0.f;
             if (labelled) loss += A.b * (log_s1 - (zl - m));
             A.loss[n] = g * loss;
-            if (MODE == kLoss) { A.sums[2 * n] = L + log_s; A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f; }
+            if (MODE == kLoss) { A.sums[2 * n] = m * A.inv_T + log_s; A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f; }
         }
     }
     if (MODE == kLoss) return;
     team_sync<TEAM>();                                         // (the bits are cleared)
     for (int k = tid; k < A.K; k += TEAM) {
         const int64_t v = E.at[k];
-        E.delta[k] = v >= 0 ? -g * A.a * A.T * (__builtin_amdgcn_exp2f((E.delta[k] - most) * kLog2e) / total) : 0.f;
+        E.delta[k] = v >= 0 ? -g * A.a * A.T * (__builtin_amdgcn_exp2f((E.delta[k] - most) * c) / total) : 0.f;
         if (v >= v0 && v < v0 + count) E.mark(place(v));
         if (labelled && v == label) *E.labelled = 1;
     }
@@ -445,10 +445,10 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         }
         if (edged) add(x_edge);
     }
-    for (int k = tid; k < A.K; k += TEAM) if (E.at[k] >= 0) sum[2] += __builtin_amdgcn_exp2f((E.delta[k] - most[1]) * kLog2e);
+    for (int k = tid; k < A.K; k += TEAM) if (E.at[k] >= 0) sum[2] += __builtin_amdgcn_exp2f((E.delta[k] - most[1]) * c);
     team_join_all<TEAM, 3, false>(sum, join + 2 * W);
     if (BY == kOneSum) sum[1] = sum[0];
-    const float total = sum[2], L = m * A.inv_T, log_s = logf(sum[0]), log_s1 = logf(sum[1]), log_total = logf(total);
+    const float total = sum[2], log_s = logf(sum[0]), log_s1 = logf(sum[1]), log_total = logf(total);
     const float unit = -g * A.a * A.T;
     const float ca = kept ? (anew ? -unit / sum[0] : -unit) : 0.f, cb = labelled ? (anew ? g * A.b / sum[1] : g * A.b) : 0.f;
 
@@ -464,8 +464,8 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         const int v = E.at[k];
         float d = 0.f;
         if (v >= 0) {
-            const float t = E.delta[k] - most[1], e = __builtin_amdgcn_exp2f(t * kLog2e);
-            if (SUMS && (e > 0.f || t != t)) loss[0] += e * ((t - log_total) - ((E.logit[k] * A.inv_T - L) - log_s));
+            const float t = (E.delta[k] - most[1]) * A.inv_T, e = __builtin_amdgcn_exp2f((E.delta[k] - most[1]) * c);
+            if (SUMS && (e > 0.f || t != t)) loss[0] += e * ((t - log_total) - ((E.logit[k] - m) * A.inv_T - log_s));
             d = unit * (e / total);
             if (WRITES) E.mark((uint32_t)v);
             if (WRITES && labelled && v == label) *E.labelled = 1;
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         team_join_all<TEAM, 1, false>(loss, join + 5 * W);
         if (tid == 0) {
             finish(loss[0]);
-            A.sums[2 * n] = L + log_s;
+            A.sums[2 * n] = m * A.inv_T + log_s;
             A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f;
         }
         return;
@@ -550,21 +550,21 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A) {
         if (TWO) s1 += scaled(p[2], p[0], m, kLog2e);
     }
     s = team_join<64, false>(s, nullptr);
-    const float L = m * A.inv_T, log_s = logf(s), log_s1 = TWO ? logf(team_join<64, false>(s1, nullptr)) : log_s;
+    const float log_s = logf(s), log_s1 = TWO ? logf(team_join<64, false>(s1, nullptr)) : log_s;
     float most = -INFINITY, total = 0.f, sum = 0.f;
     for (int k = lane; k < A.K; k += 64) {
         const int64_t v = A.a != 0.f ? top_class(A, n * A.K + k) : -1;
-        const float t = v >= 0 ? top_logit(A, n * A.K + k) * A.inv_T : -INFINITY;
+        const float t = v >= 0 ? top_logit(A, n * A.K + k) : -INFINITY;
         most = fmaxf(most, t == t ? t : INFINITY);             // (of a NaN all that follows is one)
     }
     most = team_join<64, true>(most, nullptr);
     for (int k = lane; k < A.K; k += 64) {
         const int64_t v = A.a != 0.f ? top_class(A, n * A.K + k) : -1;
-        const float t = v >= 0 ? top_logit(A, n * A.K + k) * A.inv_T - most : -INFINITY;
-        if (v < 0 || t == -INFINITY) continue;
-        const float e = __builtin_amdgcn_exp2f(t * kLog2e);
+        const float d = v >= 0 ? top_logit(A, n * A.K + k) - most : -INFINITY, t = d * A.inv_T;
+        if (v < 0 || d == -INFINITY) continue;
+        const float e = __builtin_amdgcn_exp2f(d * c);
         total += e;
-        if (e > 0.f || t != t) sum += e * (t - (((float)z[v] * A.inv_T - L) - log_s));
+        if (e > 0.f || t != t) sum += e * (t - (((float)z[v] - m) * A.inv_T - log_s));
     }
     total = team_join<64, false>(total, nullptr);
     sum = team_join<64, false>(sum, nullptr);
@@ -574,7 +574,7 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A) {
         if (label >= 0 && label < A.V) loss += A.b * (log_s1 - ((float)z[label] - m));
         const float g = A.row_grad ? A.row_grad[n] : 1.f;
         A.loss[n] = g == 0.f ? 0.f : g * loss;
-        A.sums[2 * n] = L + log_s; A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f;
+        A.sums[2 * n] = m * A.inv_T + log_s; A.sums[2 * n + 1] = A.two ? m + log_s1 : 0.f;
     }
 }
 
