@@ -23,6 +23,7 @@ struct DistillArgs {
     const float* sums_in; const float* row_grad;              // backward: saved sums; step: row_grad holds the rows' weights
     float* loss; float* sums; void* out; float* part;
     int64_t row_stride, out_stride, rows, V;
+    int64_t first;                                             // workgroups of launches before this one
     int64_t chunk; int chunks;                                 // classes of a workgroup's share of a row, shares of a row
     int K, top_dtype, wide, two;
     float T, inv_T, a, b;
@@ -234,7 +235,7 @@ template <typename T, int TEAM, bool TWO, int MODE>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs A) {
     extern __shared__ float lds[];                             // a team's: joins [16], entries
     const int tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const int64_t unit = (int64_t)blockIdx.x * (TEAM < 256 ? 256 / TEAM : 1) + team;
+    const int64_t unit = (A.first + blockIdx.x) * (TEAM < 256 ? 256 / TEAM : 1) + team;
     if (unit >= A.rows * A.chunks) return;                     // (a whole wavefront, or nobody of a workgroup that shares a row)
     const int64_t n = unit / A.chunks;
     const int share = (int)(unit - n * A.chunks);
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     constexpr int N = 16 / sizeof(T), W = TEAM / 64;
     typedef typename Run<T, N>::Vec Vec;
     const int tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const int64_t n = (int64_t)blockIdx.x * (TEAM < 256 ? 256 / TEAM : 1) + team;
+    const int64_t n = (A.first + blockIdx.x) * (TEAM < 256 ? 256 / TEAM : 1) + team;
     if (n >= A.rows) return;                                   // (a whole wavefront, or nobody of a workgroup that shares a row)
     float* join = lds + team * (6 * W + entry_floats(A.K, A.V));
     Entries E(join + 6 * W, A.K, A.V);

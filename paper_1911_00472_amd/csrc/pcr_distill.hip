@@ -52,12 +52,14 @@ void cut(DistillArgs& A, int64_t parts) {
     A.chunks = (int)((A.V + A.chunk - 1) / A.chunk);
 }
 
-template <typename T, int TEAM, int MODE> void launch_team(const DistillArgs& A, hipStream_t s) {
+template <typename T, int TEAM, int MODE> void launch_team(DistillArgs A, hipStream_t s) {
     const int teams = TEAM < 256 ? 256 / TEAM : 1, threads = TEAM < 256 ? 256 : TEAM;
-    const unsigned groups = (unsigned)((A.rows * A.chunks + teams - 1) / teams);
     const size_t lds = (size_t)teams * (16 + entry_floats(A.K, A.chunk)) * sizeof(float);
-    if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(threads), lds, s, A);
-    else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(threads), lds, s, A);
+    in_ranges((A.rows * A.chunks + teams - 1) / teams, threads, [&](int64_t first, unsigned groups) {
+        A.first = first;
+        if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(threads), lds, s, A);
+        else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(threads), lds, s, A);
+    });
 }
 // The gradient from saved sums of rows for more than a wavefront, and (MODE kLoss, kStep) rows too long for a team's registers, read twice.
 template <int MODE> void launch_distill(const DistillArgs& A, int dtype, hipStream_t s) {
@@ -71,16 +73,18 @@ template <int MODE> void launch_distill(const DistillArgs& A, int dtype, hipStre
     });
 }
 // A team that holds a row in its registers, the smallest there is: false if there is none.
-template <typename T, int TEAM, int R, int MODE> bool launch_rows(const DistillArgs& A, hipStream_t s) {
+template <typename T, int TEAM, int R, int MODE> bool launch_rows(DistillArgs A, hipStream_t s) {
     constexpr int N = 16 / sizeof(T);
     if (A.V > (int64_t)TEAM * R * N) return false;             // (elements in front of and behind the runs are held beside them)
     const int teams = TEAM < 256 ? 256 / TEAM : 1, threads = TEAM < 256 ? 256 : TEAM;
-    const dim3 groups((unsigned)((A.rows + teams - 1) / teams));
     const size_t lds = (size_t)teams * (6 * (TEAM / 64) + entry_floats(A.K, A.V)) * sizeof(float);
-    if (!A.two || A.T == 1.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kOneSum, MODE>), groups, dim3(threads), lds, s, A);
-    else if (MODE != kGrad && A.T == 2.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, MODE == kGrad ? kTwoSums : kSquare, MODE>), groups, dim3(threads), lds, s, A);
-    else if (MODE != kGrad && A.T == 4.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, MODE == kGrad ? kTwoSums : kFourth, MODE>), groups, dim3(threads), lds, s, A);
-    else hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kTwoSums, MODE>), groups, dim3(threads), lds, s, A);
+    in_ranges((A.rows + teams - 1) / teams, threads, [&](int64_t first, unsigned groups) {
+        A.first = first;
+        if (!A.two || A.T == 1.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kOneSum, MODE>), dim3(groups), dim3(threads), lds, s, A);
+        else if (MODE != kGrad && A.T == 2.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, MODE == kGrad ? kTwoSums : kSquare, MODE>), dim3(groups), dim3(threads), lds, s, A);
+        else if (MODE != kGrad && A.T == 4.f) hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, MODE == kGrad ? kTwoSums : kFourth, MODE>), dim3(groups), dim3(threads), lds, s, A);
+        else hipLaunchKernelGGL((k_distill_rows<T, TEAM, R, kTwoSums, MODE>), dim3(groups), dim3(threads), lds, s, A);
+    });
     return true;
 }
 // Whether rows go to a wavefront each: short ones, unless there are so few that a workgroup each is done sooner.  (us, wavefronts / workgroups of 256, gradient

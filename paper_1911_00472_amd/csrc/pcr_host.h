@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/pcr.h"
 
 namespace pcr {
@@ -20,6 +22,13 @@ struct OnDevice {
     }
     ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
 };
+
+// f(first, count) for ranges of a grid of `groups` workgroups: a launch holds fewer than 2^32 threads.
+inline int64_t groups_of_a_launch(int threads) { return 4294967295ll / threads; }
+template <typename F> void in_ranges(int64_t groups, int threads, F f) {
+    const int64_t most = groups_of_a_launch(threads);
+    for (int64_t first = 0; first < groups; first += most) f(first, (unsigned)std::min(most, groups - first));
+}
 
 inline int launched() { return hipGetLastError() == hipSuccess ? PCR_OK : PCR_E_DEVICE; }
 

@@ -15,6 +15,7 @@ constexpr int kPatchGroup = 64;                                // rows of a work
 struct PatchArgs {
     const uint8_t* pixels; const int32_t* shape; const int64_t* offset; const int64_t* first;
     int64_t n, rows, pixel_bytes;
+    int64_t begin;                                             // workgroups of launches before this one
     int patch, merge, frames, group;
     uint32_t by_each, by_runs;                                 // 2^32 / (runs of a patch), 2^32 / (runs of a line of it), rounded up
     float scale[3], shift[3];
@@ -75,7 +76,7 @@ template <typename T, int C, bool STAGED>
 __global__ __launch_bounds__(256) void k_patch_rows(PatchArgs A) {
     __shared__ Patch patches[kPatchGroup];
     extern __shared__ __attribute__((aligned(16))) uint8_t staged[];
-    const int64_t r0 = (int64_t)blockIdx.x * A.group;
+    const int64_t r0 = (A.begin + blockIdx.x) * A.group;
     const int P = A.patch, m = A.merge, here = (int)min((int64_t)A.group, A.rows - r0);
     if (threadIdx.x < 64) {                                    // (a wavefront)
         int64_t i = picture_of(A, r0);

@@ -134,7 +134,7 @@ int run_axes(int device, const pcr_heads* q, const pcr_heads* k, const pcr_rotat
     A.shares = tokens ? (tokens + chunk - 1) / chunk : 0;
     A.chunks = batch * A.shares;
     if (!A.shares) A.shares = 1;
-    int groups = (int)(back ? std::min<int64_t>(A.chunks, kBackGroups) : A.chunks);
+    int groups = (int)std::min<int64_t>(A.chunks, back ? kBackGroups : groups_of_a_launch(256));
     // (us, one after the other / apart: norm and rotation of 256 tokens of 40 heads 6.7 / 6.2, of 1000 9.2 / 10.5; gradient of 64 tokens of 40 heads 14.4 / 10.4,
     // of 5006 of 31 of 64, 626 workgroups, 25.2 / 20.8, of 3000 of 56, 1000 workgroups, 37.2 / 38.3)
     A.apart = q->heads && k->heads && groups <= (back ? 768 : 512);
@@ -213,8 +213,10 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
     with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         auto launch = [&](auto c, auto s) {
-            hipLaunchKernelGGL((k_patch_rows<T, decltype(c)::value, decltype(s)::value>), dim3((unsigned)((rows + A.group - 1) / A.group)), dim3(256), staged ? A.group * row_bytes : 0,
-                               (hipStream_t)hip_stream, A);
+            in_ranges((rows + A.group - 1) / A.group, 256, [&](int64_t begin, unsigned groups) {
+                A.begin = begin;
+                hipLaunchKernelGGL((k_patch_rows<T, decltype(c)::value, decltype(s)::value>), dim3(groups), dim3(256), staged ? A.group * row_bytes : 0, (hipStream_t)hip_stream, A);
+            });
         };
         auto by_channels = [&](auto s) {
             if (channels == 3) launch(std::integral_constant<int, 3>(), s);
