@@ -488,7 +488,7 @@ enum { PCR_FLOAT = 0, PCR_HALF = 1, PCR_BFLOAT = 2 };          /* IEEE 32 bits, 
  *   patch       side, 1 .. 128; merge: 1 .. 16.  Rows go through windows of merge x merge patches, window after window and, in a window,
  *               line after line (merge 1: line after line through the picture), so that patches that are merged later are neighbours
  *   frames      pictures of a clip: the first position is i mod frames (1: zero for single pictures)
- *   channels    1 or 3; mean, inv_std (host): as in pcr_crop_resize_batch
+ *   channels    of every picture, 1 or 3; mean, inv_std (host): as in pcr_crop_resize_batch
  *   d_out       dtype [rows][channels][patch][patch]: (pixel / 255 - mean) inv_std, 0 outside the picture; rows that belong to no
  *               picture's grid are 0
  *   d_positions int32 [3][rows], may be NULL: frame, row and column of the patch (0 for rows of no picture) */

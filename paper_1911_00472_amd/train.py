@@ -34,7 +34,8 @@ def _call(stream, f, *args):
 
 def patch_layout(shapes, channels, patch, merge=1, offsets=None, device=0):
     """What patch_rows needs to know of pictures of the given (height, width), one behind the other as decode_batch writes them (offsets: where
-    each begins, and the end): (shapes int32 [n, 2], offsets int64 [n + 1], first_rows int64 [n + 1]) as CUDA tensors, and the number of rows."""
+    each begins, and the end): (shapes int32 [n, 2], offsets int64 [n + 1], first_rows int64 [n + 1]) as CUDA tensors, and the number of rows.
+    shapes keeps the pictures' channels (an attribute of that name), which patch_rows holds against the number of means."""
     hw = np.asarray(shapes, np.int64).reshape(-1, 2)
     cell = patch * merge
     rows = np.where((hw > 0).all(1), (-(-hw // cell) * merge).prod(1), 0)
@@ -42,8 +43,9 @@ def patch_layout(shapes, channels, patch, merge=1, offsets=None, device=0):
         offsets = np.concatenate([[0], np.cumsum(hw.prod(1) * channels)])
     first = np.concatenate([[0], np.cumsum(rows)])
     dev = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
-    return (torch.from_numpy(hw.astype(np.int32)).to(dev), torch.from_numpy(np.asarray(offsets).astype(np.int64)).to(dev),
-            torch.from_numpy(first.astype(np.int64)).to(dev), int(first[-1]))
+    shapes = torch.from_numpy(hw.astype(np.int32)).to(dev)
+    shapes.channels = channels
+    return shapes, torch.from_numpy(np.asarray(offsets).astype(np.int64)).to(dev), torch.from_numpy(first.astype(np.int64)).to(dev), int(first[-1])
 
 
 def patch_rows(pixels, shapes, offsets, first_rows, rows, patch, mean, inv_std, merge=1, frames=1, dtype=torch.bfloat16, out=None, positions=None,
@@ -51,7 +53,10 @@ def patch_rows(pixels, shapes, offsets, first_rows, rows, patch, mean, inv_std, 
     """Normalised patch rows of ragged uint8 pictures (decode_batch's pixels; shapes, offsets and first_rows from patch_layout), and their
     positions: (dtype [rows, channels * patch * patch], int32 [3, rows]: frame, row, column).  channels = len(mean), 1 or 3; see
     pcr_patch_rows for the order of the rows and for merge and frames."""
-    return _call(stream, _train.patch_rows, pixels, shapes, offsets, first_rows, rows, patch, tuple(mean), tuple(inv_std), merge, frames, _TYPES.get(dtype, -1), out, positions)
+    mean = tuple(mean)
+    if getattr(shapes, "channels", len(mean)) != len(mean):
+        raise ValueError("mean and inv_std: a value for each of the pictures' %d channels is wanted" % shapes.channels)
+    return _call(stream, _train.patch_rows, pixels, shapes, offsets, first_rows, rows, patch, mean, tuple(inv_std), merge, frames, _TYPES.get(dtype, -1), out, positions)
 
 
 # ---- positions in queries and keys ----
