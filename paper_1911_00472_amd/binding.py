@@ -303,10 +303,12 @@ class Record:
         """(shapes, offsets, first_rows, rows) of this record's pictures for patch_rows: three CUDA tensors and the number of rows.  The pictures' channels
         must all agree (PcrError E_UNSUPPORTED otherwise)."""
         from .train import patch_layout
+        offsets = self.output_layout()                       # (first: it counts the pictures anew)
         sizes = [self.image_info(i)[:3] for i in range(self.n)]
-        if len({c for _, _, c in sizes}) > 1:
+        channels = {c for _, _, c in sizes}
+        if len(channels) > 1:
             raise PcrError(E_UNSUPPORTED, "patch_layout")
-        return patch_layout([(h, w) for w, h, _ in sizes], sizes[0][2], patch, merge, offsets=self.output_layout(), device=self.device)
+        return patch_layout([(h, w) for w, h, _ in sizes], channels.pop() if channels else None, patch, merge, offsets=offsets, device=self.device)
 
     def msssim_batch(self, a, b, out=None, stream=None):
         """Multi-scale structural similarity of every image's pictures in two decoded batches (uint8 CUDA tensors

@@ -35,7 +35,8 @@ def _call(stream, f, *args):
 def patch_layout(shapes, channels, patch, merge=1, offsets=None, device=0):
     """What patch_rows needs to know of pictures of the given (height, width), one behind the other as decode_batch writes them (offsets: where
     each begins, and the end): (shapes int32 [n, 2], offsets int64 [n + 1], first_rows int64 [n + 1]) as CUDA tensors, and the number of rows.
-    shapes keeps the pictures' channels (an attribute of that name), which patch_rows holds against the number of means."""
+    shapes keeps the pictures' channels (an attribute of that name), which patch_rows holds against the number of means; with offsets they may be None,
+    for pictures of which they are not known."""
     hw = np.asarray(shapes, np.int64).reshape(-1, 2)
     cell = patch * merge
     rows = np.where((hw > 0).all(1), (-(-hw // cell) * merge).prod(1), 0)
@@ -44,7 +45,8 @@ def patch_layout(shapes, channels, patch, merge=1, offsets=None, device=0):
     first = np.concatenate([[0], np.cumsum(rows)])
     dev = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
     shapes = torch.from_numpy(hw.astype(np.int32)).to(dev)
-    shapes.channels = channels
+    if channels is not None:
+        shapes.channels = channels
     return shapes, torch.from_numpy(np.asarray(offsets).astype(np.int64)).to(dev), torch.from_numpy(first.astype(np.int64)).to(dev), int(first[-1])
 
 
