@@ -4,7 +4,7 @@ of several axes turned into queries and keys (alone or behind a norm of every he
 The work is done by the library's HIP kernels, enqueued on the current stream (or `stream`, a hipStream_t as an integer); arguments are checked and handed on
 by the native module _train (csrc/pcr_bind.cpp).  A tensor on another stream than the one it was made on needs the caller's
 record_stream, as with any operator.  Wrong types, shapes or devices raise ValueError before anything is enqueued, what the library
-refuses raises PcrError.  rotate_axes, norm_rotate and distill_loss take part in automatic differentiation."""
+refuses raises PcrError.  rotate_axes, norm_rotate and distill_loss take part in automatic differentiation; a gradient is made on the stream of its forward pass."""
 import os
 
 import numpy as np
@@ -76,6 +76,10 @@ def axis_frequencies(sections, theta=10000.0, each=False, device=0):
     return torch.from_numpy((theta ** -power).astype(np.float32)).to(dev), torch.from_numpy(axis.astype(np.int32)).to(dev)
 
 
+def _wants_gradient(*tensors):
+    return torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in tensors)
+
+
 class _RotateAxes(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, positions, frequency, axis, adjacent, inverse):
@@ -103,8 +107,8 @@ def rotate_axes(q, k, positions, frequency, axis, adjacent=False, inverse=False,
     tokens] or [axes, batch, tokens].  A pair is (j, j + pairs), or (2 j, 2 j + 1) if `adjacent`; what is behind the pairs is not turned.  inverse:
     by minus the angle, which is the gradient.  q_out, k_out: where to (the inputs themselves, too); given, they keep the call out of automatic
     differentiation.  Returns (q, k) turned."""
-    if q_out is None and k_out is None and stream is None and torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
-        return _RotateAxes.apply(q, k, positions, frequency, axis, adjacent, inverse)
+    if q_out is None and k_out is None and _wants_gradient(q, k):
+        return _call(stream, _RotateAxes.apply, q, k, positions, frequency, axis, adjacent, inverse)
     return _call(stream, _train.rotate_axes, q, k, positions, frequency, axis, adjacent, inverse, q_out, k_out)
 
 
@@ -132,8 +136,8 @@ class _NormRotate(torch.autograd.Function):
 def norm_rotate(q, k, q_weight, k_weight, positions, frequency, axis, eps=1e-6, adjacent=False, q_out=None, k_out=None, stream=None):
     """rotate_axes of x * weight / sqrt(mean x^2 + eps), the mean over each head of queries and keys, in one pass and with one rounding.  Weights: [dim]
     of float32 or of the heads' type, or None.  Returns (q, k)."""
-    if q_out is None and k_out is None and stream is None and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
-        return _NormRotate.apply(q, k, q_weight, k_weight, positions, frequency, axis, eps, adjacent)
+    if q_out is None and k_out is None and _wants_gradient(q, k, q_weight, k_weight):
+        return _call(stream, _NormRotate.apply, q, k, q_weight, k_weight, positions, frequency, axis, eps, adjacent)
     return _call(stream, _train.norm_rotate, q, k, q_weight, k_weight, positions, frequency, axis, eps, adjacent, q_out, k_out)
 
 
