@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -86,6 +87,18 @@ int type_of(const at::Tensor& t) {
 }
 void on(const at::Tensor& t, const at::Tensor& other, const char* name) { need(t.is_cuda() && t.device() == other.device(), name, "a tensor on the GPU of the others is wanted"); }
 
+// A tensor of the caller's that a call writes: as with PyTorch's operators in place, not a leaf that requires a gradient, which would lose its place in the graph ...
+void check_written(const at::Tensor& t, const char* name) {
+    if (!t.requires_grad() || !c10::GradMode::is_enabled()) return;
+    need(!(t.is_view() ? t._base() : t).is_leaf(), name, "a leaf that requires a gradient is not written over (under torch.no_grad() it is)");
+}
+// ... and behind the call of a version of its own, so that what was kept of the old one for a gradient is not taken for it.
+void written(PyObject* o) {
+    if (o == Py_None) return;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // PyTorch's current stream of the tensor's device.
 void* stream_of(const at::Tensor& t) {
     PyObject* index = PyLong_FromLong(t.device().index());
@@ -160,6 +173,7 @@ PyObject* patch_rows(PyObject*, PyObject* const* a, Py_ssize_t given) {
         need(given_out || (dtype >= 0 && dtype <= 2), "dtype", "float32, float16 or bfloat16 is wanted");
         if (given_out) {
             on(*given_out, pixels, "out");
+            check_written(*given_out, "out");
             need(type_of(*given_out) >= 0 && given_out->is_contiguous() && given_out->numel() == rows * per, "out", "contiguous [rows, channels * patch * patch] is wanted");
         }
         if (given_positions) {
@@ -172,6 +186,8 @@ PyObject* patch_rows(PyObject*, PyObject* const* a, Py_ssize_t given) {
         check(pcr_patch_rows(device_number(pixels), (const uint8_t*)pixels.data_ptr(), (size_t)pixels.numel(), (const int32_t*)shapes.data_ptr(), (const int64_t*)offsets.data_ptr(),
                              (const int64_t*)first.data_ptr(), n, rows, patch, merge, frames, C, mean, inv_std, type_of(out), out.data_ptr(), (int32_t*)positions.data_ptr(),
                              stream_of(pixels)), "pcr_patch_rows");
+        written(a[11]);
+        written(a[12]);
         return tuple(some(out), some(positions));
     });
 }
@@ -185,6 +201,7 @@ void check_side(const at::Tensor& t, const at::Tensor& x, const char* name) {
 }
 void check_into(const at::Tensor& t, const at::Tensor& x, const char* name) {
     check_side(t, x, name);
+    check_written(t, name);
     for (int64_t i = 0; i < t.dim(); i++) need(t.stride(i) != 0 || t.size(i) < 2, name, "every element needs a place of its own");
 }
 void check_weight(const at::Tensor* w, const at::Tensor& x, const char* name) {
@@ -275,6 +292,8 @@ PyObject* rotate_axes(PyObject*, PyObject* const* a, Py_ssize_t given) {        
         Turn T(a[0], a[1], nullptr, nullptr, a[2], a[3], a[4], a[5]);
         const at::Tensor q = T.into(0, a[7], "q_out"), k = T.into(1, a[8], "k_out");
         check(pcr_rotate_axes(device_number(q), &T.side[0], &T.side[1], &T.rotation, truth(a[6]), T.dtype, stream_of(q)), "pcr_rotate_axes");
+        written(a[7]);
+        written(a[8]);
         return tuple(some(q), T.x[1] ? some(k) : none());
     });
 }
@@ -286,6 +305,8 @@ PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t given) {        
         need(eps >= 0, "eps", "not below 0");
         const at::Tensor q = T.into(0, a[9], "q_out"), k = T.into(1, a[10], "k_out");
         check(pcr_norm_rotate(device_number(q), &T.side[0], &T.side[1], &T.rotation, (float)eps, T.dtype, T.weight_dtype, stream_of(q)), "pcr_norm_rotate");
+        written(a[9]);
+        written(a[10]);
         return tuple(some(q), T.x[1] ? some(k) : none());
     });
 }
@@ -319,6 +340,8 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t given) 
         }
         check(pcr_norm_rotate_backward(device_number(q), &T.side[0], &T.side[1], &T.rotation, (float)eps, T.dtype, T.weight_dtype, bytes ? work.data_ptr() : nullptr, bytes,
                                        stream_of(q)), "pcr_norm_rotate_backward");
+        written(a[11]);
+        written(a[12]);
         return tuple(some(q), T.x[1] ? some(k) : none(), T.w[0] ? some(sums[0]) : none(), T.w[1] ? some(sums[1]) : none());
     });
 }
@@ -363,6 +386,7 @@ struct Distill {
         on(*t, z, "out");
         need(t->scalar_type() == z.scalar_type() && t->sizes() == z.sizes() && (t->size(1) == 1 || t->stride(1) == 1) && (t->size(0) < 2 || t->stride(0) != 0), "out",
              "type and shape of logits, a row contiguous, is wanted");
+        check_written(*t, "out");
         return *t;
     }
     at::Tensor work(size_t& bytes) const {
@@ -392,6 +416,7 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {   
         need(sums.scalar_type() == at::kFloat && sums.dim() == 2 && sums.size(0) == D.d.rows && sums.size(1) == 2 && sums.is_contiguous(), "sums", "contiguous float32 [rows, 2] is wanted");
         const at::Tensor out = D.into(a[9]);
         check(pcr_distill_backward(device_number(D.z), &D.d, (const float*)sums.data_ptr(), g, out.data_ptr(), out.stride(0), stream_of(D.z)), "pcr_distill_backward");
+        written(a[9]);
         return some(out);
     });
 }
@@ -405,6 +430,7 @@ PyObject* distill_step(PyObject*, PyObject* const* a, Py_ssize_t given) {       
         const at::Tensor work = D.work(bytes);
         check(pcr_distill_step(device_number(D.z), &D.d, weight, (float*)loss.data_ptr(), out.data_ptr(), out.stride(0), bytes ? work.data_ptr() : nullptr, bytes, stream_of(D.z)),
               "pcr_distill_step");
+        written(a[8]);
         return tuple(some(loss), some(out));
     });
 }

@@ -106,7 +106,7 @@ def rotate_axes(q, k, positions, frequency, axis, adjacent=False, inverse=False,
     q, k: [tokens, heads, dim] or [batch, tokens, heads, dim] (k may be None) with any strides of batch, tokens and heads; positions: integers [axes,
     tokens] or [axes, batch, tokens].  A pair is (j, j + pairs), or (2 j, 2 j + 1) if `adjacent`; what is behind the pairs is not turned.  inverse:
     by minus the angle, which is the gradient.  q_out, k_out: where to (the inputs themselves, too); given, they keep the call out of automatic
-    differentiation.  Returns (q, k) turned."""
+    differentiation (a leaf that requires a gradient is refused, as by an operator in place).  Returns (q, k) turned."""
     if q_out is None and k_out is None and _wants_gradient(q, k):
         return _call(stream, _RotateAxes.apply, q, k, positions, frequency, axis, adjacent, inverse)
     return _call(stream, _train.rotate_axes, q, k, positions, frequency, axis, adjacent, inverse, q_out, k_out)
