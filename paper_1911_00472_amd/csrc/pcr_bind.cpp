@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <cmath>
 #include <cstdarg>
@@ -49,7 +50,9 @@ void check(int rc, const char* what) {
 const at::Tensor* maybe_tensor(PyObject* o, const char* name) {
     if (o == Py_None) return nullptr;
     need(THPVariable_Check(o), name, "a tensor is wanted");
-    return &THPVariable_Unpack(o);
+    const at::Tensor& t = THPVariable_Unpack(o);
+    need(!t._fw_grad(0).defined(), name, "has a derivative of forward mode, which would be lost");
+    return &t;
 }
 const at::Tensor& tensor(PyObject* o, const char* name) {
     const at::Tensor* t = maybe_tensor(o, name);
@@ -133,6 +136,10 @@ template <typename... P> PyObject* tuple(P... parts) {
 template <typename F> PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F f) {
     if (given != wanted) {
         PyErr_Format(PyExc_TypeError, "%zd arguments are wanted, %zd given", wanted, given);
+        return nullptr;
+    }
+    if (torch::jit::tracer::isTracing()) {                     // (a trace would hold the results' allocation and not the kernel that fills them)
+        PyErr_SetString(PyExc_RuntimeError, "the operators behind the decode cannot be traced");
         return nullptr;
     }
     try {

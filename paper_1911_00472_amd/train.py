@@ -4,7 +4,8 @@ of several axes turned into queries and keys (alone or behind a norm of every he
 The work is done by the library's HIP kernels, enqueued on the current stream (or `stream`, a hipStream_t as an integer); arguments are checked and handed on
 by the native module _train (csrc/pcr_bind.cpp).  A tensor on another stream than the one it was made on needs the caller's
 record_stream, as with any operator.  Wrong types, shapes or devices raise ValueError before anything is enqueued, what the library
-refuses raises PcrError.  rotate_axes, norm_rotate and distill_loss take part in automatic differentiation; a gradient is made on the stream of its forward pass."""
+refuses raises PcrError.  rotate_axes, norm_rotate and distill_loss take part in automatic differentiation; a gradient is made on the stream of its forward pass.
+There are no derivatives of forward mode (ValueError), and no traces (RuntimeError)."""
 import os
 
 import numpy as np
