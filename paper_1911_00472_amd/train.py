@@ -77,10 +77,6 @@ def axis_frequencies(sections, theta=10000.0, each=False, device=0):
     return torch.from_numpy((theta ** -power).astype(np.float32)).to(dev), torch.from_numpy(axis.astype(np.int32)).to(dev)
 
 
-def _wants_gradient(*tensors):
-    return torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in tensors)
-
-
 class _RotateAxes(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, positions, frequency, axis, adjacent, inverse):
@@ -108,7 +104,7 @@ def rotate_axes(q, k, positions, frequency, axis, adjacent=False, inverse=False,
     tokens] or [axes, batch, tokens].  A pair is (j, j + pairs), or (2 j, 2 j + 1) if `adjacent`; what is behind the pairs is not turned.  inverse:
     by minus the angle, which is the gradient.  q_out, k_out: where to (the inputs themselves, too); given, they keep the call out of automatic
     differentiation (a leaf that requires a gradient is refused, as by an operator in place).  Returns (q, k) turned."""
-    if q_out is None and k_out is None and _wants_gradient(q, k):
+    if q_out is None and k_out is None and torch.is_grad_enabled() and (getattr(q, "requires_grad", False) or getattr(k, "requires_grad", False)):
         return _call(stream, _RotateAxes.apply, q, k, positions, frequency, axis, adjacent, inverse)
     return _call(stream, _train.rotate_axes, q, k, positions, frequency, axis, adjacent, inverse, q_out, k_out)
 
@@ -137,7 +133,8 @@ class _NormRotate(torch.autograd.Function):
 def norm_rotate(q, k, q_weight, k_weight, positions, frequency, axis, eps=1e-6, adjacent=False, q_out=None, k_out=None, stream=None):
     """rotate_axes of x * weight / sqrt(mean x^2 + eps), the mean over each head of queries and keys, in one pass and with one rounding.  Weights: [dim]
     of float32 or of the heads' type, or None.  Returns (q, k)."""
-    if q_out is None and k_out is None and _wants_gradient(q, k, q_weight, k_weight):
+    if q_out is None and k_out is None and torch.is_grad_enabled() and (getattr(q, "requires_grad", False) or getattr(k, "requires_grad", False) or
+                                                                       getattr(q_weight, "requires_grad", False) or getattr(k_weight, "requires_grad", False)):
         return _call(stream, _NormRotate.apply, q, k, q_weight, k_weight, positions, frequency, axis, eps, adjacent)
     return _call(stream, _train.norm_rotate, q, k, q_weight, k_weight, positions, frequency, axis, eps, adjacent, q_out, k_out)
 
