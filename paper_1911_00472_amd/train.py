@@ -26,7 +26,9 @@ def _call(stream, f, *args):
     """f on the current stream; on `stream`, results and working memory come from that stream's pool, so that they are not handed out while it works on them."""
     if stream is None:
         return f(*args)
-    index = next(a.get_device() for a in args if isinstance(a, torch.Tensor))
+    index = next((a.get_device() for a in args if isinstance(a, torch.Tensor) and a.is_cuda), None)
+    if index is None:                                      # (it has no tensor to work on, and says so)
+        return f(*args)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=index) if stream else torch.cuda.default_stream(index)):
         return f(*args)
 
