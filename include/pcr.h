@@ -500,7 +500,8 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
  * turned by d_position[d_axis[j]][batch][token] * d_frequency[j] radians, (x, y) -> (x cos - y sin, x sin + y cos).  A pair is
  * (j, j + pairs), or (2 j, 2 j + 1) where `adjacent` is set; elements from 2 * pairs on are not turned.
  * The angle is the product of the position and the frequency as 32-bit floats, rounded to one (2^-24 of itself off, as where a program multiplies
- * a table of frequencies by positions); its sine and cosine are taken to 2^-22 however large it is.  Positions may be negative.
+ * a table of frequencies by positions); its sine and cosine are taken to 2^-22 however large it is,
+ * and are NaN where it is infinite or NaN.  Positions may be negative.
  *   d_position  int32, or int64 where `wide` is set, with its strides;  d_frequency: float [pairs];  d_axis: int32 [pairs], 0 .. axes - 1
  *               (another value counts as the nearest of these)
  *   batch, tokens, dim (1 .. 512), pairs (0 .. dim / 2): the same for queries and keys

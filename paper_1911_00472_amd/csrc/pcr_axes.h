@@ -44,8 +44,7 @@ struct AxesArgs {
 enum { kRotate = 0, kNorm = 1, kNormBack = 2 };
 constexpr int kAxesTable = 4096;                               // pairs of sine and cosine that a workgroup keeps at most (32 KB)
 
-// f radians as a fraction of a turn, in 64 bits behind the point: f's 24 bits times 1 / (2 pi) to 128 bits, moved by f's exponent and cut.
-// (What is infinite or NaN gives some angle.)
+// f radians (a number) as a fraction of a turn, in 64 bits behind the point: f's 24 bits times 1 / (2 pi) to 128 bits, moved by f's exponent and cut.
 __device__ __forceinline__ uint64_t turns_of(float f) {
     const uint32_t bits = __float_as_uint(f), e = bits >> 23 & 255;
     const uint64_t m = (bits & 0x7fffff) | (e ? 0x800000 : 0);
@@ -68,6 +67,7 @@ __device__ __forceinline__ float2 turn_of(float angle, int inverse) {
         quarters = __builtin_rintf(angle * 0.63661974668502807617f);
         rest = __builtin_fmaf(angle, 6.4206382432985265e-9f, __builtin_fmaf(angle, 0.15915493667125701904f, -0.25f * quarters));
     } else {
+        if (!(__builtin_fabsf(angle) < INFINITY)) return make_float2(NAN, NAN);
         const uint64_t turns = turns_of(angle);
         quarters = (float)(uint32_t)((turns + (1ull << 61)) >> 62);
         rest = (float)((int64_t)(turns - ((uint64_t)(uint32_t)quarters << 62)) >> 32) * 2.3283064365386962891e-10f;      // 2^-32
