@@ -44,7 +44,8 @@ struct AxesArgs {
 enum { kRotate = 0, kNorm = 1, kNormBack = 2 };
 constexpr int kAxesTable = 4096;                               // pairs of sine and cosine that a workgroup keeps at most (32 KB)
 
-// f radians (a number) as a fraction of a turn, in 64 bits behind the point: f's 24 bits times 1 / (2 pi) to 128 bits, moved by f's exponent and cut.
+// f radians (a number) as a fraction of a turn, in 64 bits behind the point: f's 24 bits times 1 / (2 pi) to 128 bits (from 2^87 on
+// to the 64 of them that are behind the point once moved, of 192), moved by f's exponent and cut.
 __device__ __forceinline__ uint64_t turns_of(float f) {
     const uint32_t bits = __float_as_uint(f), e = bits >> 23 & 255;
     const uint64_t m = (bits & 0x7fffff) | (e ? 0x800000 : 0);
@@ -54,7 +55,7 @@ __device__ __forceinline__ uint64_t turns_of(float f) {
     uint64_t v;
     if (down >= 64) v = down < 192 ? (uint64_t)(high >> (down - 64)) : 0;
     else if (down > 0) v = (uint64_t)(high << (64 - down)) | (uint64_t)low >> down;
-    else v = (uint64_t)low << -down;
+    else v = m * (0x7f09d5f47d4d3770ull << -down | 0x36d8a5664f10e410ull >> 1 >> (63 + down));
     return bits >> 31 ? 0 - v : v;
 }
 
