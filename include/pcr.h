@@ -509,7 +509,8 @@ int pcr_patch_rows(int device_id, const uint8_t* d_pixels, size_t pixel_bytes, c
  *   (pointers may be NULL).  out may be in itself with the same strides; otherwise they must not overlap.
  *
  * pcr_rotate_axes: the rotation alone.  inverse != 0: by minus the angle, which is its gradient (grad is not used).
- * pcr_norm_rotate: y = rotation of x r w, r = 1 / sqrt(mean x^2 + eps) over the head, eps not below 0; weight: dim elements of weight_dtype, NULL: ones.
+ * pcr_norm_rotate: y = rotation of x r w, r = 1 / sqrt(mean x^2 + eps) over the head, eps not below 0, the squares as 32-bit floats (of elements beyond
+ *   2^59 or so their sum is infinite and y 0; below 2^-62 or so they are 0 beside eps); weight: dim elements of weight_dtype, NULL: ones.
  * pcr_norm_rotate_backward: grad: the gradient of y; in: x; out: the gradient of x (it may be grad or in itself); weight_grad: float [dim],
  *   the weight's gradient summed over batch, tokens and heads in a fixed order (NULL: not asked for; needs d_work otherwise).
  *   d_work: pcr_norm_rotate_workspace bytes, its content is of no account before and after.

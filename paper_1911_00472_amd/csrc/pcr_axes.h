@@ -102,6 +102,12 @@ __device__ __forceinline__ float group_sum(float v, int head, int member, int sl
     return __shfl(v, head);
 }
 
+// v^-1/2, also of numbers that the instruction takes for 0.
+__device__ __forceinline__ float inverse_root(float v) {
+    const int up = v < 1.1754943508222875e-38f ? 32 : 0;       // 2^-126
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_rsqf(__builtin_amdgcn_ldexpf(v, up + up)), up);
+}
+
 template <typename T, int N> __device__ __forceinline__ void load_weight(const AxesArgs& A, const void* w, int at, float (&x)[N]) {
     if (!w) {
 #pragma unroll
@@ -289,7 +295,7 @@ __global__ __launch_bounds__(256) void k_axes(AxesArgs A) {
 #pragma unroll
                             for (int i = 0; i < 2 * N; i++) sum = __builtin_fmaf(x[j][i], x[j][i], sum);
                         sum = group_sum(sum, head, member, group);
-                        const float rms = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, A.inv_dim, A.eps));
+                        const float rms = inverse_root(__builtin_fmaf(sum, A.inv_dim, A.eps));
 #pragma unroll
                         for (int j = 0; j < K; j++)
 #pragma unroll
