@@ -8,10 +8,22 @@ _TRAIN = ("patch_layout", "patch_rows", "axis_frequencies", "rotate_axes", "norm
           "distill_step", "distill_loss")
 
 
-def __getattr__(name):
-    """The operators of train.py, with PyTorch, when the first of them is asked for."""
-    if name in _TRAIN:
+def _deferred(name):
+    def call(*args, **kwargs):
         from . import train
+        return getattr(train, name)(*args, **kwargs)
+    call.__name__ = call.__qualname__ = name
+    return call
+
+
+def __getattr__(name):
+    """The operators of train.py, with PyTorch, when the first of them is asked for.  Where they cannot be had (nothing is built, no PyTorch) the names
+    are there all the same, for `import *`, and a call says what is missing."""
+    if name in _TRAIN:
+        try:
+            from . import train
+        except (ImportError, OSError, RuntimeError):
+            return _deferred(name)
         for n in _TRAIN:
             globals()[n] = getattr(train, n)
         return globals()[name]
