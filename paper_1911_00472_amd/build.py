@@ -23,18 +23,39 @@ def _module_command():
             "-c", "-o", SRC_BIND[:-len(".cpp")] + ".o", SRC_BIND], os.path.join(home, "lib")
 
 
-def build():
-    """Compile csrc/ into libpcr.so and _train.so (always recompiles)."""
+def build_library():
+    """Compile csrc/ into libpcr.so (always recompiles): the C ABI, which needs neither PyTorch nor Python's headers."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     compile_only = [hipcc, "-c"] + [f for f in HIPCC_FLAGS if f != "-shared"]
     sources = (SRC, SRC_TRAIN, SRC_DISTILL)
     objects = [s[:-len(".hip")] + ".o" for s in sources]
-    module, torch_lib = _module_command()
-    running = [subprocess.Popen(c) for c in [compile_only + ["-o", o, s] for s, o in zip(sources, objects)] + [module]]
+    running = [subprocess.Popen(compile_only + ["-o", o, s]) for s, o in zip(sources, objects)]
     failed = [p.args for p in running if p.wait() != 0]
     if failed:
         raise subprocess.CalledProcessError(1, failed[0])
     subprocess.check_call([hipcc] + HIPCC_FLAGS + ["-o", LIB] + objects)
+    return LIB
+
+
+def build():
+    """Compile csrc/ into libpcr.so and _train.so (always recompiles).  What keeps the module from being made is raised when the library is; a module of
+    another library is not left beside it."""
+    compiling, late = None, None
+    try:
+        module, torch_lib = _module_command()
+        compiling = subprocess.Popen(module)
+    except (ImportError, OSError) as e:
+        late = e
+    try:
+        build_library()
+    finally:
+        failed = compiling is not None and compiling.wait() != 0
+    if (late is not None or failed) and os.path.exists(MODULE):
+        os.remove(MODULE)
+    if late is not None:
+        raise late
+    if failed:
+        raise subprocess.CalledProcessError(1, module)
     subprocess.check_call([module[0], "-shared", "-o", MODULE, module[module.index("-o") + 1], "-L" + HERE, "-lpcr", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib, "-ltorch_python", "-ltorch_cpu", "-lc10"])
     return LIB
 
