@@ -230,17 +230,15 @@ template <typename T, int TEAM> __device__ __forceinline__ void write_zeros(T* o
     for (int64_t r = tid; r < runs; r += TEAM) store_run<T, N>(out + lead + r * N, none);
 }
 
-// A team of TEAM threads takes a row, or one of the shares of a row (gradient alone).  MODE: the loss and the sums, the gradient from saved sums, or both.
+// A workgroup of TEAM threads takes a row, or one of the shares of a row (gradient alone).  MODE: the loss and the sums, the gradient from saved sums, or both.
 template <typename T, int TEAM, bool TWO, int MODE>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs A) {
-    extern __shared__ float lds[];                             // a team's: joins [16], entries
-    const int tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const int64_t unit = (A.first + blockIdx.x) * (TEAM < 256 ? 256 / TEAM : 1) + team;
-    if (unit >= A.rows * A.chunks) return;                     // (a whole wavefront, or nobody of a workgroup that shares a row)
-    const int64_t n = unit / A.chunks;
+__global__ __launch_bounds__(TEAM) void k_distill(DistillArgs A) {
+    extern __shared__ float lds[];                             // joins [16], entries
+    const int tid = threadIdx.x;
+    const int64_t unit = A.first + blockIdx.x, n = unit / A.chunks;
     const int share = (int)(unit - n * A.chunks);
     int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
-    float* join = lds + team * (16 + entry_floats(A.K, A.chunk));
+    float* join = lds;
     Entries E(join + 16, A.K, A.chunk);
     const T* z = (const T*)A.logits + n * A.row_stride;
     T* out = MODE == kLoss ? nullptr : (T*)A.out + n * A.out_stride + v0;
@@ -251,7 +249,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill(DistillArgs
         if (MODE == kStep && tid == 0) A.loss[n] = 0.f;
         return;
     }
-    // A row whose sums are made anew goes to one team whole: it is read before any of it is written, which may be in its place.
+    // A row whose sums are made anew goes to one workgroup whole: it is read before any of it is written, which may be in its place.
     const float saved = MODE == kGrad ? A.sums_in[2 * n] : 0.f, saved1 = MODE == kGrad ? A.sums_in[2 * n + 1] : 0.f;
     const bool anew = MODE != kGrad || saved_too_far(saved) || (TWO && saved_too_far(saved1));
     if (MODE == kGrad && anew) {

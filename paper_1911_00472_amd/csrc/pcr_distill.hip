@@ -53,12 +53,11 @@ void cut(DistillArgs& A, int64_t parts) {
 }
 
 template <typename T, int TEAM, int MODE> void launch_team(DistillArgs A, hipStream_t s) {
-    const int teams = TEAM < 256 ? 256 / TEAM : 1, threads = TEAM < 256 ? 256 : TEAM;
-    const size_t lds = (size_t)teams * (16 + entry_floats(A.K, A.chunk)) * sizeof(float);
-    in_ranges((A.rows * A.chunks + teams - 1) / teams, threads, [&](int64_t first, unsigned groups) {
+    const size_t lds = (size_t)(16 + entry_floats(A.K, A.chunk)) * sizeof(float);
+    in_ranges(A.rows * A.chunks, TEAM, [&](int64_t first, unsigned groups) {
         A.first = first;
-        if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(threads), lds, s, A);
-        else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(threads), lds, s, A);
+        if (A.two && A.T != 1.f) hipLaunchKernelGGL((k_distill<T, TEAM, true, MODE>), dim3(groups), dim3(TEAM), lds, s, A);
+        else hipLaunchKernelGGL((k_distill<T, TEAM, false, MODE>), dim3(groups), dim3(TEAM), lds, s, A);
     });
 }
 // The gradient from saved sums of rows for more than a wavefront, and (MODE kLoss, kStep) rows too long for a team's registers, read twice.
