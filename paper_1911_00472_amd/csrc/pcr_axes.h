@@ -64,14 +64,13 @@ __device__ __forceinline__ uint64_t turns_of(float f) {
 // sin(pi r) / r and (cos(pi r) - 1) / r^2 are polynomials of third degree in r^2, fitted to least maximal error over that range (10^-9).
 __device__ __forceinline__ float2 turn_of(float angle, int inverse) {
     float rest, quarters;
-    if (__builtin_fabsf(angle) < 1048576.f) {
+    if (__builtin_expect(__builtin_fabsf(angle) < 1048576.f, 1)) {
         quarters = __builtin_rintf(angle * 0.63661974668502807617f);
         rest = __builtin_fmaf(angle, 6.4206382432985265e-9f, __builtin_fmaf(angle, 0.15915493667125701904f, -0.25f * quarters));
     } else {
-        if (!(__builtin_fabsf(angle) < INFINITY)) return make_float2(NAN, NAN);
         const uint64_t turns = turns_of(angle);
         quarters = (float)(uint32_t)((turns + (1ull << 61)) >> 62);
-        rest = (float)((int64_t)(turns - ((uint64_t)(uint32_t)quarters << 62)) >> 32) * 2.3283064365386962891e-10f;      // 2^-32
+        rest = __builtin_fmaf((float)((int64_t)(turns - ((uint64_t)(uint32_t)quarters << 62)) >> 32), 2.3283064365386962891e-10f, angle - angle);      // 2^-32; NaN of what is no number
     }
     const float r = rest + rest, u = r * r;
     const float sine = r * __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(-0.5876994729042053f, u, 2.5496182441711426f), u, -5.167703151702881f), u, 3.141592502593994f);
