@@ -14,6 +14,8 @@
 // saved sums of 4096 rows of 131072 half-precision logits: 426 (430).  Short rows are bound by the trips to memory of a wavefront that follow each other:
 // 16384 rows of 300 classes with 10 entries take 15 (4).
 #pragma once
+#include <type_traits>
+
 #include "pcr_vec.h"
 
 namespace pcr {
@@ -87,12 +89,20 @@ struct Entries {
         const uint32_t bit = v % (uint32_t)kEntryBits, mask = 1u << bit % 32;
         if (atomicOr(&seen[bit / 32], mask) & mask) atomicOr(&several[bit / 32], mask);
     }
-    // Behind it: what all entries at the class of entry e add.
+    // Behind it: what all entries at the class of entry e add, if several are ...
     __device__ __forceinline__ float sum(int e, uint32_t v, int K) const {
         const uint32_t bit = v % (uint32_t)kEntryBits;
-        if (!(several[bit / 32] >> bit % 32 & 1)) return delta[e];
+        return several[bit / 32] >> bit % 32 & 1 ? sum_of_all(e, K) : delta[e];
+    }
+    // ... and where no class is marked.
+    __device__ __forceinline__ float sum_of_all(int e, int K) const {
+        const int mine = at[e];
         float all = 0.f;
-        for (int k = 0; k < K; k++) all += at[k] == at[e] ? delta[k] : 0.f;
+        for (int k = 0; k < K; k++) {
+            const int v = at[k];
+            const float d = delta[k];
+            all += v == mine ? d : 0.f;
+        }
         return all;
     }
 };
@@ -189,13 +199,8 @@ template <bool TWO> struct ByMaximum {
         return TWO ? __builtin_fmaf(cb, __builtin_amdgcn_exp2f((x - m) * kLog2e), v) : v;
     }
 };
-// Saved sums that are too far from 0: from 128 on the two roundings in one come to more than 2^-17, and every element of the gradient is off by that part of
-// itself; where a float holds nothing of the sum's logarithm beside the maximum, x / T less it is a rounding error of any size.  The maximum and the sums of
-// such a row are made anew.
-__device__ __forceinline__ bool saved_too_far(float L) { return !(__builtin_fabsf(L) < 128.f); }
-
-template <typename T, int TEAM, typename D> __device__ __forceinline__ void write_dense(const T* z, T* out, int64_t count, const D& dense, int tid) {
-    constexpr int N = 16 / sizeof(T), U = 4;
+template <typename T, int TEAM, int U = 4, typename D> __device__ __forceinline__ void write_dense(const T* z, T* out, int64_t count, const D& dense, int tid) {
+    constexpr int N = 16 / sizeof(T);
     const int64_t lead = min(count, (int64_t)((-(uintptr_t)out & 15) / sizeof(T)));
     const int64_t runs = (count - lead) / N, tail = lead + runs * N;
     if (tid < lead) { float x[1]; load_run<T, 1>(z + tid, x); x[0] = dense(x[0]); store_run<T, 1>(out + tid, x); }
@@ -230,6 +235,28 @@ template <typename T, int TEAM> __device__ __forceinline__ void write_zeros(T* o
     for (int64_t r = tid; r < runs; r += TEAM) store_run<T, N>(out + lead + r * N, none);
 }
 
+// Saved sums that are too far from 0: from 128 on the two roundings in one come to more than 2^-17, and every element of the gradient is off by that part of
+// itself; where a float holds nothing of the sum's logarithm beside the maximum, x / T less it is a rounding error of any size.  The maximum and the sums of
+// such a row are made anew (write_anew).
+__device__ __forceinline__ bool saved_too_far(float L) { return !(__builtin_fabsf(L) < 128.f); }
+// Such a row's gradient, by one team: the row is read before any of it is written, which may be in its place.  The entries hold what they add.
+template <typename T, int TEAM, bool TWO>
+__device__ __forceinline__ void write_anew(const DistillArgs& A, const T* z, T* out, const Entries& E, float ca, float cb, int64_t label, float zl, float* join, int tid) {
+    const float c = A.inv_T * kLog2e;
+    const RowSums R = row_sums<T, TEAM, TWO, 1>(z, A.V, c, tid);           // (one run at a time: the kernel keeps its registers)
+    const float m = team_join<TEAM, true>(R.m, join);
+    const float s = team_join<TEAM, false>(scaled(R.s, R.m, m, c), join);
+    const float s1 = TWO ? team_join<TEAM, false>(scaled(R.s1, R.m, m, kLog2e), join) : s;
+    const ByMaximum<TWO> dense = {c, m, TWO ? ca / s : (ca + cb) / s, cb / s1};
+    write_dense<T, TEAM, 1>(z, out, A.V, dense, tid);
+    team_sync<TEAM>();
+    for (int e = tid; e < A.K; e += TEAM) {
+        const int64_t v = E.at[e];
+        if (v >= 0) out[v] = (T)(dense(E.logit[e]) + (E.sum_of_all(e, A.K) - (v == label ? cb : 0.f)));
+    }
+    if (tid == 0 && label >= 0 && label < A.V && !*E.labelled) out[label] = (T)(dense(zl) - cb);
+}
+
 // A workgroup of TEAM threads takes a row, or one of the shares of a row (gradient alone).  MODE: the loss and the sums, the gradient from saved sums, or both.
 template <typename T, int TEAM, bool TWO, int MODE>
 __global__ __launch_bounds__(TEAM) void k_distill(DistillArgs A) {
@@ -237,7 +264,7 @@ __global__ __launch_bounds__(TEAM) void k_distill(DistillArgs A) {
     const int tid = threadIdx.x;
     const int64_t unit = A.first + blockIdx.x, n = unit / A.chunks;
     const int share = (int)(unit - n * A.chunks);
-    int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
+    const int64_t v0 = share * A.chunk, count = min(A.chunk, A.V - v0);
     float* join = lds;
     Entries E(join + 16, A.K, A.chunk);
     const T* z = (const T*)A.logits + n * A.row_stride;
@@ -249,15 +276,6 @@ __global__ __launch_bounds__(TEAM) void k_distill(DistillArgs A) {
         if (MODE == kStep && tid == 0) A.loss[n] = 0.f;
         return;
     }
-    // A row whose sums are made anew goes to one workgroup whole: it is read before any of it is written, which may be in its place.
-    const float saved = MODE == kGrad ? A.sums_in[2 * n] : 0.f, saved1 = MODE == kGrad ? A.sums_in[2 * n + 1] : 0.f;
-    const bool anew = MODE != kGrad || saved_too_far(saved) || (TWO && saved_too_far(saved1));
-    if (MODE == kGrad && anew) {
-        if (share) return;
-        count = A.V;
-    }
-    // Where a class has its bit: the chunk's bits are taken again for every chunk of a whole row.
-    auto place = [&](int64_t v) { return MODE == kGrad && anew ? (uint32_t)v % (uint32_t)A.chunk : (uint32_t)(v - v0); };
     if (MODE != kLoss) E.clear<TEAM>(tid);
     // entries: softmax of the teacher's logits over those that count
     float most = load_entries<T, TEAM>(A, n, z, E, tid);
@@ -277,9 +295,11 @@ __global__ __launch_bounds__(TEAM) void k_distill(DistillArgs A) {
         return;
     }
     // What the dense part is taken against: the saved sums, or (exact also where the logarithm is lost beside it) the maximum and the sums' reciprocals.
-    float m = 0.f, s = 1.f, s1 = 1.f;
-    if (anew) {
-        RowSums R = row_sums<T, TEAM, TWO, MODE == kGrad ? 1 : 4>(z, A.V, c, tid);     // (a gradient keeps its registers, and with them two workgroups a compute unit)
+    float m = 0.f, s = 1.f, s1 = 1.f, saved = 0.f, saved1 = 0.f;
+    if (MODE == kGrad) {
+        saved = A.sums_in[2 * n]; saved1 = A.sums_in[2 * n + 1];
+    } else {
+        RowSums R = row_sums<T, TEAM, TWO>(z, A.V, c, tid);
         m = team_join<TEAM, true>(R.m, join);
         s = team_join<TEAM, false>(scaled(R.s, R.m, m, c), join);
         s1 = TWO ? team_join<TEAM, false>(scaled(R.s1, R.m, m, kLog2e), join) : s;
@@ -305,27 +325,30 @@ __global__ __launch_bounds__(TEAM) void k_distill(DistillArgs A) {
     for (int k = tid; k < A.K; k += TEAM) {
         const int64_t v = E.at[k];
         E.delta[k] = v >= 0 ? -g * A.a * A.T * (__builtin_amdgcn_exp2f((E.delta[k] - most) * c) / total) : 0.f;
-        if (v >= v0 && v < v0 + count) E.mark(place(v));
+        if (v >= v0 && v < v0 + count) E.mark((uint32_t)(v - v0));
         if (labelled && v == label) *E.labelled = 1;
     }
-    auto write = [&](auto dense) {
-        if (!TWO) dense.ca += dense.cb;
-        write_dense<T, TEAM>(z + v0, out, count, dense, tid);
-        team_sync<TEAM>();                                     // the dense part is written, the entries are marked
-        for (int e = tid; e < A.K; e += TEAM) {
-            const int64_t v = E.at[e];
-            if (v < v0 || v >= v0 + count) continue;
-            const float x[1] = {dense(E.logit[e]) + (E.sum(e, place(v), A.K) - (v == label ? g * A.b : 0.f))};
-            store_run<T, 1>(out + (v - v0), x);
-        }
-        if (tid == 0 && labelled && !*E.labelled && label >= v0 && label < v0 + count) {
-            const float x[1] = {dense(zl) - g * A.b};
-            store_run<T, 1>(out + (label - v0), x);
-        }
-    };
     const float ca = kept ? g * A.a * A.T : 0.f, cb = labelled ? g * A.b : 0.f;
-    if (anew) write(ByMaximum<TWO>{c, m, ca / s, cb / s1});
-    else if (MODE == kGrad) write(BySaved<TWO>{A.inv_T, saved, saved1, ca, cb});
+    if (MODE == kGrad && (saved_too_far(saved) || (TWO && saved_too_far(saved1)))) {
+        if (share == 0) write_anew<T, TEAM, TWO>(A, z, out, E, ca, cb, labelled ? label : -1, zl, join, tid);
+        return;
+    }
+    typename std::conditional<MODE == kGrad, BySaved<TWO>, ByMaximum<TWO>>::type dense;
+    if constexpr (MODE == kGrad) dense = {A.inv_T, saved, saved1, ca, cb};
+    else dense = {c, m, ca / s, cb / s1};
+    if (!TWO) dense.ca += dense.cb;
+    write_dense<T, TEAM>(z + v0, out, count, dense, tid);
+    team_sync<TEAM>();                                         // the dense part is written, the entries are marked
+    for (int e = tid; e < A.K; e += TEAM) {
+        const int64_t v = E.at[e];
+        if (v < v0 || v >= v0 + count) continue;
+        const float x[1] = {dense(E.logit[e]) + (E.sum(e, (uint32_t)(v - v0), A.K) - (v == label ? g * A.b : 0.f))};
+        store_run<T, 1>(out + (v - v0), x);
+    }
+    if (tid == 0 && labelled && !*E.labelled && label >= v0 && label < v0 + count) {
+        const float x[1] = {dense(zl) - g * A.b};
+        store_run<T, 1>(out + (label - v0), x);
+    }
 }
 
 // Several values at a time, with one barrier: `lds` holds C floats for every wavefront of the team and is used by no other join.
@@ -397,7 +420,6 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     if (TEAM > 64 && WRITES && g == 0.f) return left_out();
     const int64_t label = A.labels && A.b != 0.f ? A.labels[n] : -1;
     const float saved = SUMS ? 0.f : A.sums_in[2 * n], saved1 = SUMS ? 0.f : A.sums_in[2 * n + 1];
-    const bool anew = SUMS || saved_too_far(saved) || (BY != kOneSum && saved_too_far(saved1));
     const int V = (int)A.V, lead = min(V, (int)((-(uintptr_t)z & 15) / sizeof(T))), runs = (V - lead) / N, tail = lead + runs * N;
     if (WRITES) E.clear<TEAM>(tid);
     Vec raw[R];
@@ -415,7 +437,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     float most[2] = {x_edge, load_entries<T, TEAM>(A, n, z, E, tid)};            // of the logits, of the kept teacher's logits
     const bool labelled = label >= 0 && label < A.V;
     const float zl = labelled ? (float)z[label] : 0.f;
-    if (anew) {
+    if (SUMS) {
 #pragma unroll
         for (int u = 0; u < R; u++)
 #pragma unroll
@@ -432,7 +454,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         sum[0] += e;
         sum[1] += e1;
     };
-    if (anew) {
+    if (SUMS) {
 #pragma unroll
         for (int u = 0; u < R; u++) {
             if (u * TEAM < runs) {                             // (the same for the team)
@@ -449,7 +471,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
     if (BY == kOneSum) sum[1] = sum[0];
     const float total = sum[2], log_s = logf(sum[0]), log_s1 = logf(sum[1]), log_total = logf(total);
     const float unit = -g * A.a * A.T;
-    const float ca = kept ? (anew ? -unit / sum[0] : -unit) : 0.f, cb = labelled ? (anew ? g * A.b / sum[1] : g * A.b) : 0.f;
+    const float ca = kept ? (SUMS ? -unit / sum[0] : -unit) : 0.f, cb = labelled ? (SUMS ? g * A.b / sum[1] : g * A.b) : 0.f;
 
     // entries: their share of the loss, and what each adds to the dense part of its class
     auto finish = [&](float entries) {                         // the row's loss, from the sum of the entries' shares
@@ -480,40 +502,37 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_distill_rows(Distil
         }
         return;
     }
-    auto write = [&](auto dense) {
-        T* to = out + lead;
-#pragma unroll
-        for (int u = 0; u < R; u++)
-            if (tid + u * TEAM < runs) {
-                float x[N];
-                take_again<T>(raw[u], x);
-#pragma unroll
-                for (int i = 0; i < N; i++) x[i] = dense(x[i]);
-                store_run<T, N>(to + (tid + u * TEAM) * N, x);
-            }
-        if (edged) out[edge] = (T)dense(x_edge);
-        team_join_all<TEAM, 1, false>(loss, join + 5 * W);     // (the dense part and the entries are behind this barrier, too)
-        team_sync<TEAM>();
-        if (SUMS && tid == 0) finish(loss[0]);
-        for (int e = tid; e < A.K; e += TEAM) {
-            const int v = E.at[e];
-            if (v >= 0) out[v] = (T)(dense(E.logit[e]) + (E.sum(e, (uint32_t)v, A.K) - (v == label ? g * A.b : 0.f)));
-        }
-        if (tid == 0 && labelled && !*E.labelled) out[label] = (T)(dense(zl) - g * A.b);
+    constexpr bool TWO = BY != kOneSum;
+    if (!SUMS && (saved_too_far(saved) || (TWO && saved_too_far(saved1))))
+        return write_anew<T, TEAM, TWO>(A, z, out, E, ca, cb, labelled ? label : -1, zl, join, tid);
+    const BySaved<TWO> by_saved = {A.inv_T, saved, saved1, TWO ? ca : ca + cb, cb};
+    auto dense = [&](float x) {
+        if (!SUMS) return by_saved(x);
+        float e, e1 = 0.f;
+        exps<BY>(x, m, c, A.T, e, e1);
+        if (BY == kOneSum) return (ca + cb) * e;
+        if (BY == kSquare) return e * __builtin_fmaf(cb, e, ca);
+        return __builtin_fmaf(cb, e1, ca * e);
     };
-    if constexpr (SUMS) {
-        write([&](float x) {
-            float e, e1 = 0.f;
-            exps<BY>(x, m, c, A.T, e, e1);
-            if (BY == kOneSum) return (ca + cb) * e;
-            if (BY == kSquare) return e * __builtin_fmaf(cb, e, ca);
-            return __builtin_fmaf(cb, e1, ca * e);
-        });
-    } else {
-        constexpr bool TWO = BY != kOneSum;
-        if (anew) write(ByMaximum<TWO>{c, m, TWO ? ca : ca + cb, cb});
-        else write(BySaved<TWO>{A.inv_T, saved, saved1, TWO ? ca : ca + cb, cb});
+    T* to = out + lead;
+#pragma unroll
+    for (int u = 0; u < R; u++)
+        if (tid + u * TEAM < runs) {
+            float x[N];
+            take_again<T>(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = dense(x[i]);
+            store_run<T, N>(to + (tid + u * TEAM) * N, x);
+        }
+    if (edged) out[edge] = (T)dense(x_edge);
+    team_join_all<TEAM, 1, false>(loss, join + 5 * W);         // (the dense part and the entries are behind this barrier, too)
+    team_sync<TEAM>();
+    if (SUMS && tid == 0) finish(loss[0]);
+    for (int e = tid; e < A.K; e += TEAM) {
+        const int v = E.at[e];
+        if (v >= 0) out[v] = (T)(dense(E.logit[e]) + (E.sum(e, (uint32_t)v, A.K) - (v == label ? g * A.b : 0.f)));
     }
+    if (tid == 0 && labelled && !*E.labelled) out[label] = (T)(dense(zl) - g * A.b);
 }
 
 // Few rows: shares of a row are summed by workgroups of their own and joined by k_distill_join, a wavefront to a row.
