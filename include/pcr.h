@@ -474,8 +474,9 @@ int pcr_stage_ms_history(pcr_record* rec, double* sum_ms, uint32_t* launches, ui
  * All of these take the device's number, work on device memory, enqueue on hip_stream and allocate nothing.  `dtype` is the type of
  * what is read and written; sums, statistics and angles are held in 32 bits or more and every result is rounded once.
  * Strides and offsets count elements and may pass 32 bits.  An element lies at a multiple of its size; wider alignment is used where
- * it is there and not needed.  Results do not depend on anything but the inputs (no order of atomics).  Errors: PCR_E_ARG null
- * pointers, unknown types; PCR_E_RANGE sizes outside what is said; PCR_E_DEVICE; with any of them nothing is enqueued. */
+ * it is there and not needed.  Results depend on nothing but the inputs and the way they lie (no order of atomics; alignment and strides
+ * choose in which order a sum is made, and with it its last bits).  Errors: PCR_E_ARG null pointers, unknown types; PCR_E_RANGE sizes outside what
+ * is said, with both of which nothing is enqueued; PCR_E_DEVICE. */
 enum { PCR_FLOAT = 0, PCR_HALF = 1, PCR_BFLOAT = 2 };          /* IEEE 32 bits, IEEE 16 bits, the upper 16 bits of IEEE 32 */
 
 /* Normalised patch rows of n pictures at their own sizes, one picture's after another's, with their positions.

@@ -14,10 +14,10 @@
 // in LDS, for all heads of both sides; then a row (a head of a token) goes to a group of lanes, a lane holding one slot: a run of pairs, that is
 // two runs of elements of up to 16 bytes, so that pairs meet in a lane whichever way they lie.  The sums of a norm go round the group.  The next row is loaded
 // while one is worked on; a lane steps from row to row by adding (with a division a row, and 64-bit strides, there were 21 instructions an element, and 10 now).
-// us (floor at a large copy's 5.0 TB/s): inverse rotation of 65536 tokens of 40 heads of 128, bfloat 241 (269); rotation of 49999 tokens of 32 heads of 72 in
-// neighbouring pairs, half 92 (92); norm and rotation of 8204 tokens of 16 heads of 96 in 32 bits 19 (20); gradient of norm and rotation of 32768 tokens of
-// 40 heads of 128, bfloat 209 + 5 for the sums (201).  One head of queries and keys alone is not at its floor: 307 (258) for 2 million tokens of 80, its
-// gradient behind a norm 735 (394); there is an angle to make for every two rows.
+// us (what the bytes take at the 5.0 TB/s of a large copy, which kernels that read more than they write can pass): inverse rotation of 65536 tokens of 40 heads
+// of 128, bfloat 241 (269); rotation of 49999 tokens of 32 heads of 72 in neighbouring pairs, half 92 (92); norm and rotation of 8204 tokens of 16 heads of 96 in 32
+// bits 19 (20); gradient of norm and rotation of 32768 tokens of 40 heads of 128, bfloat 209 + 5 for the sums (201).  One head of queries and keys alone is slower
+// than a copy: 321 (262) for 2 million tokens of 80 and three axes, its gradient behind a norm 739 (393); there is an angle to make for every two rows.
 #pragma once
 #include "pcr_vec.h"
 
@@ -59,9 +59,11 @@ __device__ __forceinline__ uint64_t turns_of(float f) {
     return bits >> 31 ? 0 - v : v;
 }
 
-// Cosine and sine of an angle, the sine's sign turned over for an inverse.  The angle becomes quarter turns and r, the rest as half-turns (-1/4 .. 1/4): the
-// constant 1 / (2 pi) in two floats (2^-48 of it is missing, 2^-30 turns at 2^20 radians), the products in fused operations, the rest off by 2^-27 turns;
-// sin(pi r) / r and (cos(pi r) - 1) / r^2 are polynomials of third degree in r^2, fitted to least maximal error over that range (10^-9).
+// Cosine and sine of an angle, the sine's sign turned over for an inverse.  The angle becomes quarter turns and r, the rest as half-turns (-1/4 .. 1/4, and up
+// to 0.28 near 2^20 radians, where the product that is rounded to quarters is off itself): the constant 1 / (2 pi) in two floats (2^-48 of it is missing, 2^-30
+// turns at 2^20 radians), the products in fused operations, the rest off by 2^-27 turns; sin(pi r) / r and (cos(pi r) - 1) / r^2 are polynomials of third
+// degree in r^2, fitted to least maximal error over -1/4 .. 1/4.  With their coefficients as the floats that they are the sine is off by 2.6e-8 and the cosine by
+// 7e-9 there, by 7.3e-8 and 1.2e-8 at 0.28; in all 1.7e-7 at most over seven million angles below 2^20 (2^-22 is 2.4e-7).
 __device__ __forceinline__ float2 turn_of(float angle, int inverse) {
     float rest, quarters;
     if (__builtin_expect(__builtin_fabsf(angle) < 1048576.f, 1)) {

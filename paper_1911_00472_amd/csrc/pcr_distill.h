@@ -9,10 +9,10 @@
 // Sums over a row are made in 32 bits relative to its maximum.  Bound by memory: a row is read once for the loss, and read and written once for loss and
 // gradient: a team of threads holds it in its registers, packed as it came, and makes its exponentials where they are used (k_distill_rows).  Rows too
 // long for that are read with a running maximum and again for the gradient (k_distill), a few long ones in shares (k_distill_part, k_distill_join).
-// us (floor at a large copy's 5.0 TB/s): loss and gradient of 4096 rows of 50001 bfloat logits with labels, T = 2: 168 (164), read twice 323; of 2048 of
-// 131071: 247 (215); of 4096 of 32000: 106 (105); of 8192 of 10000: 72 (66); loss of 8192 rows of 50001: 181 (164), with a running maximum 262; gradient from
-// saved sums of 4096 rows of 131072 half-precision logits: 426 (430).  Short rows are bound by the trips to memory of a wavefront that follow each other:
-// 16384 rows of 300 classes with 10 entries take 15 (4).
+// us (what the bytes take at the 5.0 TB/s of a large copy): loss and gradient of 4096 rows of 50001 bfloat logits with labels, T = 2: 166 (164), read twice 323; of
+// 2048 of 131071: 261 (215), 243 with T = 1; of 4096 of 32000: 106 (105); of 8192 of 10000: 73 (66); loss of 8192 rows of 50001: 182 (164), with a running maximum
+// 262; gradient from saved sums of 4096 rows of 131072 half-precision logits: 423 (430).  Short rows are bound by the trips to memory of a wavefront that
+// follow each other: 16384 rows of 300 classes with 10 entries take 13 for the loss (2), 16 for the gradient (4), 18 for both (4).
 #pragma once
 #include <type_traits>
 
@@ -375,7 +375,7 @@ template <int TEAM, int C, bool MAX> __device__ __forceinline__ void team_join_a
 }
 
 // exp((x - m) / T) and, where BY is not kOneSum, exp(x - m): by an exponential of its own, or as the second or fourth power of the first (T = 2, 4), which is
-// twice or four times as far off, 2^-21 of itself.  (2048 rows of 131071 logits with labels: 265 us with T = 2, 307 with T = 3; 8192 of 10000: 69 with T = 4, 74.)
+// twice or four times as far off, 2^-21 of itself.  (2048 rows of 131071 logits with labels: 261 us with T = 2, 278 with T = 4, 300 with T = 3; 8192 of 10000: 73, 74, 77.)
 enum { kOneSum = 1, kTwoSums = 0, kSquare = 2, kFourth = 4 };
 template <int BY> __device__ __forceinline__ void exps(float x, float m, float c, float T, float& e, float& e1) {
     const float y = (x - m) * c;

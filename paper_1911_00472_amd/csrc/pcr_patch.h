@@ -2,7 +2,8 @@
 //
 // Row r of picture i holds a patch as [channel][y][x], (pixel / 255 - mean) inv_std, written as one multiply-add of the pixel with
 // inv_std / 255 and -mean inv_std (its error, 2^-24 of each of the two, is far below the rounding to 16 bits and within three units of 32).
-// Bound by memory: a pixel byte in, two or four bytes out.  1024 photographs of 300 to 500 pixels a side, us (floor: the bytes at a large copy's 5.0 TB/s):
+// Bound by memory: a pixel byte in, two or four bytes out.  1024 photographs of 300 to 500 pixels a side, us (the bytes at the 5.0 TB/s of a large copy, which reads
+// as much as it writes):
 // patches of 14, bfloat 304, in windows of 2 x 2 319 (312), of 16 285 (305), of 8 300 (310), of 28 303; 512 of them in 32 bits, patches of 16 245 (253), of 14 247.
 // An element a lane and loads of bytes took 1228 with patches of 14; eight pixels a lane with stores in pieces 504; one load of a lane under way at a time 340.
 #pragma once

@@ -151,14 +151,14 @@ def distill_forward(logits, top_index, top_logits, labels=None, temperature=1.0,
 
 
 def distill_backward(row_grad, logits, top_index, top_logits, sums, labels=None, temperature=1.0, distill_part=1.0, label_part=0.0, out=None, stream=None):
-    """The gradient of the logits for row_grad, the gradient of every row's loss (float32 [rows]), from distill_forward's sums.  out: where to (the logits
-    themselves, too)."""
+    """The gradient of the logits for row_grad, the gradient of every row's loss (float32 [rows]), from distill_forward's sums (which are made anew from the
+    logits for rows whose sums are 128 or more in magnitude).  out: where to (the logits themselves, too, if they are no leaf that requires a gradient)."""
     return _call(stream, _train.distill_backward, row_grad, logits, top_index, top_logits, sums, labels, temperature, distill_part, label_part, out)
 
 
 def distill_step(logits, top_index, top_logits, row_weight, labels=None, temperature=1.0, distill_part=1.0, label_part=0.0, out=None, stream=None):
     """(loss, gradient) in one pass: loss[n] = row_weight[n] * distill_forward's loss, and the gradient of their sum.  A row of weight 0 is left out whatever
-    it holds.  out: where the gradient goes (the logits themselves, too)."""
+    it holds.  out: where the gradient goes (the logits themselves, too, if they are no leaf that requires a gradient)."""
     return _call(stream, _train.distill_step, logits, top_index, top_logits, row_weight, labels, temperature, distill_part, label_part, out)
 
 
