@@ -564,6 +564,76 @@ int pcr_distill_backward(int device_id, const pcr_distill* d, const float* sums,
 int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weight, float* loss, void* out, int64_t out_stride, void* d_work,
                      size_t work_bytes, void* hip_stream);
 
+/* ---- layers of a network that trains on the pictures ----
+ *
+ * What stands between its matrix products, under the same rules as above: group norm with an activation over feature maps, a bias of attention for the
+ * relative position of its tokens, dropout onto a residual.
+ *
+ * Group norm, channels last: x [image][pixel][channel] with strides of images and pixels, channels contiguous; `groups` groups of channels / groups channels each
+ * (channels 1 .. 16384, groups 1 .. 4096, a divisor of channels).  Over the pixels and channels of a group  m = mean x, r = 1 / sqrt(mean (x - m)^2 + eps),
+ * y = act((x - m) r weight + bias); weight, bias: [channel] of weight_dtype (float, or dtype), NULL: ones and zeros.  activation: PCR_ACT_NONE;
+ * RELU (0 for z <= 0, with slope 0 there); SILU z / (1 + exp(-z)); GELU z (1 + erf(z / sqrt 2)) / 2.
+ * pcr_group_norm_forward: out: y (it may be x with its strides; otherwise they must not overlap); stats float [image][group][2]: m and r.
+ * pcr_group_norm_backward: grad: the gradient of y; stats: as forward gave them; out: the gradient of x (it may be grad or x with its strides); weight_grad, bias_grad: float
+ *   [channel], summed over images and pixels in a fixed order (NULL: not asked for).  eps is not used.  No images or pixels: weight and bias gradients are zeros.
+ * d_work: pcr_group_norm_workspace bytes for the pass that is to be made (backward: 0 or 1), its content is of no account before and after. */
+enum { PCR_ACT_NONE = 0, PCR_ACT_RELU = 1, PCR_ACT_SILU = 2, PCR_ACT_GELU = 3 };
+typedef struct pcr_group_norm {
+    const void* x; int64_t x_image, x_pixel;
+    void* out; int64_t out_image, out_pixel;
+    const void* grad; int64_t grad_image, grad_pixel;
+    const void* weight; const void* bias; float* stats; float* weight_grad; float* bias_grad;
+    int64_t images, pixels, channels;
+    int32_t groups, activation, dtype, weight_dtype;
+    float eps, reserved;
+} pcr_group_norm;
+int pcr_group_norm_workspace(const pcr_group_norm* norm, int backward, size_t* nbytes);
+int pcr_group_norm_forward(int device_id, const pcr_group_norm* norm, void* d_work, size_t work_bytes, void* hip_stream);
+int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_work, size_t work_bytes, void* hip_stream);
+
+/* A learned bias for the relative position of queries and keys, by buckets: with positions of up to four axes (as of pcr_patch_rows),
+ *   bucket = sum over the axes a of map[a][reach + min(max(key position - query position, -reach), reach)]     (as 32-bit integers),
+ *   bias[batch][head][query][key] = table[bucket][head]; 0 for a bucket outside 0 .. buckets - 1.
+ * Where segments are given, a query and a key of different segments have -inf, and all keys of a query whose segment is below 0 (padding) 0.
+ *   positions    int32, or int64 where `wide` is set, [axes][batch][token] with their strides (the same for every sequence: a batch stride of 0)
+ *   segments     int32 [batch][token] with their strides, of queries and keys, or both NULL
+ *   map          int32 [axes][2 reach + 1]; axes 1 .. 4, reach 0 .. 2^24;  buckets 1 .. 2^24, heads up to 65535
+ *   table        [bucket][head] of table_dtype (float, or dtype)
+ *   values       dtype, with strides of batch, heads and queries, keys contiguous: the bias, written; of the backward pass its gradient, read
+ * pcr_position_bias_backward: table_grad float [bucket][head]: the sum of the gradient over the pairs of each bucket, in a fixed order; pairs that have no
+ *   bias add nothing, whatever their gradient holds.  d_work: pcr_position_bias_workspace bytes. */
+typedef struct pcr_places {
+    const void* position; int64_t axis_stride, batch_stride, token_stride;
+    const int32_t* segment; int64_t segment_batch_stride, segment_token_stride;
+} pcr_places;
+typedef struct pcr_position_table {
+    pcr_places query, key;
+    const int32_t* map; const void* table;
+    void* values; int64_t value_batch, value_head, value_query;
+    int64_t batch, heads, queries, keys, buckets;
+    int32_t axes, reach, wide, dtype, table_dtype, reserved;
+} pcr_position_table;
+int pcr_position_bias(int device_id, const pcr_position_table* t, void* hip_stream);
+int pcr_position_bias_workspace(const pcr_position_table* t, size_t* nbytes);
+int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float* table_grad, void* d_work, size_t work_bytes, void* hip_stream);
+
+/* Dropout: out[row][column] = residual + (kept ? x / (1 - p) : 0), one rounding; a dropped element is 0 whatever it holds.  Element e = row * dim + column is dropped where
+ * word e mod 4 of Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) for the key seed[0] (low word first) and the counter words (e / 4's low word, e / 4's high word + 65536 call,
+ * seed[1]'s low and high word) is below p 2^32 (rounded to the nearest; p = 1 drops everything).  The mask depends on nothing else, not on strides or alignment, and its gradient
+ * is the call without a residual on the incoming gradient.
+ *   x          dtype; residual (may be NULL) and out: out_dtype, which is dtype, or one of the two is PCR_FLOAT.  Rows contiguous, row strides in elements.
+ *              out may be x (where the types are the same) or residual with the same strides; otherwise they must not overlap
+ *   seed       device, int64 [2]: key and step; read when the work runs, so that a captured graph that counts the step up drops anew at every replay
+ *   used       device, int64 [2], may be NULL: seed as it was read, for the gradient
+ *   p          0 .. 1;  call: 0 .. 65535, tells the dropouts of a step apart;  rows * dim below 2^50 */
+typedef struct pcr_dropout {
+    const void* x; const void* residual; void* out; const int64_t* seed; int64_t* used;
+    int64_t rows, dim, x_row, residual_row, out_row;
+    double p;
+    int32_t dtype, out_dtype, call, reserved;
+} pcr_dropout;
+int pcr_dropout_add(int device_id, const pcr_dropout* d, void* hip_stream);
+
 /* Diagnostics: the rate (10^9 instructions per second, whole device) at which `waves_per_cu` (1..32)
  * resident wavefronts per compute unit issue chains of dependent scalar-ALU instructions -- the kind of
  * work the wave-uniform entropy decoders consist of (Section 4.2 of the paper names the decode as the

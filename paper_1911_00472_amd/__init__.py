@@ -5,7 +5,8 @@ from .binding import (E_ARG, E_DEVICE, E_FORMAT, E_NOMEM, E_RANGE, E_TRUNCATED, 
                       probe_scalar_issue_rate, record_write, record_write_indexed, scan_ends, transcode_files, transcode_progressive, transcode_symbol_counts)
 
 _TRAIN = ("patch_layout", "patch_rows", "axis_frequencies", "rotate_axes", "norm_rotate", "norm_rotate_backward", "distill_forward", "distill_backward",
-          "distill_step", "distill_loss")
+          "distill_step", "distill_loss", "group_norm_forward", "group_norm_backward", "group_norm", "position_buckets", "position_bias", "position_bias_backward", "dropout",
+          "dropout_backward")
 
 
 def _deferred(name):

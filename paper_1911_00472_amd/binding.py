@@ -92,6 +92,13 @@ SYMBOLS = {
     "pcr_distill_forward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "pcr_distill_backward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp]),
     "pcr_distill_step": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp, ctypes.c_size_t, _vp]),
+    "pcr_group_norm_workspace": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "pcr_group_norm_forward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, ctypes.c_size_t, _vp]),
+    "pcr_group_norm_backward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, ctypes.c_size_t, _vp]),
+    "pcr_position_bias": (ctypes.c_int, [ctypes.c_int, _vp, _vp]),
+    "pcr_position_bias_workspace": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_size_t)]),
+    "pcr_position_bias_backward": (ctypes.c_int, [ctypes.c_int, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "pcr_dropout_add": (ctypes.c_int, [ctypes.c_int, _vp, _vp]),
     "pcr_strerror": (ctypes.c_char_p, [ctypes.c_int]),
 }
 

@@ -7,6 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "pcr_lib.hip")                # the decoder, the loader, records
 SRC_TRAIN = os.path.join(HERE, "csrc", "pcr_train.hip")        # the operators behind the decode
 SRC_DISTILL = os.path.join(HERE, "csrc", "pcr_distill.hip")
+SRC_LAYERS = os.path.join(HERE, "csrc", "pcr_layers.hip")      # group norm, position bias, dropout
 SRC_BIND = os.path.join(HERE, "csrc", "pcr_bind.cpp")          # their arguments, as a Python module
 LIB = os.path.join(HERE, "libpcr.so")
 MODULE = os.path.join(HERE, "_train.so")
@@ -27,8 +28,8 @@ def build_library():
     """Compile csrc/ into libpcr.so (always recompiles): the C ABI, which needs neither PyTorch nor Python's headers."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     compile_only = [hipcc, "-c"] + [f for f in HIPCC_FLAGS if f != "-shared"]
-    sources = (SRC, SRC_TRAIN, SRC_DISTILL)
-    objects = [s[:-len(".hip")] + ".o" for s in sources]
+    sources = (SRC, SRC_TRAIN, SRC_DISTILL, SRC_LAYERS)
+    objects = [os.path.join(os.path.dirname(LIB), os.path.basename(s)[:-len(".hip")] + ".o") for s in sources]
     running = [subprocess.Popen(compile_only + ["-o", o, s]) for s, o in zip(sources, objects)]
     failed = [p.args for p in running if p.wait() != 0]
     if failed:

@@ -1,4 +1,4 @@
-// Python module _train: the operators behind the decode (include/pcr.h) on PyTorch tensors.  Checks of arguments, allocation of results
+// Python module _train: the operators behind the decode and the layers of a network (include/pcr.h) on PyTorch tensors.  Checks of arguments, allocation of results
 // and the call of the C entry point, for train.py: a call made of ctypes and Python checks takes 15 to 25 us of the host's time, which is three to five
 // times what a small call takes the GPU, and 5 to 8 us here.
 // Every function takes its arguments by position and works on PyTorch's current stream; a wrong argument raises ValueError, an error of the
@@ -442,6 +442,263 @@ PyObject* distill_step(PyObject*, PyObject* const* a, Py_ssize_t given) {       
     });
 }
 
+// ---- layers between matrix products ----
+
+// A tensor's dimensions but the last, from `from` on, as one: how many places there are, and their stride.  False: they do not lie at one stride.
+bool one_stride(const at::Tensor& t, int64_t from, int64_t& places, int64_t& stride) {
+    places = 1;
+    stride = 0;
+    for (int64_t d = t.dim() - 2; d >= from; d--) {
+        if (t.size(d) == 1) continue;
+        if (places == 1) stride = t.stride(d);
+        else if (t.stride(d) != stride * places && t.numel()) return false;
+        places *= t.size(d);
+    }
+    return true;
+}
+bool row_lies(const at::Tensor& t) { return t.size(-1) == 1 || t.stride(-1) == 1 || !t.numel(); }
+
+struct GroupNorm {
+    const at::Tensor& x;
+    pcr_group_norm n = {};
+    GroupNorm(PyObject* at_x, PyObject* groups, PyObject* weight, PyObject* bias, PyObject* activation) : x(tensor(at_x, "x")) {
+        need(x.is_cuda() && type_of(x) >= 0 && x.dim() >= 2, "x", "float32, float16 or bfloat16 [images, ..., channels] on the GPU is wanted");
+        n.dtype = type_of(x);
+        n.channels = x.size(-1);
+        n.images = x.size(0);
+        place(x, "x", n.x_image, n.x_pixel);
+        n.x = x.data_ptr();
+        n.groups = small(groups, "groups");
+        need(n.groups >= 1 && n.channels >= 1 && n.channels % n.groups == 0, "groups", "a divisor of the channels is wanted");
+        n.activation = small(activation, "activation");
+        need(n.activation >= 0 && n.activation <= PCR_ACT_GELU, "activation", "none, relu, silu or gelu is wanted");
+        const at::Tensor *w = maybe_tensor(weight, "weight"), *b = maybe_tensor(bias, "bias");
+        check_weight(w, x, "weight");
+        check_weight(b, x, "bias");
+        need(!w || !b || w->scalar_type() == b->scalar_type(), "weight and bias: one type is wanted");
+        n.weight_dtype = w ? type_of(*w) : b ? type_of(*b) : n.dtype;
+        n.weight = w ? w->data_ptr() : nullptr;
+        n.bias = b ? b->data_ptr() : nullptr;
+    }
+    void place(const at::Tensor& t, const char* name, int64_t& image, int64_t& pixel) {
+        need(row_lies(t) && one_stride(t, 1, n.pixels, pixel), name, "channels that follow each other, and pixels at one stride, are wanted");
+        image = t.size(0) > 1 ? t.stride(0) : 0;
+    }
+    at::Tensor into(PyObject* o, const char* name) {
+        const at::Tensor* t = maybe_tensor(o, name);
+        if (t) {
+            on(*t, x, name);
+            need(t->scalar_type() == x.scalar_type() && t->sizes() == x.sizes(), name, "the type and shape of x is wanted");
+            check_written(*t, name);
+            for (int64_t i = 0; i < t->dim(); i++) need(t->stride(i) != 0 || t->size(i) < 2, name, "every element needs a place of its own");
+        }
+        const at::Tensor out = t ? *t : at::empty(x.sizes(), x.options());
+        place(out, name, n.out_image, n.out_pixel);
+        n.out = out.data_ptr();
+        return out;
+    }
+    at::Tensor work(int backward, size_t& bytes) const {
+        check(pcr_group_norm_workspace(&n, backward, &bytes), "pcr_group_norm_workspace");
+        return bytes ? at::empty({(int64_t)bytes}, x.options().dtype(at::kByte)) : at::Tensor();
+    }
+};
+
+PyObject* group_norm_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {  // x groups weight bias eps activation out
+    return guarded(given, 7, [&] {
+        GroupNorm G(a[0], a[1], a[2], a[3], a[5]);
+        const double eps = number(a[4]);
+        need(eps >= 0, "eps", "not below 0");
+        G.n.eps = (float)eps;
+        const at::Tensor out = G.into(a[6], "out"), stats = at::empty({G.n.images, G.n.groups, 2}, G.x.options().dtype(at::kFloat));
+        G.n.stats = (float*)stats.data_ptr();
+        size_t bytes = 0;
+        const at::Tensor work = G.work(0, bytes);
+        check(pcr_group_norm_forward(device_number(G.x), &G.n, bytes ? work.data_ptr() : nullptr, bytes, stream_of(G.x)), "pcr_group_norm_forward");
+        written(a[6]);
+        return tuple(some(out), some(stats));
+    });
+}
+
+PyObject* group_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t given) { // grad x groups weight bias stats activation dx
+    return guarded(given, 8, [&] {
+        GroupNorm G(a[1], a[2], a[3], a[4], a[6]);
+        const at::Tensor &g = tensor(a[0], "grad"), &stats = tensor(a[5], "stats");
+        on(g, G.x, "grad");
+        need(g.scalar_type() == G.x.scalar_type() && g.sizes() == G.x.sizes(), "grad", "the type and shape of x is wanted");
+        G.place(g, "grad", G.n.grad_image, G.n.grad_pixel);
+        G.n.grad = g.data_ptr();
+        on(stats, G.x, "stats");
+        need(stats.scalar_type() == at::kFloat && stats.dim() == 3 && stats.size(0) == G.n.images && stats.size(1) == G.n.groups && stats.size(2) == 2 && stats.is_contiguous(), "stats",
+             "contiguous float32 [images, groups, 2] is wanted");
+        G.n.stats = (float*)stats.data_ptr();
+        const at::Tensor out = G.into(a[7], "dx");
+        at::Tensor sums[2];
+        for (int z = 0; z < 2; z++)
+            if (z ? G.n.bias : G.n.weight) {
+                sums[z] = at::empty({G.n.channels}, G.x.options().dtype(at::kFloat));
+                (z ? G.n.bias_grad : G.n.weight_grad) = (float*)sums[z].data_ptr();
+            }
+        size_t bytes = 0;
+        const at::Tensor work = G.work(1, bytes);
+        check(pcr_group_norm_backward(device_number(G.x), &G.n, bytes ? work.data_ptr() : nullptr, bytes, stream_of(G.x)), "pcr_group_norm_backward");
+        written(a[7]);
+        return tuple(some(out), G.n.weight ? some(sums[0]) : none(), G.n.bias ? some(sums[1]) : none());
+    });
+}
+
+// Positions and segments of queries and keys, and what they are like: a bias, or the gradient of its table.
+struct PositionTable {
+    const at::Tensor& positions;
+    pcr_position_table t = {};
+    bool batched = false;
+    PositionTable(PyObject* q, PyObject* k, PyObject* map, PyObject* q_segments, PyObject* k_segments) : positions(tensor(q, "positions")) {
+        const at::Tensor *keys = maybe_tensor(k, "key_positions"), *s = maybe_tensor(q_segments, "segments"), *ks = maybe_tensor(k_segments, "key_segments");
+        const at::Tensor& m = tensor(map, "buckets");
+        need(positions.is_cuda(), "positions", "a tensor on the GPU is wanted");
+        need(s || !ks, "key_segments", "without segments");
+        need(!s || ks || !keys, "key_segments", "are wanted where there are key_positions and segments");
+        if (!keys) keys = &positions;
+        if (s && !ks) ks = s;
+        t.batch = 1;
+        place(positions, "positions", t.query, t.queries);
+        place(*keys, "key_positions", t.key, t.keys);
+        need(keys->size(0) == positions.size(0) && keys->scalar_type() == positions.scalar_type(), "key_positions", "the axes and the type of positions are wanted");
+        if (s) {
+            place_segments(*s, "segments", t.query, t.queries);
+            place_segments(*ks, "key_segments", t.key, t.keys);
+        }
+        t.wide = positions.scalar_type() == at::kLong;
+        need(positions.size(0) >= 1 && positions.size(0) <= 4, "positions", "one to four axes are wanted");
+        t.axes = (int32_t)positions.size(0);
+        on(m, positions, "buckets");
+        need(m.scalar_type() == at::kInt && m.dim() == 2 && m.size(0) == t.axes && m.size(1) % 2 == 1 && m.is_contiguous(), "buckets", "contiguous int32 [axes, 2 * reach + 1] is wanted");
+        need(m.size(1) / 2 <= (1 << 24), "buckets", "out of range");
+        t.reach = (int32_t)(m.size(1) / 2);
+        t.map = (const int32_t*)m.data_ptr();
+    }
+    void sequences(const at::Tensor& p, const char* name, int64_t n) {
+        need(!batched || t.batch == n, name, "one number of sequences is wanted");
+        batched = true;
+        t.batch = n;
+    }
+    void place(const at::Tensor& p, const char* name, pcr_places& P, int64_t& tokens) {
+        on(p, positions, name);
+        need((p.scalar_type() == at::kInt || p.scalar_type() == at::kLong) && (p.dim() == 2 || p.dim() == 3), name, "int32 or int64 [axes, tokens] or [axes, batch, tokens] is wanted");
+        if (p.dim() == 3) sequences(p, name, p.size(1));
+        tokens = p.size(-1);
+        P.position = p.data_ptr(); P.axis_stride = p.stride(0); P.batch_stride = p.dim() == 3 ? p.stride(1) : 0; P.token_stride = p.stride(-1);
+    }
+    void place_segments(const at::Tensor& p, const char* name, pcr_places& P, int64_t tokens) {
+        on(p, positions, name);
+        need(p.scalar_type() == at::kInt && (p.dim() == 1 || p.dim() == 2) && p.size(-1) == tokens, name, "int32 [tokens] or [batch, tokens] is wanted");
+        if (p.dim() == 2) sequences(p, name, p.size(0));
+        P.segment = (const int32_t*)p.data_ptr(); P.segment_batch_stride = p.dim() == 2 ? p.stride(0) : 0; P.segment_token_stride = p.stride(-1);
+    }
+    // The bias or its gradient, [heads, queries, keys] or [batch, heads, queries, keys].
+    void place_values(const at::Tensor& v, const char* name) {
+        on(v, positions, name);
+        need(type_of(v) >= 0 && v.dim() == (batched ? 4 : 3) && (!batched || v.size(0) == t.batch) && v.size(-2) == t.queries && v.size(-1) == t.keys && row_lies(v), name,
+             "float32, float16 or bfloat16 [(batch,) heads, queries, keys], keys that follow each other, is wanted");
+        t.dtype = type_of(v);
+        t.heads = v.size(-3);
+        t.values = v.data_ptr(); t.value_batch = batched ? v.stride(0) : 0; t.value_head = v.stride(-3); t.value_query = v.stride(-2);
+    }
+};
+
+PyObject* position_bias(PyObject*, PyObject* const* a, Py_ssize_t given) {       // table positions buckets key_positions segments key_segments dtype out
+    return guarded(given, 8, [&] {
+        const at::Tensor& table = tensor(a[0], "table");
+        PositionTable P(a[1], a[3], a[2], a[4], a[5]);
+        on(table, P.positions, "table");
+        need(type_of(table) >= 0 && table.dim() == 2 && table.size(0) >= 1 && table.is_contiguous(), "table", "contiguous float32, float16 or bfloat16 [buckets, heads] is wanted");
+        const at::Tensor* to = maybe_tensor(a[7], "out");
+        const int dtype = small(a[6], "dtype");
+        need(to || dtype <= 2, "dtype", "float32, float16 or bfloat16 is wanted");
+        at::Tensor out;
+        if (to) {
+            P.place_values(*to, "out");
+            need(P.t.heads == table.size(1), "out", "the heads of table are wanted");
+            check_written(*to, "out");
+            for (int64_t i = 0; i < to->dim(); i++) need(to->stride(i) != 0 || to->size(i) < 2, "out", "every element needs a place of its own");
+            out = *to;
+        } else {
+            const auto kind = dtype < 0 ? table.scalar_type() : dtype == PCR_FLOAT ? at::kFloat : dtype == PCR_HALF ? at::kHalf : at::kBFloat16;
+            const auto options = table.options().dtype(kind);
+            out = P.batched ? at::empty({P.t.batch, table.size(1), P.t.queries, P.t.keys}, options) : at::empty({table.size(1), P.t.queries, P.t.keys}, options);
+            P.place_values(out, "out");
+        }
+        need(table.scalar_type() == at::kFloat || table.scalar_type() == out.scalar_type(), "table", "float32 or the result's type is wanted");
+        P.t.table = table.data_ptr();
+        P.t.table_dtype = type_of(table);
+        P.t.buckets = table.size(0);
+        check(pcr_position_bias(device_number(table), &P.t, stream_of(table)), "pcr_position_bias");
+        written(a[7]);
+        return some(out);
+    });
+}
+
+PyObject* position_bias_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {   // grad positions buckets count key_positions segments key_segments
+    return guarded(given, 7, [&] {
+        const at::Tensor& g = tensor(a[0], "grad");
+        PositionTable P(a[1], a[4], a[2], a[5], a[6]);
+        P.place_values(g, "grad");
+        P.t.buckets = integer(a[3]);
+        need(P.t.buckets >= 1 && P.t.buckets <= (1 << 24), "count", "out of range");
+        const at::Tensor sums = at::empty({P.t.buckets, P.t.heads}, g.options().dtype(at::kFloat));
+        size_t bytes = 0;
+        check(pcr_position_bias_workspace(&P.t, &bytes), "pcr_position_bias_workspace");
+        const at::Tensor work = bytes ? at::empty({(int64_t)bytes}, g.options().dtype(at::kByte)) : at::Tensor();
+        check(pcr_position_bias_backward(device_number(g), &P.t, (float*)sums.data_ptr(), bytes ? work.data_ptr() : nullptr, bytes, stream_of(g)), "pcr_position_bias_backward");
+        return some(sums);
+    });
+}
+
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t given) {             // x p seed call residual dtype out used: (result, the seed as it was read or None)
+    return guarded(given, 8, [&] {
+        const at::Tensor &x = tensor(a[0], "x"), &seed = tensor(a[2], "seed");
+        const at::Tensor *residual = maybe_tensor(a[4], "residual"), *to = maybe_tensor(a[6], "out");
+        pcr_dropout d = {};
+        need(x.is_cuda() && type_of(x) >= 0 && x.dim() >= 1, "x", "float32, float16 or bfloat16 [..., dim] on the GPU is wanted");
+        on(seed, x, "seed");
+        need(seed.scalar_type() == at::kLong && seed.dim() == 1 && seed.size(0) == 2 && seed.is_contiguous(), "seed", "contiguous int64 [2] is wanted");
+        d.p = number(a[1]);
+        need(d.p >= 0.0 && d.p <= 1.0, "p", "0 to 1 is wanted");
+        d.call = small(a[3], "call");
+        need(d.call >= 0 && d.call <= 65535, "call", "0 to 65535 is wanted");
+        d.dim = x.size(-1);
+        auto place = [&](const at::Tensor& t, const char* name, int64_t& stride) {
+            on(t, x, name);
+            need(t.sizes() == x.sizes() && row_lies(t) && one_stride(t, 0, d.rows, stride), name, "x's shape, with rows whose elements follow each other, at one stride, is wanted");
+            if (d.rows < 2) stride = d.dim;
+        };
+        place(x, "x", d.x_row);
+        d.x = x.data_ptr(); d.dtype = type_of(x);
+        auto fits = [&](int dtype) { return dtype >= 0 && (dtype == d.dtype || dtype == PCR_FLOAT || d.dtype == PCR_FLOAT); };
+        if (residual) {
+            place(*residual, "residual", d.residual_row);
+            need(type_of(*residual) == d.dtype || type_of(*residual) == PCR_FLOAT, "residual", "the type of x, or float32 beside it, is wanted");
+            d.residual = residual->data_ptr();
+        }
+        const int wanted = small(a[5], "dtype");               // (-1: the residual's type, or x's)
+        d.out_dtype = to ? type_of(*to) : wanted >= 0 ? wanted : residual ? type_of(*residual) : d.dtype;
+        need(fits(d.out_dtype) && d.out_dtype <= 2, to ? "out" : "dtype", "the type of x, or float32 beside it, is wanted");
+        need(!residual || type_of(*residual) == d.out_dtype, "residual", "the result's type is wanted");
+        if (to) {
+            check_written(*to, "out");
+            for (int64_t i = 0; i < to->dim(); i++) need(to->stride(i) != 0 || to->size(i) < 2, "out", "every element needs a place of its own");
+        }
+        const at::Tensor out = to ? *to : at::empty(x.sizes(), x.options().dtype(d.out_dtype == PCR_FLOAT ? at::kFloat : d.out_dtype == PCR_HALF ? at::kHalf : at::kBFloat16));
+        place(out, "out", d.out_row);
+        d.out = out.data_ptr();
+        const at::Tensor used = truth(a[7]) ? at::empty({2}, seed.options()) : at::Tensor();
+        d.seed = (const int64_t*)seed.data_ptr();
+        d.used = used.defined() ? (int64_t*)used.data_ptr() : nullptr;
+        check(pcr_dropout_add(device_number(x), &d, stream_of(x)), "pcr_dropout_add");
+        written(a[6]);
+        return tuple(some(out), used.defined() ? some(used) : none());
+    });
+}
+
 PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t given) {              // PcrError, the function that gives a device's current stream
     return guarded(given, 2, [&] {
         Py_INCREF(a[0]);
@@ -454,7 +711,7 @@ PyObject* set_up(PyObject*, PyObject* const* a, Py_ssize_t given) {             
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ENTRY(patch_rows), ENTRY(rotate_axes), ENTRY(norm_rotate), ENTRY(norm_rotate_backward), ENTRY(distill_forward), ENTRY(distill_backward),
-                           ENTRY(distill_step), ENTRY(set_up), {nullptr, nullptr, 0, nullptr}};
+                           ENTRY(distill_step), ENTRY(group_norm_forward), ENTRY(group_norm_backward), ENTRY(position_bias), ENTRY(position_bias_backward), ENTRY(dropout), ENTRY(set_up), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_train", "The operators behind the decode on PyTorch tensors.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,327 @@
+// C ABI of the layers of a network that trains on the pictures (see include/pcr.h): group norm with an activation, position bias, dropout.  Checks of arguments,
+// choice of a kernel, launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/pcr.h"
+#include "pcr_bias.h"
+#include "pcr_dropout.h"
+#include "pcr_group_norm.h"
+#include "pcr_host.h"
+
+using namespace pcr;
+
+namespace {
+
+template <int N> using Int = std::integral_constant<int, N>;
+
+bool multiple(const void* p, int64_t a, int64_t b, size_t size, int unit) { return ((uint64_t)(uintptr_t)p / size | (uint64_t)a | (uint64_t)b) % unit == 0; }
+
+// ---- group norm ----
+
+int check_norm(const pcr_group_norm* N, bool back) {
+    if (!N || !known_type(N->dtype) || !known_type(N->weight_dtype) || (N->weight_dtype != PCR_FLOAT && N->weight_dtype != N->dtype)) return PCR_E_ARG;
+    if (N->activation < PCR_ACT_NONE || N->activation > PCR_ACT_GELU) return PCR_E_ARG;
+    if (N->channels < 1 || N->channels > 16384 || N->groups < 1 || N->groups > 4096 || N->channels % N->groups) return PCR_E_RANGE;
+    if (N->images < 0 || N->pixels < 0 || N->images > kMaxGrid || N->pixels > (1ll << 40)) return PCR_E_RANGE;
+    if (!back && !(N->eps >= 0.f && isfinite(N->eps))) return PCR_E_RANGE;
+    if (N->images && N->pixels && (!N->x || !N->out || !N->stats || (back && !N->grad))) return PCR_E_ARG;
+    return PCR_OK;
+}
+
+struct NormPlan {
+    int64_t chunk;
+    int chunks, run;
+    size_t part_bytes, sums_bytes;
+};
+NormPlan plan_norm(const pcr_group_norm* N, bool back) {
+    NormPlan P = {};
+    const size_t size = type_size(N->dtype);
+    // Chunks of a picture's pixels: 2048 workgroups in all, of 64 KB at least.
+    const int64_t row = N->channels * (int64_t)size;
+    int64_t chunks = std::min<int64_t>((2048 + N->images - 1) / std::max<int64_t>(1, N->images), (N->pixels * row + 65535) / 65536);
+    chunks = std::max<int64_t>(1, std::min<int64_t>(chunks, N->pixels));
+    P.chunk = (N->pixels + chunks - 1) / chunks;
+    P.chunks = P.chunk ? (int)((N->pixels + P.chunk - 1) / P.chunk) : 0;
+    P.part_bytes = (size_t)N->images * P.chunks * N->groups * 2 * sizeof(float);
+    P.sums_bytes = back ? (size_t)N->images * P.chunks * N->channels * 2 * sizeof(float) : 0;
+    // Runs of up to 16 bytes of channels.
+    P.run = (int)(16 / size);
+    for (; P.run > 1; P.run >>= 1) {
+        if (N->channels % P.run) continue;
+        if (multiple(N->x, N->x_image, N->x_pixel, size, P.run) && multiple(N->out, N->out_image, N->out_pixel, size, P.run) &&
+            (!back || multiple(N->grad, N->grad_image, N->grad_pixel, size, P.run)))
+            break;
+    }
+    return P;
+}
+NormArgs norm_args(const pcr_group_norm* N, const NormPlan& P, void* d_work) {
+    NormArgs A = {};
+    A.x = N->x; A.grad = N->grad; A.weight = N->weight; A.bias = N->bias; A.out = N->out; A.stats = N->stats;
+    A.part = (float*)d_work; A.sums = (float*)((char*)d_work + P.part_bytes);
+    A.images = N->images; A.pixels = N->pixels;
+    A.x_image = N->x_image; A.x_pixel = N->x_pixel; A.grad_image = N->grad_image; A.grad_pixel = N->grad_pixel; A.out_image = N->out_image; A.out_pixel = N->out_pixel;
+    A.chunk = P.chunk; A.chunks = P.chunks; A.channels = (int)N->channels; A.groups = N->groups; A.each = (int)(N->channels / N->groups);
+    A.activation = N->activation; A.weight_float = N->weight_dtype == PCR_FLOAT; A.eps = N->eps;
+    return A;
+}
+template <typename F> void with_run(int dtype, int run, F f) {
+    with_type(dtype, [&](auto t) {
+        if (run == 8) { if constexpr (sizeof(t) == 2) f(t, Int<8>()); }
+        else if (run == 4) f(t, Int<4>());
+        else if (run == 2) f(t, Int<2>());
+        else f(t, Int<1>());
+    });
+}
+
+// ---- position bias ----
+
+constexpr int kBiasLds = 144 * 1024;                           // of a workgroup, at most
+
+int check_bias(const pcr_position_table* t, bool back) {
+    if (!t || !known_type(t->dtype)) return PCR_E_ARG;
+    if (!back && (!known_type(t->table_dtype) || (t->table_dtype != PCR_FLOAT && t->table_dtype != t->dtype))) return PCR_E_ARG;
+    if (t->axes < 1 || t->axes > 4 || t->reach < 0 || t->reach > (1 << 24) || t->buckets < 1 || t->buckets > (1 << 24) || t->heads < 0 || t->heads > 65535) return PCR_E_RANGE;
+    if (t->batch < 0 || t->queries < 0 || t->keys < 0 || t->batch > kMaxGrid || t->queries > kMaxGrid || t->keys > kMaxGrid) return PCR_E_RANGE;
+    if (t->queries && t->keys && t->batch > (1ll << 50) / t->queries / t->keys) return PCR_E_RANGE;
+    if (!t->query.segment != !t->key.segment) return PCR_E_ARG;
+    if (t->batch && t->queries && t->keys && t->heads && (!t->query.position || !t->key.position || !t->map || !t->values || (!back && !t->table))) return PCR_E_ARG;
+    return PCR_OK;
+}
+BiasArgs bias_args(const pcr_position_table* t) {
+    BiasArgs A = {};
+    const pcr_places* from[2] = {&t->query, &t->key};
+    Places* to[2] = {&A.q, &A.k};
+    for (int z = 0; z < 2; z++) {
+        to[z]->position = from[z]->position; to[z]->segment = from[z]->segment;
+        to[z]->axis = from[z]->axis_stride; to[z]->batch = from[z]->batch_stride; to[z]->token = from[z]->token_stride;
+        to[z]->segment_batch = from[z]->segment_batch_stride; to[z]->segment_token = from[z]->segment_token_stride;
+    }
+    A.map = t->map; A.table = t->table; A.values = t->values;
+    A.value_batch = t->value_batch; A.value_head = t->value_head; A.value_query = t->value_query;
+    A.batch = t->batch; A.heads = t->heads; A.queries = t->queries; A.keys = t->keys; A.buckets = t->buckets;
+    const int64_t V = 16 / (int64_t)type_size(t->dtype);
+    A.runs = (A.keys + V - 1) / V;
+    A.items = A.batch * A.queries * A.runs;
+    A.axes = t->axes; A.reach = t->reach; A.wide = t->wide; A.table_float = t->table_dtype == PCR_FLOAT;
+    return A;
+}
+void set_step(BiasArgs& A, int64_t step) {
+    A.step_run = step % A.runs;
+    A.step_query = step / A.runs % A.queries;
+    A.step_batch = step / A.runs / A.queries;
+}
+
+// How the gradient is divided: wavefronts (heads) of a workgroup, copies of a wavefront's bins, ranges of buckets (each goes through all items), shares of the items.
+struct BiasPlan { int waves, copies, ranges; int64_t held, shares, share_items; size_t lds; bool held_map; };
+BiasPlan plan_bias(const pcr_position_table* t) {
+    BiasPlan P = {};
+    const BiasArgs A = bias_args(t);
+    const int V = 16 / (int)type_size(t->dtype);
+    const int64_t map_bytes = (int64_t)t->axes * (2 * t->reach + 1) * 4;
+    P.held_map = map_bytes <= 32 * 1024;
+    P.held = std::min<int64_t>(t->buckets, 8192);
+    P.ranges = (int)((t->buckets + P.held - 1) / P.held);
+    P.copies = 64;
+    while (P.copies > 1 && P.held * P.copies > 4096) P.copies >>= 1;
+    const int64_t bins = P.held * P.copies;
+    auto bytes = [&](int64_t w) { return w * 64 * (2 * V + V) + 32 + w * bins * 4 + (P.copies < 64 ? (w * bins + 15) / 16 * 16 : 0) + (P.held_map ? map_bytes : 0); };
+    const int64_t blocks = (t->heads + 7) / 8;
+    P.waves = (int)std::max<int64_t>(1, (t->heads + std::max<int64_t>(1, blocks) - 1) / std::max<int64_t>(1, blocks));
+    while (P.waves > 1 && bytes(P.waves) > 80 * 1024) P.waves--;
+    P.lds = (size_t)bytes(P.waves);
+    const int64_t head_blocks = std::max<int64_t>(1, (t->heads + P.waves - 1) / P.waves);
+    const int64_t tile = P.waves * 64;
+    P.shares = std::max<int64_t>(1, std::min<int64_t>((A.items + tile - 1) / tile, (1024 + head_blocks - 1) / head_blocks));
+    P.share_items = (A.items + P.shares - 1) / P.shares;
+    P.share_items = (P.share_items + 63) / 64 * 64;
+    P.shares = P.share_items ? std::max<int64_t>(1, (A.items + P.share_items - 1) / P.share_items) : 1;
+    return P;
+}
+
+template <typename K> bool allow_lds(K kernel, size_t bytes) {
+    return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pcr_group_norm_workspace(const pcr_group_norm* norm, int backward, size_t* nbytes) {
+    if (!norm || !nbytes) return PCR_E_ARG;
+    if (!known_type(norm->dtype)) return PCR_E_ARG;
+    if (norm->channels < 1 || norm->channels > 16384 || norm->groups < 1 || norm->groups > 4096 || norm->channels % norm->groups || norm->images < 0 || norm->pixels < 0 ||
+        norm->images > kMaxGrid || norm->pixels > (1ll << 40)) return PCR_E_RANGE;
+    const NormPlan P = plan_norm(norm, backward != 0);
+    *nbytes = P.part_bytes + P.sums_bytes;
+    return PCR_OK;
+}
+
+int pcr_group_norm_forward(int device_id, const pcr_group_norm* norm, void* d_work, size_t work_bytes, void* hip_stream) {
+    const int rc = check_norm(norm, false);
+    if (rc) return rc;
+    if (!norm->images || !norm->pixels) return PCR_OK;
+    const NormPlan P = plan_norm(norm, false);
+    if (!d_work) return PCR_E_ARG;
+    if (work_bytes < P.part_bytes) return PCR_E_RANGE;
+    if (norm->images * P.chunks > groups_of_a_launch(kNormThreads)) return PCR_E_RANGE;
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
+    const NormArgs A = norm_args(norm, P, d_work);
+    const hipStream_t s = (hipStream_t)hip_stream;
+    with_run(norm->dtype, P.run, [&](auto t, auto v) {
+        typedef decltype(t) T;
+        constexpr int V = decltype(v)::value;
+        const unsigned groups = (unsigned)(A.images * A.chunks);
+        hipLaunchKernelGGL((k_norm_sums<T, V>), dim3(groups), dim3(kNormThreads), (kNormThreads * V + 2 * A.groups) * sizeof(float), s, A);
+        hipLaunchKernelGGL(k_norm_stats, dim3((unsigned)((A.images * A.groups + 63) / 64)), dim3(64), 0, s, A);
+        hipLaunchKernelGGL((k_norm_apply<T, V>), dim3(groups), dim3(kNormThreads), 0, s, A);
+    });
+    return launched();
+}
+
+int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_work, size_t work_bytes, void* hip_stream) {
+    const int rc = check_norm(norm, true);
+    if (rc) return rc;
+    const NormPlan P = plan_norm(norm, true);
+    const bool none = !norm->images || !norm->pixels;
+    if (!none && !d_work) return PCR_E_ARG;
+    if (!none && work_bytes < P.part_bytes + P.sums_bytes) return PCR_E_RANGE;
+    if (norm->images * P.chunks > groups_of_a_launch(kNormThreads)) return PCR_E_RANGE;
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
+    const NormArgs A = norm_args(norm, P, d_work);
+    const hipStream_t s = (hipStream_t)hip_stream;
+    if (!none)
+        with_run(norm->dtype, P.run, [&](auto t, auto v) {
+            typedef decltype(t) T;
+            constexpr int V = decltype(v)::value;
+            const unsigned groups = (unsigned)(A.images * A.chunks);
+            hipLaunchKernelGGL((k_norm_back_sums<T, V>), dim3(groups), dim3(kNormThreads), (kNormThreads * V + 2 * A.groups) * sizeof(float), s, A);
+            hipLaunchKernelGGL((k_norm_back_apply<T, V>), dim3(groups), dim3(kNormThreads), 2 * A.groups * sizeof(float), s, A);
+        });
+    if (norm->weight_grad || norm->bias_grad) {
+        NormWeightSums W = {A.sums, norm->weight_grad, norm->bias_grad, none ? 0 : A.images * A.chunks, A.channels};
+        hipLaunchKernelGGL(k_norm_weight_sums, dim3((2 * A.channels + 15) / 16), dim3(1024), 0, s, W);
+    }
+    return launched();
+}
+
+int pcr_position_bias(int device_id, const pcr_position_table* t, void* hip_stream) {
+    const int rc = check_bias(t, false);
+    if (rc) return rc;
+    if (!t->batch || !t->queries || !t->keys || !t->heads) return PCR_OK;
+    BiasArgs A = bias_args(t);
+    const size_t size = type_size(t->dtype);
+    const size_t map_bytes = (size_t)t->axes * (2 * t->reach + 1) * 4;
+    auto lds = [&](int heads) { return ((size_t)(t->buckets + 2) * heads * size + 15) / 16 * 16 + map_bytes; };
+    // Heads side by side: 16 bytes of them, fewer where the table is long.
+    int together = (int)(16 / size);
+    while (together > 1 && (together >= 2 * t->heads || lds(together) > 72 * 1024)) together >>= 1;
+    const bool held = lds(together) <= (size_t)kBiasLds;
+    if (!held) together = 4;
+    const size_t bytes = held ? lds(together) : 0;
+    const int threads = bytes > 36 * 1024 ? 1024 : 256;
+    const int64_t most = bytes > 72 * 1024 ? 256 : bytes > 36 * 1024 ? 512 : 2048;
+    const int64_t blocks = (t->heads + together - 1) / together;
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((A.items + 2 * threads - 1) / (2 * threads), (most + blocks - 1) / blocks));
+    set_step(A, groups * threads);
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
+    bool ok = true;
+    with_type(t->dtype, [&](auto v) {
+        typedef decltype(v) T;
+        auto launch = [&](auto h, auto in_lds) {
+            const auto kernel = k_bias<T, decltype(h)::value, decltype(in_lds)::value>;
+            ok = allow_lds(kernel, bytes);
+            if (ok) hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)blocks), dim3(threads), bytes, (hipStream_t)hip_stream, A);
+        };
+        if (!held) launch(Int<4>(), std::false_type());
+        else if (together == 8) { if constexpr (sizeof(T) == 2) launch(Int<8>(), std::true_type()); }
+        else if (together == 4) launch(Int<4>(), std::true_type());
+        else if (together == 2) launch(Int<2>(), std::true_type());
+        else launch(Int<1>(), std::true_type());
+    });
+    if (!ok) return PCR_E_DEVICE;
+    return launched();
+}
+
+int pcr_position_bias_workspace(const pcr_position_table* t, size_t* nbytes) {
+    if (!nbytes) return PCR_E_ARG;
+    const int rc = check_bias(t, true);
+    if (rc) return rc;
+    const BiasPlan P = plan_bias(t);
+    *nbytes = (size_t)P.shares * t->heads * t->buckets * sizeof(float);
+    return PCR_OK;
+}
+
+int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float* table_grad, void* d_work, size_t work_bytes, void* hip_stream) {
+    const int rc = check_bias(t, true);
+    if (rc) return rc;
+    if (!t->heads) return PCR_OK;
+    if (!table_grad) return PCR_E_ARG;
+    const BiasPlan P = plan_bias(t);
+    const bool none = !t->batch || !t->queries || !t->keys;
+    if (!none && !d_work) return PCR_E_ARG;
+    if (!none && work_bytes < (size_t)P.shares * t->heads * t->buckets * sizeof(float)) return PCR_E_RANGE;
+    BiasArgs A = bias_args(t);
+    A.part = (float*)d_work; A.share_items = P.share_items; A.held_buckets = P.held; A.waves = P.waves; A.copies = P.copies;
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    bool ok = true;
+    if (!none)
+        with_type(t->dtype, [&](auto v) {
+            const auto kernel = P.held_map ? k_bias_back<decltype(v), true> : k_bias_back<decltype(v), false>;
+            ok = allow_lds(kernel, P.lds);
+            for (int r = 0; ok && r < P.ranges; r++) {
+                A.first_bucket = r * P.held;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares, (unsigned)((t->heads + P.waves - 1) / P.waves)), dim3(P.waves * 64), P.lds, s, A);
+            }
+        });
+    if (!ok) return PCR_E_DEVICE;
+    BiasSums S = {A.part, table_grad, none ? 0 : P.shares, t->heads, t->buckets};
+    hipLaunchKernelGGL(k_bias_sums, dim3((unsigned)std::min<int64_t>((t->heads * t->buckets + 255) / 256, 65536)), dim3(256), 0, s, S);
+    return launched();
+}
+
+int pcr_dropout_add(int device_id, const pcr_dropout* d, void* hip_stream) {
+    if (!d || !known_type(d->dtype) || !known_type(d->out_dtype) || (d->dtype != d->out_dtype && d->dtype != PCR_FLOAT && d->out_dtype != PCR_FLOAT)) return PCR_E_ARG;
+    if (d->rows < 0 || d->dim < 0 || d->call < 0 || d->call > 65535 || !(d->p >= 0.0 && d->p <= 1.0)) return PCR_E_RANGE;
+    if (d->dim && d->rows > (1ll << 50) / d->dim) return PCR_E_RANGE;
+    if (!d->rows || !d->dim) return PCR_OK;
+    if (!d->x || !d->out || !d->seed) return PCR_E_ARG;
+    DropArgs A = {};
+    A.x = d->x; A.residual = d->residual; A.out = d->out; A.seed = d->seed; A.used = d->used;
+    A.count = d->rows * d->dim; A.dim = d->dim; A.x_row = d->x_row; A.residual_row = d->residual_row; A.out_row = d->out_row;
+    const double below = rint(d->p * 4294967296.0);
+    A.below = below >= 4294967296.0 ? 0xffffffffu : (uint32_t)below;
+    A.scale = below >= 4294967296.0 ? 0.f : (float)(1.0 / (1.0 - d->p));
+    A.call = (uint32_t)d->call;
+    const bool flat = d->rows == 1 || (d->x_row == d->dim && d->out_row == d->dim && (!d->residual || d->residual_row == d->dim));
+    // (e / dim by a product is exact as long as both are below 2^32)
+    A.by_dim = A.count < (1ll << 32) && d->dim > 1 ? ~0ull / (uint64_t)d->dim + 1 : 0;
+    const OnDevice on(device_id);
+    if (!on.ok) return PCR_E_DEVICE;
+    auto launch = [&](auto t, auto u) {
+        typedef decltype(t) T;
+        typedef decltype(u) U;
+        in_ranges((A.count + 256 * kDropRun - 1) / (256 * kDropRun), 256, [&](int64_t begin, unsigned groups) {
+            A.begin = begin * 256;
+            if (flat) hipLaunchKernelGGL((k_dropout<T, U, true>), dim3(groups), dim3(256), 0, (hipStream_t)hip_stream, A);
+            else hipLaunchKernelGGL((k_dropout<T, U, false>), dim3(groups), dim3(256), 0, (hipStream_t)hip_stream, A);
+        });
+    };
+    with_type(d->dtype, [&](auto t) {
+        if (d->out_dtype == d->dtype) launch(t, t);
+        else with_type(d->out_dtype, [&](auto u) {
+            if constexpr ((sizeof(t) == 4) != (sizeof(u) == 4)) launch(t, u);
+        });
+    });
+    return launched();
+}
+
+}  // extern "C"

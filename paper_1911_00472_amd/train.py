@@ -1,10 +1,11 @@
 """The operators between a decoded record and a transformer that trains on it (include/pcr.h): patch rows and their positions, positions
-of several axes turned into queries and keys (alone or behind a norm of every head), and distillation from a teacher's top logits.
+of several axes turned into queries and keys (alone or behind a norm of every head), and distillation from a teacher's top logits; and layers of a network that
+trains on the pictures: group norm with an activation, a bias of attention for relative positions, dropout.
 
 The work is done by the library's HIP kernels, enqueued on the current stream (or `stream`, a hipStream_t as an integer); arguments are checked and handed on
 by the native module _train (csrc/pcr_bind.cpp).  A tensor on another stream than the one it was made on needs the caller's
 record_stream, as with any operator.  Wrong types, shapes or devices raise ValueError before anything is enqueued, what the library
-refuses raises PcrError.  rotate_axes, norm_rotate and distill_loss take part in automatic differentiation; a gradient is made on the stream of its forward pass.
+refuses raises PcrError.  rotate_axes, norm_rotate, distill_loss, group_norm, position_bias and dropout take part in automatic differentiation; a gradient is made on the stream of its forward pass.
 There are no derivatives of forward mode (ValueError), and no traces (RuntimeError)."""
 import os
 
@@ -180,3 +181,153 @@ class _DistillLoss(torch.autograd.Function):
 def distill_loss(logits, top_index, top_logits, labels=None, temperature=1.0, distill_part=1.0, label_part=0.0):
     """distill_forward's loss of every row (float32 [rows]), differentiable in the logits."""
     return _DistillLoss.apply(logits, top_index, top_logits, labels, temperature, distill_part, label_part)
+
+
+# ---- group norm ----
+
+_ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+def _activation(name):
+    if not isinstance(name, (str, type(None))) or name not in _ACTIVATIONS:
+        raise ValueError("activation: none, relu, silu or gelu is wanted")
+    return _ACTIVATIONS[name]
+
+
+def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, activation=None, out=None, stream=None):
+    """(y, stats) of feature maps x [images, ..., channels], channels last: activation((x - m) * weight / sqrt(var + eps) + bias), mean m and variance over the
+    pixels of an image and the channels of a group.  Weight and bias: [channels] of float32 or of x's type, or None.  activation: None, "relu", "silu" or "gelu" (with the
+    error function).  Pixels of any one stride (a slice of channels, too); a tensor [images, channels, height, width] in channels-last memory comes as x.permute(0, 2, 3, 1).
+    stats: float32 [images, groups, 2], m and 1 / sqrt(var + eps), which group_norm_backward takes.  out: where y goes (x itself, too)."""
+    return _call(stream, _train.group_norm_forward, x, groups, weight, bias, eps, _activation(activation), out)
+
+
+def group_norm_backward(grad, x, groups, weight, bias, stats, activation=None, dx=None, stream=None):
+    """Gradient of group_norm from its stats: (dx, dweight, dbias), the last two in float32 (None where there is no weight or bias), summed in a fixed order.  dx: where to
+    (grad or x themselves, too)."""
+    return _call(stream, _train.group_norm_backward, grad, x, groups, weight, bias, stats, _activation(activation), dx)
+
+
+class _GroupNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, groups, weight, bias, eps, activation):
+        y, stats = _train.group_norm_forward(x, groups, weight, bias, eps, activation, None)
+        ctx.save_for_backward(x, weight, bias, stats)
+        ctx.how = groups, activation
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        x, weight, bias, stats = ctx.saved_tensors
+        groups, activation = ctx.how
+        dx, dw, db = _train.group_norm_backward(g.contiguous(), x, groups, weight, bias, stats, activation, None)
+        return dx, None, dw.to(weight.dtype) if dw is not None else None, db.to(bias.dtype) if db is not None else None, None, None
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation=None, stream=None):
+    """group_norm_forward's y, differentiable in x, weight and bias."""
+    if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(weight, "requires_grad", False) or getattr(bias, "requires_grad", False)):
+        return _call(stream, _GroupNorm.apply, x, groups, weight, bias, eps, _activation(activation))
+    return group_norm_forward(x, groups, weight, bias, eps, activation, stream=stream)[0]
+
+
+# ---- position bias ----
+
+def position_buckets(exact, coarse=0, far=0, one_sided=False, device=0):
+    """(buckets int32 [axes, 2 * reach + 1], their number) for position_bias.  On either side of an axis the distances below `exact` (0 among them) have a bucket each, those
+    from `exact` to `far` share `coarse` buckets whose widths grow by a constant factor, and the last bucket takes all that is farther; one_sided: keys ahead of their query
+    count as distance 0.  An axis' buckets follow each other from the farthest behind to the farthest ahead (one_sided: from distance 0 on), and those of several axes
+    are combined with the last axis' together.  exact, coarse, far: numbers, or one for each axis: position_buckets((8, 8)) gives a bucket to every difference in a
+    window of 8 x 8, position_buckets(8, 8, 128) is 31 buckets for one line of tokens."""
+    axes = max(len(v) if isinstance(v, (tuple, list)) else 1 for v in (exact, coarse, far))
+    exact, coarse, far = ([int(n) for n in v] if isinstance(v, (tuple, list)) else [int(v)] * axes for v in (exact, coarse, far))
+    if not len(exact) == len(coarse) == len(far) == axes or not 1 <= axes <= 4:
+        raise ValueError("exact, coarse, far: one to four axes are wanted, a value for each")
+    if any(e < 1 or c < 0 or (c and f <= e) for e, c, f in zip(exact, coarse, far)):
+        raise ValueError("exact at least 1, coarse at least 0, and far above exact where there are coarse buckets, are wanted")
+    reach = max(f if c else e - 1 for e, c, f in zip(exact, coarse, far))
+    rows, count = [], 1
+    for e, c, f in reversed(list(zip(exact, coarse, far))):
+        # bucket e + j of a side begins at the first distance x of x^c >= e^(c - j) f^j
+        side, j = [], 0
+        for x in range(reach + 1):
+            while j + 1 < c and x ** c >= e ** (c - j - 1) * f ** (j + 1):
+                j += 1
+            side.append(x if x < e else e + j if c else e - 1)
+        last = e + c - 1
+        row = side[:0:-1] + [0] * (reach + 1) if one_sided else [last - b for b in side[:0:-1]] + [last + b for b in side]
+        rows.append(np.asarray(row, np.int64) * count)
+        count *= e + c if one_sided else 2 * last + 1
+    if count > 2 ** 24:
+        raise ValueError("more than 2^24 buckets")
+    dev = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+    return torch.from_numpy(np.stack(rows[::-1]).astype(np.int32)).to(dev), count
+
+
+class _PositionBias(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, positions, buckets, key_positions, segments, key_segments, dtype):
+        ctx.save_for_backward(positions, buckets, key_positions, segments, key_segments)
+        ctx.table = table.shape[0], table.dtype
+        return _train.position_bias(table, positions, buckets, key_positions, segments, key_segments, dtype, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        positions, buckets, key_positions, segments, key_segments = ctx.saved_tensors
+        count, dtype = ctx.table
+        return (_train.position_bias_backward(_dense(g), positions, buckets, count, key_positions, segments, key_segments).to(dtype),) + (None,) * 6
+
+
+def position_bias(table, positions, buckets, key_positions=None, segments=None, key_segments=None, dtype=None, out=None, stream=None):
+    """A learned bias of attention for relative positions: [heads, queries, keys], or [batch, heads, queries, keys] where positions or segments are of several sequences.  table:
+    [buckets, heads] of float32 or of the result's type (dtype, or the table's); positions (and key_positions, where keys are not the queries' tokens: a single new
+    token against all before it): integers [axes, tokens] or [axes, batch, tokens], as patch_rows gives them; buckets: int32 [axes, 2 * reach + 1] (position_buckets).
+    The pair's bucket is the sum over the axes of buckets[axis, reach + difference], the difference key - query held between -reach and reach; outside of the table it has no
+    bias (0).  segments (and key_segments): int32 [tokens] or [batch, tokens], which of several packed sequences a token is of: pairs of different segments are -inf, rows
+    of queries whose segment is below 0 (padding) are 0.  out: where to, keys contiguous (rows may be padded); given, it keeps the call out of automatic differentiation."""
+    kind = -1 if dtype is None else _TYPES.get(dtype, 3)
+    if out is None and torch.is_grad_enabled() and getattr(table, "requires_grad", False):
+        return _call(stream, _PositionBias.apply, table, positions, buckets, key_positions, segments, key_segments, kind)
+    return _call(stream, _train.position_bias, table, positions, buckets, key_positions, segments, key_segments, kind, out)
+
+
+def position_bias_backward(grad, positions, buckets, count, key_positions=None, segments=None, key_segments=None, stream=None):
+    """Gradient of position_bias's table: float32 [count, heads], the sum of grad over the pairs of each bucket, in a fixed order.  What grad holds of pairs without a
+    bias (of different segments, of padding) is not looked at."""
+    return _call(stream, _train.position_bias_backward, grad, positions, buckets, count, key_positions, segments, key_segments)
+
+
+# ---- dropout ----
+
+def dropout_backward(grad, p, seed, call=0, dtype=None, out=None, stream=None):
+    """Gradient of x of dropout(x, p, seed, call): grad, of the result's type, where x was kept, over the probability of that; of `dtype`, x's type (None: grad's)."""
+    return _call(stream, _train.dropout, grad, p, seed, call, None, -1 if dtype is None else _TYPES.get(dtype, 3), out, False)[0]
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, call, residual):
+        y, used = _train.dropout(x, p, seed, call, residual, -1, None, True)
+        ctx.save_for_backward(used)
+        ctx.how = p, call, _TYPES[x.dtype]
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        p, call, kind = ctx.how
+        dx = _train.dropout(g.contiguous(), p, ctx.saved_tensors[0], call, None, kind, None, False)[0] if ctx.needs_input_grad[0] else None
+        return dx, None, None, None, g if ctx.needs_input_grad[4] else None
+
+
+def dropout(x, p, seed, call=0, residual=None, out=None, stream=None):
+    """residual + x / (1 - p) where x is kept, residual (or 0) where it is dropped, each element with probability p; of residual's type, which is x's or float32.  No mask is
+    stored: element e of x (in the order of its indexes) is dropped by word e of a counter-based generator (Philox4x32-10; include/pcr.h has the counters) for seed, an
+    int64 CUDA tensor [2] of key and step, and call, 0 .. 65535, which tells the dropouts of one step apart.  The seed is read when the work runs (a captured graph may count
+    its step up), and kept as it was read for the gradient.  x, residual: [..., dim], rows at one stride.  out: where to (x or residual themselves, too); given, it
+    keeps the call out of automatic differentiation."""
+    if out is None and torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(residual, "requires_grad", False)):
+        return _call(stream, _Dropout.apply, x, p, seed, call, residual)
+    return _call(stream, _train.dropout, x, p, seed, call, residual, -1, out, False)[0]

@@ -1,0 +1,301 @@
+"""The bias for relative positions and its table's gradient against the definition.
+
+The bias is a value of the table in the result's type, or 0 or -inf: equal.  The gradient's sums are made in 32 bits over a share of the pairs, at most 2^10 additions
+after each other of at most half a unit, 2^-24, each: 2^-14 of the sum of the magnitudes; the shares are added in 64 bits and rounded once."""
+import pytest
+import torch
+
+import paper_1911_00472_amd as pkg
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def generator(seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return gen
+
+
+def pairs(positions, key_positions, buckets, count, segments=None, key_segments=None):
+    """On the host: (bucket [B, Q, K], count where there is none; whether the pair is of different segments)."""
+    def batched(p):
+        return p.cpu().long() if p.dim() == 3 else p.cpu().long()[:, None]
+    q, k, m = batched(positions), batched(key_positions), buckets.cpu()
+    reach = m.shape[1] // 2
+    difference = [(k[a].double()[:, None, :] - q[a].double()[:, :, None]).clamp(-reach, reach).long() for a in range(m.shape[0])]
+    bucket = sum(m[a][d + reach].long() for a, d in enumerate(difference))
+    bucket = torch.where((bucket >= 0) & (bucket < count), bucket, count)
+    apart = torch.zeros_like(bucket, dtype=torch.bool)
+    if segments is not None:
+        s, t = (x.cpu() if x.dim() == 2 else x.cpu()[None] for x in (segments, key_segments))
+        apart = (s[:, :, None] != t[:, None, :]) & (s >= 0)[:, :, None]
+        bucket = torch.where((s < 0)[:, :, None], count, bucket)
+        bucket, apart = torch.broadcast_tensors(bucket, apart)
+    return bucket, apart
+
+
+def bias(table, dtype, bucket, apart):
+    rows = torch.cat([table.cpu().to(dtype), torch.zeros((1, table.shape[1]), dtype=dtype)])
+    y = rows[bucket].permute(0, 3, 1, 2)
+    return torch.where(apart[:, None], torch.tensor(-float("inf"), dtype=dtype), y)
+
+
+def check_gradient(got, g, bucket, apart, count):
+    H = g.shape[1]
+    use = (bucket < count) & ~apart
+    use, bucket = (x.expand(g.shape[0], -1, -1) for x in (use, bucket))
+    want, size = (torch.zeros((count, H), dtype=torch.float64) for _ in range(2))
+    for h in range(H):
+        v, b = g[:, h].double().cpu()[use], bucket[use]
+        want[:, h].index_add_(0, b, v)
+        size[:, h].index_add_(0, b, v.abs())
+    off = (got.double().cpu() - want).abs()
+    assert got.shape == want.shape and got.dtype == torch.float32
+    assert bool((off <= 2.0 ** -14 * size + 2.0 ** -24 * want.abs() + 2.0 ** -126).all()), float((off - 2.0 ** -14 * size).max())
+
+
+def packed(B, T, gen, pictures=3, padding=True):
+    """Segments of T tokens: a few runs, the last of them padding."""
+    cuts = torch.randint(0, T + 1, (B, pictures), generator=gen, device="cuda").sort(1).values
+    s = (torch.arange(T, device="cuda")[None, :, None] >= cuts[:, None, :]).sum(-1).int()
+    return torch.where(s == pictures, -1, s).int() if padding else s
+
+
+SETTINGS = [  # batch, queries, keys, heads, buckets (exact, coarse, far, one_sided), segments
+    (None, 1, 1, 1, (1,), False), (None, 1, 1, 1, ((2, 2),), True), (2, 1, 700, 16, (16, 16, 128, True), False), (3, 5, 5, 3, ((4, 4),), True), (1, 64, 64, 6, ((8, 8),), False),
+    (None, 33, 17, 12, (8, 8, 128), True), (2, 129, 131, 5, ((3, 7, 7), 0, 0), True), (1, 200, 199, 25, ((5, 9), (3, 0), (40, 0)), False), (4, 3, 1030, 7, (9, 15, 800), True),
+    (None, 300, 300, 2, ((32, 32),), True), (1, 70, 513, 9, ((20, 20), (4, 4), (90, 95)), False), (70, 2, 9, 4, ((2, 2, 2, 2),), False), (2, 40, 40, 33, (3,), True),
+    (None, 90, 88, 1, ((60, 60),), False), (1, 17, 4000, 3, (2, 1, 4), False),
+]
+
+
+def setting(B, Q, K, axes, with_segments, gen, far, kind=torch.int32):
+    shape = lambda n: (axes, n) if B is None else (axes, B, n)  # noqa: E731
+    q, k = (torch.randint(-far, far + 1, shape(n), generator=gen, device="cuda", dtype=kind) for n in (Q, K))
+    s = t = None
+    if with_segments:
+        s, t = packed(B or 1, Q, gen), packed(B or 1, K, gen)
+        if B is None:
+            s, t = s[0], t[0]
+    return q, k, s, t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,Q,K,H,how,segments", SETTINGS)
+def test_bias_and_gradient(B, Q, K, H, how, segments, dtype):
+    gen = generator(Q + K)
+    buckets, count = pkg.position_buckets(*how)
+    q, k, s, t = setting(B, Q, K, buckets.shape[0], segments, gen, buckets.shape[1] // 2 + 3)
+    places = dict(key_positions=k, segments=s, key_segments=t)
+    bucket, apart = pairs(q, k, buckets, count, s, t)
+    for table_type in {dtype, torch.float32}:
+        table = torch.randn((count, H), generator=gen, device="cuda").to(table_type)
+        y = pkg.position_bias(table, q, buckets, dtype=dtype, **places)
+        want = bias(table, dtype, bucket, apart)
+        assert torch.equal(y.cpu(), want if B is not None else want[0])
+    g = torch.randn(y.shape, generator=gen, device="cuda").to(dtype)
+    got = pkg.position_bias_backward(g, q, buckets, count, **places)
+    check_gradient(got, g if B is not None else g[None], bucket, apart, count)
+    assert torch.equal(got, pkg.position_bias_backward(g, q, buckets, count, **places))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("count,reach", [(5000, 300), (9000, 10), (40000, 2000), (20, 9000), (100, 20000), (7, 60000)])
+def test_long_tables_and_maps(count, reach, dtype):
+    """Tables and maps that do not fit beside each other, whose buckets go in any order, with some outside of the table."""
+    gen = generator(count)
+    buckets = torch.randint(0, count, (1, 2 * reach + 1), generator=gen, device="cuda", dtype=torch.int32)
+    buckets[0, ::7], buckets[0, 1::7] = -1, count
+    q, k = (torch.randint(-reach, reach, (1, n), generator=gen, device="cuda") for n in (150, 222))
+    bucket, apart = pairs(q, k, buckets, count)
+    assert bool((bucket == count).any())
+    table = torch.randn((count, 5), generator=gen, device="cuda").to(dtype)
+    assert torch.equal(pkg.position_bias(table, q, buckets, k).cpu(), bias(table, dtype, bucket, apart)[0])
+    g = torch.randn((5, 150, 222), generator=gen, device="cuda").to(dtype)
+    check_gradient(pkg.position_bias_backward(g, q, buckets, count, k), g[None], bucket, apart, count)
+
+
+def test_axes_add_as_32_bit_integers_and_may_miss_the_table():
+    buckets = torch.tensor([[-1, 0, 2], [2 ** 31 - 1, 1, -2 ** 31]], dtype=torch.int32, device="cuda")
+    positions = torch.tensor([[0, 1, 0], [0, 0, 1]], device="cuda")
+    table = torch.randn((4, 2), device="cuda")
+    y = pkg.position_bias(table, positions, buckets)
+    q = positions.cpu()
+    for i in range(3):
+        for j in range(3):
+            d = [int(q[a, j] - q[a, i]) for a in range(2)]
+            b = sum(int(buckets[a, 1 + d[a]]) for a in range(2))
+            b = (b + 2 ** 31) % 2 ** 32 - 2 ** 31
+            assert torch.equal(y[:, i, j], table[b] if 0 <= b < 4 else torch.zeros(2, device="cuda")), (i, j)
+
+
+@pytest.mark.parametrize("kind", [torch.int32, torch.int64])
+def test_far_positions(kind):
+    """Differences that pass the positions' type are held at the reach."""
+    low, high = (-2 ** 31, 2 ** 31 - 1) if kind == torch.int32 else (-2 ** 63, 2 ** 63 - 1)
+    p = torch.tensor([[low, low + 1, -5, 0, 5, high - 1, high]], dtype=kind, device="cuda")
+    buckets, count = pkg.position_buckets(7)
+    table = torch.randn((count, 3), device="cuda")
+    y = pkg.position_bias(table, p, buckets).cpu()
+    values = p[0].tolist()
+    for i, a in enumerate(values):
+        for j, b in enumerate(values):
+            assert torch.equal(y[:, i, j], table[6 + max(-6, min(6, b - a))].cpu()), (a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides(dtype):
+    """Positions, segments, results and gradients that lie in other ways than behind each other."""
+    gen = generator(11)
+    B, Q, K, H = 3, 21, 37, 6
+    buckets, count = pkg.position_buckets((5, 5))
+    q, k, s, t = setting(B, Q, K, 2, True, gen, 6)
+    table = torch.randn((count, H), generator=gen, device="cuda").to(dtype)
+    want = pkg.position_bias(table, q, buckets, k, s, t)
+    turned = [x.permute(2, 1, 0).contiguous().permute(2, 1, 0) for x in (q, k)] + [x.T.contiguous().T for x in (s, t)]
+    assert torch.equal(pkg.position_bias(table, turned[0], buckets, *turned[1:]), want)
+    for room in (torch.full((B, H, Q, K + 3), 7.0, device="cuda", dtype=dtype), torch.full((Q, B, H, K + 8), 7.0, device="cuda", dtype=dtype).permute(1, 2, 0, 3)):
+        out = room[..., :K]
+        assert pkg.position_bias(table, q, buckets, k, s, t, out=out) is out
+        assert torch.equal(out, want) and bool((room[..., K:] == 7).all())
+    g = torch.randn((Q, H, B, K + 1), generator=gen, device="cuda").to(dtype).permute(2, 1, 0, 3)[..., 1:]
+    bucket, apart = pairs(q, k, buckets, count, s, t)
+    check_gradient(pkg.position_bias_backward(g, q, buckets, count, k, s, t), g, bucket, apart, count)
+    one = torch.randn((1, 1, 1, K), generator=gen, device="cuda").to(dtype).expand(B, H, Q, K)
+    check_gradient(pkg.position_bias_backward(one, turned[0], buckets, count, *turned[1:]), one, bucket, apart, count)
+
+
+def test_sequences_share_positions_or_segments():
+    gen = generator(12)
+    buckets, count = pkg.position_buckets(6)
+    table = torch.randn((count, 4), generator=gen, device="cuda")
+    p, s = torch.arange(30, device="cuda")[None], packed(3, 30, gen)
+    y = pkg.position_bias(table, p, buckets, segments=s)                       # positions of all, segments of each
+    assert y.shape == (3, 4, 30, 30)
+    for b in range(3):
+        assert torch.equal(y[b], pkg.position_bias(table, p, buckets, segments=s[b]))
+    k = torch.randint(0, 30, (1, 3, 50), generator=gen, device="cuda")
+    y = pkg.position_bias(table, p, buckets, key_positions=k)                  # queries of all, keys of each
+    for b in range(3):
+        assert torch.equal(y[b], pkg.position_bias(table, p, buckets, key_positions=k[:, b]))
+    g = torch.randn(y.shape, generator=gen, device="cuda")
+    bucket, apart = pairs(p, k, buckets, count)
+    check_gradient(pkg.position_bias_backward(g, p, buckets, count, k), g, bucket, apart, count)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_pairs_without_a_bias_are_not_looked_at(dtype):
+    gen = generator(13)
+    buckets, count = pkg.position_buckets((4, 4))
+    q, k, s, t = setting(2, 60, 61, 2, True, gen, 5)
+    bucket, apart = pairs(q, k, buckets, count, s, t)
+    g = torch.randn((2, 5, 60, 61), generator=gen, device="cuda").to(dtype)
+    want = pkg.position_bias_backward(g, q, buckets, count, k, s, t)
+    nowhere = (apart | (bucket == count)).cuda()[:, None].expand_as(g)
+    for v in (float("nan"), float("inf"), torch.finfo(dtype).min):
+        assert torch.equal(pkg.position_bias_backward(g.masked_fill(nowhere, v), q, buckets, count, k, s, t), want)
+    one = g.clone()
+    i = (~nowhere[1, 3]).nonzero()[0]
+    one[1, 3, i[0], i[1]] = float("nan")                       # ... and of the others everything
+    got = pkg.position_bias_backward(one, q, buckets, count, k, s, t)
+    at = int(bucket[1, i[0], i[1]])
+    assert bool(got[at, 3].isnan()) and int(got.isnan().sum()) == 1
+
+
+def test_no_tokens_and_no_heads():
+    buckets, count = pkg.position_buckets(4)
+    for q, k, h in ((0, 5, 2), (5, 0, 2), (3, 3, 0)):
+        a, b = (torch.arange(n, device="cuda")[None] for n in (q, k))
+        table = torch.randn((count, h), device="cuda", requires_grad=True)
+        y = pkg.position_bias(table, a, buckets, b)
+        assert y.shape == (h, q, k)
+        y.sum().backward()
+        assert table.grad.shape == table.shape and not table.grad.any()
+    p = torch.zeros((1, 0, 4), dtype=torch.int32, device="cuda")
+    assert pkg.position_bias(table, p, buckets).shape == (0, 0, 4, 4)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_differentiation(dtype):
+    gen = generator(14)
+    buckets, count = pkg.position_buckets(5, 3, 20)
+    table = torch.randn((count, 4), generator=gen, device="cuda").to(dtype).requires_grad_()
+    p = torch.arange(50, device="cuda")[None]
+    y = pkg.position_bias(table, p, buckets)
+    g = torch.randn((50, 50, 4), generator=gen, device="cuda").to(dtype).permute(2, 0, 1)
+    y.backward(g)
+    assert torch.equal(table.grad, pkg.position_bias_backward(g.contiguous(), p, buckets, count).to(dtype))
+    table.grad = None
+    pkg.position_bias(table, p, buckets).sum().backward()       # (a gradient whose strides are 0)
+    bucket, apart = pairs(p, p, buckets, count)
+    number = torch.stack([(bucket == b).sum() for b in range(count)]).to(dtype)
+    assert torch.equal(table.grad.cpu(), number[:, None].expand(-1, 4))
+    # by differences: a step of one entry moves as many results as it has pairs
+    for b in (0, 3, count - 1):
+        step = torch.zeros((count, 4), device="cuda", dtype=dtype)
+        step[b, 2] = 1.0
+        assert float(pkg.position_bias(step, p, buckets).float().sum()) == float((bucket == b).sum())
+
+
+def test_captured_and_replayed():
+    gen = generator(15)
+    buckets, count = pkg.position_buckets((16, 16))
+    p, s = torch.randint(0, 20, (2, 2, 100), generator=gen, device="cuda"), packed(2, 100, gen)
+    table, g = torch.randn((count, 5), generator=gen, device="cuda"), torch.randn((2, 5, 100, 100), generator=gen, device="cuda")
+    pkg.position_bias_backward(g, p, buckets, count, segments=s)
+    pkg.position_bias(table, p, buckets, segments=s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = pkg.position_bias(table, p, buckets, segments=s)
+        d = pkg.position_bias_backward(g, p, buckets, count, segments=s)
+    for seed in range(4):
+        new = generator(20 + seed)
+        table.copy_(torch.randn(table.shape, generator=new, device="cuda"))
+        g.copy_(torch.randn(g.shape, generator=new, device="cuda"))
+        p.copy_(torch.randint(0, 20, p.shape, generator=new, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone(), d.clone()
+        assert torch.equal(got[0], pkg.position_bias(table, p, buckets, segments=s)) and torch.equal(got[1], pkg.position_bias_backward(g, p, buckets, count, segments=s))
+
+
+def test_results_behind_2_to_the_32_elements():
+    """Offsets of 64 bits, in values and their gradient: 25 heads over 14000 tokens."""
+    T, H = 14000, 25
+    buckets, count = pkg.position_buckets(4, 4, 64)
+    p = torch.arange(T, device="cuda", dtype=torch.int32)[None]
+    table = torch.randn((count, H), device="cuda").half()
+    y = pkg.position_bias(table, p, buckets)
+    for i in (0, 5000, T - 1):
+        at = buckets[0].long()[(p[0].long() - i).clamp(-64, 64) + 64]
+        assert torch.equal(y[:, i], table[at].T)
+    y.fill_(1.0)
+    n = (T - torch.arange(T, device="cuda")).long()
+    want = torch.zeros(count, dtype=torch.float64, device="cuda")
+    for d in (0, 1, 2, 3):                                     # the exact ones
+        want[7 + d] = want[7 - d] = n[d]
+    got = pkg.position_bias_backward(y, p, buckets, count)
+    exact = slice(4, 11)
+    assert torch.equal(got[exact].double(), want[exact, None].expand(-1, H))
+    assert abs(float(got.double().sum()) / (T * T * H) - 1) < 2.0 ** -14
+
+
+def test_refusals():
+    buckets, count = pkg.position_buckets((4, 4))
+    p, s, table = torch.zeros((2, 10), dtype=torch.int32, device="cuda"), torch.zeros(10, dtype=torch.int32, device="cuda"), torch.randn((count, 3), device="cuda")
+    g = torch.randn((3, 10, 10), device="cuda")
+    f, b = pkg.position_bias, pkg.position_bias_backward
+    for call in (lambda: f(table, p.cpu(), buckets), lambda: f(table.cpu(), p, buckets), lambda: f(table, p, buckets.cpu()), lambda: f(table, p.float(), buckets), lambda: f(table, p[:1], buckets),
+                 lambda: f(table, p[0], buckets), lambda: f(table, p, buckets.long()), lambda: f(table, p, buckets[:, 1:].contiguous()), lambda: f(table, p, buckets.T.contiguous().T),
+                 lambda: f(table[0], p, buckets), lambda: f(table.T.contiguous().T, p, buckets), lambda: f(table.double(), p, buckets), lambda: f(table.half(), p, buckets, dtype=torch.float32),
+                 lambda: f(table, p, buckets, dtype=torch.float64), lambda: f(table, p, buckets, p.long()), lambda: f(table, p, buckets, segments=s[:5]), lambda: f(table, p, buckets, segments=s.long()),
+                 lambda: f(table, p, buckets, key_segments=s), lambda: f(table, p, buckets, p, segments=s), lambda: f(table, p, buckets, segments=s.expand(3, 10), key_positions=p[:, None].expand(2, 4, 10)),
+                 lambda: f(table, p, buckets, out=g[:2]), lambda: f(table, p, buckets, out=g.transpose(1, 2)), lambda: f(table, p, buckets, out=g[:, :1].expand(3, 10, 10)), lambda: f(table, p, buckets, out=g[None]),
+                 lambda: f(table, p, buckets, out=g.clone().requires_grad_()), lambda: f(table.bfloat16(), p, buckets, out=g), lambda: f(table[:0], p, buckets),
+                 lambda: b(g, p, buckets, 0), lambda: b(g, p, buckets, 2 ** 24 + 1), lambda: b(g[:, :9], p, buckets, count), lambda: b(g.transpose(1, 2), p, buckets, count),
+                 lambda: b(g.double(), p, buckets, count), lambda: b(g[None], p, buckets, count), lambda: b(None, p, buckets, count),
+                 lambda: f(table, torch.zeros((5, 10), dtype=torch.int32, device="cuda"), torch.zeros((5, 3), dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
