@@ -79,7 +79,7 @@ template <typename F> void with_run(int dtype, int run, F f) {
 
 // ---- position bias ----
 
-constexpr int kBiasLds = 144 * 1024;                           // of a workgroup, at most
+constexpr int64_t kBiasLds = 152 * 1024;                         // of a workgroup, at most
 
 int check_bias(const pcr_position_table* t, bool back) {
     if (!t || !known_type(t->dtype)) return PCR_E_ARG;
@@ -120,27 +120,34 @@ struct BiasPlan { int waves, copies, ranges; int64_t held, shares, share_items; 
 BiasPlan plan_bias(const pcr_position_table* t) {
     BiasPlan P = {};
     const BiasArgs A = bias_args(t);
-    const int V = 16 / (int)type_size(t->dtype);
+    const int64_t V = 16 / (int64_t)type_size(t->dtype);
     const int64_t map_bytes = (int64_t)t->axes * (2 * t->reach + 1) * 4;
     P.held_map = map_bytes <= 32 * 1024;
-    P.held = std::min<int64_t>(t->buckets, 8192);
-    P.ranges = (int)((t->buckets + P.held - 1) / P.held);
+    P.ranges = (int)((t->buckets + 4095) / 4096);
+    P.held = (t->buckets + P.ranges - 1) / P.ranges;
+    const int64_t held = (P.held + 7) / 8 * 8, elements = std::max<int64_t>(1, A.items * V);
+    auto bytes = [&](int64_t w, int64_t copies) {
+        const int64_t tile = t->dtype == PCR_FLOAT ? BackTile<float>::bytes((int)w) : BackTile<__bf16>::bytes((int)w);
+        return 2 * tile + w * (held * copies + 64) * 8 + (P.held_map ? map_bytes : 0);
+    };
+    // Few elements: one share.
+    const int64_t few = 16384;
+    const int64_t most_shares = elements <= few ? 1 : std::max<int64_t>(1, elements / std::max<int64_t>(4 * held, 4096));
     P.copies = 64;
-    while (P.copies > 1 && P.held * P.copies > 4096) P.copies >>= 1;
-    const int64_t bins = P.held * P.copies;
-    auto bytes = [&](int64_t w) { return w * 64 * (2 * V + V) + 32 + w * bins * 4 + (P.copies < 64 ? (w * bins + 15) / 16 * 16 : 0) + (P.held_map ? map_bytes : 0); };
-    const int64_t blocks = (t->heads + 7) / 8;
-    P.waves = (int)std::max<int64_t>(1, (t->heads + std::max<int64_t>(1, blocks) - 1) / std::max<int64_t>(1, blocks));
-    while (P.waves > 1 && bytes(P.waves) > 80 * 1024) P.waves--;
-    P.lds = (size_t)bytes(P.waves);
+    while (P.copies > 1 && held * P.copies > std::max(held, std::min<int64_t>(1024, elements / most_shares / 2))) P.copies >>= 1;
+    const int64_t blocks = std::max<int64_t>(1, (t->heads + kBackWaves - 1) / kBackWaves);
+    P.waves = (int)std::max<int64_t>(1, (t->heads + blocks - 1) / blocks);
+    while (P.waves > 1 && bytes(P.waves, P.copies) > kBiasLds) P.waves--;
+    P.lds = (size_t)bytes(P.waves, P.copies);
     const int64_t head_blocks = std::max<int64_t>(1, (t->heads + P.waves - 1) / P.waves);
-    const int64_t tile = P.waves * 64;
-    P.shares = std::max<int64_t>(1, std::min<int64_t>((A.items + tile - 1) / tile, (1024 + head_blocks - 1) / head_blocks));
+    const int64_t resident = 256 * std::max<int64_t>(1, std::min<int64_t>(16 / P.waves, (int64_t)(160 * 1024 / P.lds)));
+    P.shares = std::max<int64_t>(1, std::min<int64_t>(most_shares, resident / (head_blocks * P.ranges)));
     P.share_items = (A.items + P.shares - 1) / P.shares;
     P.share_items = (P.share_items + 63) / 64 * 64;
     P.shares = P.share_items ? std::max<int64_t>(1, (A.items + P.share_items - 1) / P.share_items) : 1;
     return P;
 }
+size_t bias_work(const pcr_position_table* t, const BiasPlan& P) { return P.shares == 1 ? 0 : (size_t)P.shares * t->heads * t->buckets * sizeof(float); }
 
 template <typename K> bool allow_lds(K kernel, size_t bytes) {
     return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
@@ -254,7 +261,7 @@ int pcr_position_bias_workspace(const pcr_position_table* t, size_t* nbytes) {
     const int rc = check_bias(t, true);
     if (rc) return rc;
     const BiasPlan P = plan_bias(t);
-    *nbytes = (size_t)P.shares * t->heads * t->buckets * sizeof(float);
+    *nbytes = bias_work(t, P);
     return PCR_OK;
 }
 
@@ -265,10 +272,12 @@ int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float
     if (!table_grad) return PCR_E_ARG;
     const BiasPlan P = plan_bias(t);
     const bool none = !t->batch || !t->queries || !t->keys;
-    if (!none && !d_work) return PCR_E_ARG;
-    if (!none && work_bytes < (size_t)P.shares * t->heads * t->buckets * sizeof(float)) return PCR_E_RANGE;
+    const bool direct = !none && P.shares == 1;
+    if (!none && !direct && !d_work) return PCR_E_ARG;
+    if (!none && !direct && work_bytes < bias_work(t, P)) return PCR_E_RANGE;
     BiasArgs A = bias_args(t);
-    A.part = (float*)d_work; A.share_items = P.share_items; A.held_buckets = P.held; A.waves = P.waves; A.copies = P.copies;
+    if (!none) set_step(A, P.waves * 64);
+    A.direct = direct; A.part = direct ? table_grad : (float*)d_work; A.share_items = P.share_items; A.held_buckets = P.held; A.waves = P.waves; A.copies = P.copies;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
     const hipStream_t s = (hipStream_t)hip_stream;
@@ -277,14 +286,12 @@ int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float
         with_type(t->dtype, [&](auto v) {
             const auto kernel = P.held_map ? k_bias_back<decltype(v), true> : k_bias_back<decltype(v), false>;
             ok = allow_lds(kernel, P.lds);
-            for (int r = 0; ok && r < P.ranges; r++) {
-                A.first_bucket = r * P.held;
-                hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares, (unsigned)((t->heads + P.waves - 1) / P.waves)), dim3(P.waves * 64), P.lds, s, A);
-            }
+            if (ok) hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares, (unsigned)((t->heads + P.waves - 1) / P.waves), (unsigned)P.ranges), dim3(P.waves * 64), P.lds, s, A);
         });
     if (!ok) return PCR_E_DEVICE;
+    if (direct) return launched();
     BiasSums S = {A.part, table_grad, none ? 0 : P.shares, t->heads, t->buckets};
-    hipLaunchKernelGGL(k_bias_sums, dim3((unsigned)std::min<int64_t>((t->heads * t->buckets + 255) / 256, 65536)), dim3(256), 0, s, S);
+    hipLaunchKernelGGL(k_bias_sums, dim3((unsigned)((t->heads * t->buckets + 63) / 64)), dim3(1024), 0, s, S);
     return launched();
 }
 

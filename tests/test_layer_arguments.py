@@ -91,10 +91,11 @@ def test_position_bias():
     assert L.pcr_position_bias(0, by(table(table=None)), None) == pkg.E_ARG and L.pcr_position_bias(0, by(table(table_dtype=4)), None) == pkg.E_ARG
     assert L.pcr_position_bias(0, by(table(dtype=1, table_dtype=2)), None) == pkg.E_ARG
     assert L.pcr_position_bias(0, None, None) == pkg.E_ARG and L.pcr_position_bias_workspace(None, by(need)) == pkg.E_ARG and L.pcr_position_bias_workspace(by(table()), None) == pkg.E_ARG
-    assert L.pcr_position_bias_workspace(by(table()), by(need)) == pkg.OK and need.value > 0
-    assert L.pcr_position_bias_backward(0, by(table()), None, at, need.value, None) == pkg.E_ARG
-    assert L.pcr_position_bias_backward(0, by(table()), at, None, need.value, None) == pkg.E_ARG
-    assert L.pcr_position_bias_backward(0, by(table()), at, at, need.value - 1, None) == pkg.E_RANGE
+    long = dict(queries=1000, keys=1000)
+    assert L.pcr_position_bias_workspace(by(table(**long)), by(need)) == pkg.OK and need.value > 0
+    assert L.pcr_position_bias_backward(0, by(table(**long)), None, at, need.value, None) == pkg.E_ARG
+    assert L.pcr_position_bias_backward(0, by(table(**long)), at, None, need.value, None) == pkg.E_ARG
+    assert L.pcr_position_bias_backward(0, by(table(**long)), at, at, need.value - 1, None) == pkg.E_RANGE
     assert L.pcr_position_bias(0, by(table(keys=0, query=Places(), key=Places(), map=None, values=None)), None) == pkg.OK
 
 
