@@ -12,6 +12,8 @@ struct Places {                                                    // of queries
     const void* position; const int32_t* segment;
     int64_t axis, batch, token, segment_batch, segment_token;      // strides
 };
+typedef uint16_t Places8 __attribute__((ext_vector_type(8)));     // of eight keys
+struct Steps { uint32_t run, query, batch; };                      // of an item
 struct BiasArgs {
     Places q, k;
     const int32_t* map; const void* table; void* values;           // values: the bias, or its incoming gradient
@@ -20,7 +22,9 @@ struct BiasArgs {
     int64_t step_batch, step_query, step_run;                      // a thread's step to its next item
     int axes, reach, wide, table_float;
     // gradient
-    float* part; int64_t share_items, held_buckets;  // part: [share][head][bucket]; direct: one share, [bucket][head]
+    float* part; Places8* places; uint64_t* live;                  // part: [share][head][bucket]; direct: one share, [bucket][head]
+    int64_t first_bucket, held_buckets;
+    Steps near, far;                                               // from one item of a lane to the next; from the last of those that are under way together to the first of the next ones
     int waves, copies, direct;
 };
 
@@ -36,10 +40,17 @@ enum : uint32_t { kNoBias = 0, kNeverSeen = 1 };                   // behind the
 struct Item { int64_t b, i, run; };
 __device__ __forceinline__ Item item_at(const BiasArgs& A, int64_t t) {
     Item I;
-    const int64_t row = t / A.runs;
-    I.run = t - row * A.runs;
-    I.b = row / A.queries;
-    I.i = row - I.b * A.queries;
+    if (t >> 32 | A.runs >> 32) {                                  // (a division in 64 bits takes 130 instructions, in 32 bits 25)
+        const int64_t row = t / A.runs;
+        I.run = t - row * A.runs;
+        I.b = row / A.queries;
+        I.i = row - I.b * A.queries;
+    } else {
+        const uint32_t row = (uint32_t)t / (uint32_t)A.runs, b = row / (uint32_t)A.queries;
+        I.run = (uint32_t)t - row * (uint32_t)A.runs;
+        I.b = b;
+        I.i = row - b * (uint32_t)A.queries;
+    }
     return I;
 }
 __device__ __forceinline__ void step_on(Item& I, const BiasArgs& A) {
@@ -52,46 +63,71 @@ __device__ __forceinline__ void step_on(Item& I, const BiasArgs& A) {
 
 template <int V> __device__ __forceinline__ int64_t first_key(const BiasArgs& A, const Item& I) { return min(I.run * V, max(A.keys - V, (int64_t)0)); }
 
-// The buckets of an item's keys; buckets + kNoBias where there is none, buckets + kNeverSeen across segments.  Keys behind the row's end (of rows of fewer than V): of no account.
+// Positions (or segments) of an item's keys.  Keys behind the row's end (of rows of fewer than V): of no account.
+template <typename P, int V> __device__ __forceinline__ void load_places(const P* from, int64_t stride, int here, P without, P (&at)[V]) {
+    if (here == V && stride == 1) {
+#pragma unroll
+        for (int v = 0; v < V; v += 4) {
+            const typename Run<P, 4>::Vec four = reinterpret_cast<const typename Run<P, 4>::Loose*>(from + v)->v;
+#pragma unroll
+            for (int u = 0; u < 4; u++) at[v + u] = four[u];
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; v++) at[v] = v < here ? from[v * stride] : without;
+    }
+}
+// The buckets of an item's keys, less `start`: `none` for one that is not below `limit`, `never` for one of another segment, all `none` for a query that is padding.  AXES: so many 32-bit
+// positions whose keys, V at least, follow each other in memory, as their segments do; 0: any.
 template <typename P, int V> __device__ __forceinline__ void sum_axes(const BiasArgs& A, const int32_t* map, const Item& I, int here, int32_t (&sum)[V]) {
     const int width = 2 * A.reach + 1;
     for (int a = 0; a < A.axes; a++) {
         const P query = ((const P*)A.q.position)[a * A.q.axis + I.b * A.q.batch + I.i * A.q.token];
-        const P* key = (const P*)A.k.position + a * A.k.axis + I.b * A.k.batch + first_key<V>(A, I) * A.k.token;
         P at[V];
-        if (here == V && A.k.token == 1) {
+        load_places<P, V>((const P*)A.k.position + a * A.k.axis + I.b * A.k.batch + first_key<V>(A, I) * A.k.token, A.k.token, here, query, at);
+        const int32_t* middle = map + a * width + A.reach;
 #pragma unroll
-            for (int v = 0; v < V; v += 4) {
-                const typename Run<P, 4>::Vec four = reinterpret_cast<const typename Run<P, 4>::Loose*>(key + v)->v;
-#pragma unroll
-                for (int u = 0; u < 4; u++) at[v + u] = four[u];
-            }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; v++) at[v] = v < here ? key[v * A.k.token] : query;
-        }
-#pragma unroll
-        for (int v = 0; v < V; v++) sum[v] = (int32_t)((uint32_t)sum[v] + (uint32_t)map[a * width + A.reach + apart(at[v], query, A.reach)]);
+        for (int v = 0; v < V; v++) sum[v] = (int32_t)((uint32_t)sum[v] + (uint32_t)middle[apart(at[v], query, A.reach)]);
     }
 }
-template <int V> __device__ __forceinline__ void buckets_of(const BiasArgs& A, const int32_t* map, const Item& I, int here, uint32_t (&bucket)[V]) {
-    int32_t sum[V];
+template <int V, int AXES> __device__ __forceinline__ void buckets_of(const BiasArgs& A, const int32_t* map, const Item& I, int here, uint32_t start, uint32_t limit, uint32_t none,
+                                                                       uint32_t never, uint32_t (&bucket)[V]) {
+    int32_t mine = 0, other[V], sum[V];
 #pragma unroll
-    for (int v = 0; v < V; v++) sum[v] = 0;
-    if (A.wide) sum_axes<int64_t, V>(A, map, I, here, sum);
-    else sum_axes<int32_t, V>(A, map, I, here, sum);
-    const uint32_t count = (uint32_t)A.buckets;
+    for (int v = 0; v < V; v++) sum[v] = (int32_t)(0u - start);
+    if constexpr (AXES > 0) {
+        const int64_t key = first_key<V>(A, I);
+        int32_t query[AXES], at[AXES][V];
 #pragma unroll
-    for (int v = 0; v < V; v++) bucket[v] = (uint32_t)sum[v] < count ? (uint32_t)sum[v] : count + kNoBias;
-    if (A.q.segment) {
-        const int32_t mine = A.q.segment[I.b * A.q.segment_batch + I.i * A.q.segment_token];
-        const int32_t* key = A.k.segment + I.b * A.k.segment_batch + first_key<V>(A, I) * A.k.segment_token;
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            const int32_t other = v < here ? key[v * A.k.segment_token] : mine;
-            if (mine < 0) bucket[v] = count + kNoBias;
-            else if (other != mine) bucket[v] = count + kNeverSeen;
+        for (int a = 0; a < AXES; a++) {
+            query[a] = ((const int32_t*)A.q.position)[a * A.q.axis + I.b * A.q.batch + I.i * A.q.token];
+            load_places<int32_t, V>((const int32_t*)A.k.position + a * A.k.axis + I.b * A.k.batch + key, 1, V, 0, at[a]);
         }
+        if (A.q.segment) {
+            mine = A.q.segment[I.b * A.q.segment_batch + I.i * A.q.segment_token];
+            load_places<int32_t, V>(A.k.segment + I.b * A.k.segment_batch + key, 1, V, 0, other);
+        }
+        const int width = 2 * A.reach + 1;
+#pragma unroll
+        for (int a = 0; a < AXES; a++) {
+            const int32_t* middle = map + a * width + A.reach;
+#pragma unroll
+            for (int v = 0; v < V; v++) sum[v] = (int32_t)((uint32_t)sum[v] + (uint32_t)middle[apart(at[a][v], query[a], A.reach)]);
+        }
+    } else {
+        if (A.wide) sum_axes<int64_t, V>(A, map, I, here, sum);
+        else sum_axes<int32_t, V>(A, map, I, here, sum);
+        if (A.q.segment) {
+            mine = A.q.segment[I.b * A.q.segment_batch + I.i * A.q.segment_token];
+            load_places<int32_t, V>(A.k.segment + I.b * A.k.segment_batch + first_key<V>(A, I) * A.k.segment_token, A.k.segment_token, here, mine, other);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; v++) bucket[v] = (uint32_t)sum[v] < limit ? (uint32_t)sum[v] : none;
+    if (A.q.segment) {
+        if (mine < 0) never = none;
+#pragma unroll
+        for (int v = 0; v < V; v++) bucket[v] = mine >= 0 && other[v] == mine ? bucket[v] : never;
     }
 }
 
@@ -101,7 +137,7 @@ template <typename T> __device__ __forceinline__ T table_value(const BiasArgs& A
 
 // The bias.  H: heads of a workgroup, whose values of a bucket lie side by side in LDS, so that a key costs one read for all of them; HELD: the map and the table of these
 // heads are in LDS (else read where they are).  V keys of H heads are V reads and H stores of 16 bytes.
-template <typename T, int H, bool HELD> __global__ __launch_bounds__(1024) void k_bias(BiasArgs A) {
+template <typename T, int H, bool HELD, int AXES> __global__ __launch_bounds__(1024) void k_bias(BiasArgs A) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int V = 16 / sizeof(T);
     typedef typename Run<T, H>::Vec Entry;
@@ -126,7 +162,8 @@ template <typename T, int H, bool HELD> __global__ __launch_bounds__(1024) void 
     const int here = (int)min((int64_t)V, A.keys);
     for (; t < A.items; t += (int64_t)gridDim.x * blockDim.x, step_on(I, A)) {
         uint32_t bucket[V];
-        buckets_of<V>(A, HELD ? map : A.map, I, here, bucket);
+        const uint32_t count = (uint32_t)A.buckets;
+        buckets_of<V, AXES>(A, HELD ? map : A.map, I, here, 0, count, count + kNoBias, count + kNeverSeen, bucket);
         T* out = (T*)A.values + I.b * A.value_batch + first_head * A.value_head + I.i * A.value_query + first_key<V>(A, I);
         if constexpr (HELD) {
             Entry entry[V];
@@ -161,129 +198,175 @@ template <typename T, int H, bool HELD> __global__ __launch_bounds__(1024) void 
     }
 }
 
-// The table's gradient.  A workgroup takes a share of the items and a head for each of its wavefronts, whose bins, in LDS and in 64 bits, are its own: they are added to in
-// the order of its instructions, and lanes of one instruction that meet in a bin in the order in which the LDS unit takes lanes of the same address, which nothing else
-// has a part in.  Where there are few buckets a wavefront has several copies of its bins, for the lanes in turn, so that few meet.
-// (LDS adds floats of 64 bits in 9 clocks a wavefront's instruction, those of 32 in 193: a long sequence of 4096 tokens and 12 heads took 1063 us with these.)
-// The items' buckets are made by all wavefronts, one item a thread, in a tile that all of them then go through; the next tile is made while the values of one are on
-// their way.  Pairs without a bias go to bins that nobody reads, one for each lane, and runs of nothing else are not loaded.  HELD: the map is in LDS, too.
-constexpr int kBackWaves = 8;
-constexpr int64_t kNoItem = -1;
-// Where a bucket's bins begin: neighbouring lanes' runs are eight keys apart, which would be every eighth bin; buckets' lowest bits are mixed with those of 32s.
-__device__ __forceinline__ uint32_t bin_of(uint32_t bucket, int copies) { return (bucket ^ (bucket >> 5 & 7)) * copies; }
+// ---- the table's gradient ----
+//
+// First every pair's bucket is found once for all heads (k_bias_places), as 16 bits; then the values are added by a kernel that reads both side by side, share by
+// share of the items (k_bias_bins), and the shares' sums are added in 64 bits (k_bias_sums).  Items are runs of eight keys here whatever the type.
+constexpr int kRun = 8;                                            // keys of an item
 
-template <typename T> struct BackTile {                            // LDS, for one tile of 64 items a wavefront
-    static constexpr int V = 16 / sizeof(T);
-    typedef uint16_t Places __attribute__((ext_vector_type(V)));
-    Places* place; int64_t* where;                                 // bins of an item's keys; where its values lie
-    static __host__ __device__ int64_t bytes(int waves) { return (int64_t)waves * 64 * (2 * V + 8); }
-    __device__ BackTile(char* at, int waves) {
-        place = (Places*)at;
-        where = (int64_t*)(place + waves * 64);
-    }
-};
+__host__ __device__ __forceinline__ int bins_of(int64_t held, int copies) { return (int)held * copies; }
 
-template <typename T, bool HELD> __global__ __launch_bounds__(512) void k_bias_back(BiasArgs A) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    typedef BackTile<T> Tile;
-    constexpr int V = Tile::V;
-    typedef typename Run<T, V>::Vec Values;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = A.waves, copies = A.copies;
-    const int bins = (int)(A.held_buckets + 7) / 8 * 8 * copies;
-    const int64_t tile_bytes = Tile::bytes(waves);
-    double* all_bins = (double*)(lds + 2 * tile_bytes);
-    int32_t* held_map = (int32_t*)(all_bins + waves * (bins + 64));
-    double* mine = all_bins + wave * (bins + 64);
-    for (int e = threadIdx.x; e < waves * (bins + 64); e += blockDim.x) all_bins[e] = 0.0;
+// places[item][key]: the bin of the pair, in the copy for the lane that will add it, or behind the bins one of 64 that nobody reads.  Buckets outside
+// first_bucket .. first_bucket + held_buckets - 1 have none.  live: a bit for every item of 64 that has a pair.
+template <bool HELD, int AXES> __global__ __launch_bounds__(256) void k_bias_places(BiasArgs A) {
+    extern __shared__ __attribute__((aligned(16))) int32_t held_map[];
     if (HELD) {
         const int places = A.axes * (2 * A.reach + 1);
-        for (int e = threadIdx.x; e < places; e += blockDim.x) held_map[e] = A.map[e];
-    }
-    __syncthreads();
-
-    const int64_t head = (int64_t)blockIdx.y * waves + wave, first_bucket = blockIdx.z * A.held_buckets;
-    const T* values = (const T*)A.values + head * A.value_head;
-    const int64_t from = (int64_t)blockIdx.x * A.share_items, to = min(from + A.share_items, A.items);
-    const int here = (int)min((int64_t)V, A.keys);
-
-    int64_t t = from + threadIdx.x;
-    Item I = item_at(A, t);
-    auto make = [&](const Tile& tile) {                            // of the items from t on, one a thread
-        typename Tile::Places place;
-#pragma unroll
-        for (int v = 0; v < V; v++) place[v] = (uint16_t)(bins + lane);
-        bool any = false;
-        if (t < to) {
-            uint32_t bucket[V];
-            buckets_of<V>(A, HELD ? held_map : A.map, I, here, bucket);
-            const int again = (int)(I.run * V - first_key<V>(A, I));       // (keys of the run before)
-#pragma unroll
-            for (int v = 0; v < V; v++) {
-                const uint32_t b = bucket[v] - (uint32_t)first_bucket;
-                if (v < here && v >= again && bucket[v] < A.buckets && b < A.held_buckets) {
-                    place[v] = (uint16_t)(bin_of(b, copies) + (lane & (copies - 1)));
-                    any = true;
-                }
-            }
-        }
-        tile.place[threadIdx.x] = place;
-        tile.where[threadIdx.x] = any ? I.b * A.value_batch + I.i * A.value_query + first_key<V>(A, I) : kNoItem;
-    };
-    make(Tile(lds, waves));
-    __syncthreads();
-    for (int64_t t0 = from, k = 0; t0 < to; t0 += waves * 64, k ^= 1) {
-        const Tile tile(lds + k * tile_bytes, waves);
-        Values got[kBackWaves];
-        uint32_t live = 0;
-        if (head < A.heads) {
-#pragma unroll
-            for (int s = 0; s < kBackWaves; s++)
-                if (s < waves) {
-                    const int64_t at = tile.where[s * 64 + lane];
-                    if (at != kNoItem) {
-                        live |= 1u << s;
-                        if (here == V) got[s] = reinterpret_cast<const typename Run<T, V>::Loose*>(values + at)->v;
-                        else {
-#pragma unroll
-                            for (int v = 0; v < V; v++) got[s][v] = v < here ? values[at + v] : (T)0.f;
-                        }
-                    }
-                }
-        }
-        t += waves * 64;
-        step_on(I, A);
-        if (t0 + waves * 64 < to) make(Tile(lds + (k ^ 1) * tile_bytes, waves));
-        if (head < A.heads) {
-#pragma unroll
-            for (int s = 0; s < kBackWaves; s++)
-                if (s < waves && live >> s & 1) {
-                    const typename Tile::Places place = tile.place[s * 64 + lane];
-#pragma unroll
-                    for (int v = 0; v < V; v++) unsafeAtomicAdd(&mine[place[v]], (double)(float)got[s][v]);
-                }
-        }
+        for (int e = threadIdx.x; e < places; e += 256) held_map[e] = A.map[e];
         __syncthreads();
     }
-    // A wavefront's sums over the copies of its bins.
-    if (head < A.heads) {
-        float* part = A.direct ? A.part + head : A.part + ((int64_t)blockIdx.x * A.heads + head) * A.buckets;
-        const int64_t step = A.direct ? A.heads : 1;
-        const int side_by_side = 64 / copies;
-        for (int b0 = lane / copies; b0 < A.held_buckets + lane / copies; b0 += 4 * side_by_side) {
-            double sum[4];
+    const int here = (int)min((int64_t)kRun, A.keys), lane = threadIdx.x & 63;
+    const uint32_t nowhere = bins_of(A.held_buckets, A.copies) + lane, held = (uint32_t)A.held_buckets, copy = lane & (A.copies - 1);
+    const int shift = 31 - __clz(A.copies);
+    const int64_t end = (A.items + 63) / 64 * 64;
+    int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    Item I = item_at(A, t);
+    for (; t < end; t += (int64_t)gridDim.x * 256, step_on(I, A)) {
+        uint32_t place[kRun], least = ~0u;
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int b = b0 + j * side_by_side;
-                sum[j] = b < A.held_buckets ? mine[bin_of(b, copies) + (lane & (copies - 1))] : 0.0;
+        for (int v = 0; v < kRun; v++) place[v] = nowhere;
+        if (t < A.items) {
+            uint32_t bucket[kRun];
+            buckets_of<kRun, AXES>(A, HELD ? held_map : A.map, I, here, (uint32_t)A.first_bucket, held, ~0u, ~0u, bucket);
+            const int again = (int)(I.run * kRun - first_key<kRun>(A, I));     // (keys of the run before)
+            if (again > 0 || here < kRun) {
+#pragma unroll
+                for (int v = 0; v < kRun; v++)
+                    if (v < again || v >= here) bucket[v] = ~0u;
             }
-            for (int d = 1; d < copies; d <<= 1)
 #pragma unroll
-                for (int j = 0; j < 4; j++) sum[j] += __shfl_xor(sum[j], d);
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int64_t b = b0 + j * side_by_side;
-                if ((lane & (copies - 1)) == 0 && b < A.held_buckets && first_bucket + b < A.buckets) part[(first_bucket + b) * step] = (float)sum[j];
+            for (int v = 0; v < kRun; v++) {
+                place[v] = bucket[v] < held ? bucket[v] << shift | copy : nowhere;
+                least = min(least, bucket[v]);
             }
+        }
+        Places8 packed;
+#pragma unroll
+        for (int v = 0; v < kRun; v++) packed[v] = (uint16_t)place[v];
+        A.places[t] = packed;
+        const uint64_t live = __ballot(least < held);
+        if (lane == 0) A.live[t / 64] = live;
+    }
+}
+
+// Where an item's values lie, stepped through with little arithmetic.
+template <typename T> struct Place {
+    const T* row;
+    uint32_t b, i, run;
+    __device__ __forceinline__ void begin(const BiasArgs& A, const T* values, int64_t t) {
+        const Item I = item_at(A, t);
+        b = (uint32_t)I.b; i = (uint32_t)I.i; run = (uint32_t)I.run;
+        row = values + b * A.value_batch + i * A.value_query;
+    }
+    __device__ __forceinline__ void on(const BiasArgs& A, const T* values, const Steps& by) {
+        run += by.run;
+        const bool more = run >= (uint32_t)A.runs;
+        if (more || by.query | by.batch) {
+            if (more) { run -= (uint32_t)A.runs; i++; }
+            i += by.query;
+            b += by.batch;
+            if (i >= (uint32_t)A.queries) { i -= (uint32_t)A.queries; b++; }
+            row = values + b * A.value_batch + i * A.value_query;
+        }
+    }
+    __device__ __forceinline__ const T* at(uint32_t last) const { return row + min(run * kRun, last); }      // last: where a row's last run begins
+};
+// A run of values as it lies in memory; 8 of 16 or 32 bits.
+template <typename T> struct Eight {
+    typename Run<T, 16 / sizeof(T)>::Vec part[sizeof(T) / 2];
+    template <bool WHOLE> __device__ __forceinline__ void load(const T* p, int here) {
+        constexpr int V = 16 / sizeof(T);
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(T) / 2); i++) part[i] = reinterpret_cast<const typename Run<T, V>::Loose*>(p + i * V)->v;
+        } else {
+#pragma unroll
+            for (int v = 0; v < kRun; v++) part[v / V][v % V] = v < here ? p[v] : (T)0.f;
+        }
+    }
+    __device__ __forceinline__ float at(int v) const { return (float)part[v / (16 / sizeof(T))][v % (16 / sizeof(T))]; }
+};
+
+// A wavefront has a share and a head, and bins for that in LDS, in 64 bits, which are its own: they are added to in the order of its instructions, and lanes
+// of one instruction that meet in a bin in the order in which the LDS unit takes lanes of the same address, which nothing else has a part in.  Where there are few buckets
+// there are several copies of the bins, for the lanes in turn, so that few meet.
+// (LDS adds floats of 64 bits in 9 clocks a wavefront's instruction, those of 32 in 193.  Sums of up to 64 buckets as matrix products, each pair a row with a one at its
+// bucket, took 94 to 99 % of this kernel's time with 8 and more heads and 120 to 200 % with fewer: both wait for memory.)
+constexpr int kBinItems = 4;                                       // items of a lane that are under way together
+// WHOLE: rows have eight keys at least.
+template <typename T, bool WHOLE> __global__ __launch_bounds__(512) void k_bias_bins(BiasArgs A) {
+    extern __shared__ __attribute__((aligned(16))) double all_bins[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bins = bins_of(A.held_buckets, A.copies), copies = A.copies;
+    double* mine = all_bins + wave * (bins + 64);
+    const int64_t head = (int64_t)blockIdx.y * A.waves + wave;
+    if (head >= A.heads) return;                                   // (wavefronts do not wait for each other)
+    for (int e = lane; e < bins + 64; e += 64) mine[e] = 0.0;
+    const T* values = (const T*)A.values + head * A.value_head;
+    const int here = (int)min((int64_t)kRun, A.keys);
+    const int64_t blocks = (A.items + 63) / 64, stride = (int64_t)gridDim.x * kBinItems;      // blocks of 64 items
+
+    struct Stage { Places8 place[kBinItems]; Eight<T> value[kBinItems]; uint64_t live[kBinItems]; };
+    typedef const __attribute__((address_space(4))) uint64_t* Scalars;         // (read by scalar loads: the vector loads under way are not waited for)
+    const uint32_t last = (uint32_t)max(A.keys - kRun, (int64_t)0);
+    Place<T> at;
+    int64_t block = (int64_t)blockIdx.x * kBinItems;
+    at.begin(A, values, block * 64 + lane);
+    uint64_t live[kBinItems];
+    auto look = [&]() {
+#pragma unroll
+        for (int u = 0; u < kBinItems; u++) live[u] = block + u < blocks ? ((Scalars)(uintptr_t)A.live)[block + u] : 0;
+    };
+    look();
+    // The next items.  All lanes load, those of items without a pair what is at the beginning: the compiler lets no load pass another one that stands under a condition.
+    auto fetch = [&](Stage& S) {
+#pragma unroll
+        for (int u = 0; u < kBinItems; u++) {
+            S.live[u] = live[u];
+            S.place[u] = A.places[min(block + u, blocks - 1) * 64 + lane];
+            S.value[u].template load<WHOLE>(live[u] >> lane & 1 ? at.at(last) : values, here);
+            at.on(A, values, A.near);
+        }
+        block += stride;
+        at.on(A, values, A.far);
+        look();
+    };
+    auto add = [&](const Stage& S) {
+#pragma unroll
+        for (int u = 0; u < kBinItems; u++)
+            if (S.live[u]) {
+#pragma unroll
+                for (int v = 0; v < kRun; v++) unsafeAtomicAdd(&mine[S.place[u][v]], (double)S.value[u].at(v));
+            }
+    };
+    Stage one, other;
+    fetch(one);
+    while (true) {
+        if (block >= blocks) { add(one); break; }
+        fetch(other);
+        add(one);
+        if (block >= blocks) { add(other); break; }
+        fetch(one);
+        add(other);
+    }
+    // The sums over the copies.
+    float* part = A.direct ? A.part + head : A.part + ((int64_t)blockIdx.x * A.heads + head) * A.buckets;
+    const int64_t step = A.direct ? A.heads : 1;
+    const int side_by_side = 64 / copies;
+    for (int b0 = lane / copies; b0 < A.held_buckets + lane / copies; b0 += 4 * side_by_side) {
+        double sum[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int b = b0 + j * side_by_side;
+            sum[j] = b < A.held_buckets ? mine[b * copies + (lane & (copies - 1))] : 0.0;
+        }
+        for (int d = 1; d < copies; d <<= 1)
+#pragma unroll
+            for (int j = 0; j < 4; j++) sum[j] += __shfl_xor(sum[j], d);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int64_t b = b0 + j * side_by_side;
+            if ((lane & (copies - 1)) == 0 && b < A.held_buckets && A.first_bucket + b < A.buckets) part[(A.first_bucket + b) * step] = (float)sum[j];
         }
     }
 }

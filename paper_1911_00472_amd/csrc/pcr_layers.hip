@@ -115,39 +115,39 @@ void set_step(BiasArgs& A, int64_t step) {
     A.step_batch = step / A.runs / A.queries;
 }
 
+// The axes, where there are up to three of 32-bit positions and every run of `run` keys lies in one piece; else 0.
+int plain_axes(const pcr_position_table* t, int run) {
+    const bool plain = !t->wide && t->keys >= run && t->key.token_stride == 1 && (!t->key.segment || t->key.segment_token_stride == 1);
+    return plain && t->axes <= 3 ? t->axes : 0;
+}
+
 // How the gradient is divided: wavefronts (heads) of a workgroup, copies of a wavefront's bins, ranges of buckets (each goes through all items), shares of the items.
-struct BiasPlan { int waves, copies, ranges; int64_t held, shares, share_items; size_t lds; bool held_map; };
+struct BiasPlan { int waves, copies, ranges; int64_t held, shares, items, runs; size_t lds, places_bytes, live_bytes, part_bytes; };
 BiasPlan plan_bias(const pcr_position_table* t) {
     BiasPlan P = {};
-    const BiasArgs A = bias_args(t);
-    const int64_t V = 16 / (int64_t)type_size(t->dtype);
-    const int64_t map_bytes = (int64_t)t->axes * (2 * t->reach + 1) * 4;
-    P.held_map = map_bytes <= 32 * 1024;
+    P.runs = (t->keys + kRun - 1) / kRun;
+    P.items = t->batch * t->queries * P.runs;
     P.ranges = (int)((t->buckets + 4095) / 4096);
     P.held = (t->buckets + P.ranges - 1) / P.ranges;
-    const int64_t held = (P.held + 7) / 8 * 8, elements = std::max<int64_t>(1, A.items * V);
-    auto bytes = [&](int64_t w, int64_t copies) {
-        const int64_t tile = t->dtype == PCR_FLOAT ? BackTile<float>::bytes((int)w) : BackTile<__bf16>::bytes((int)w);
-        return 2 * tile + w * (held * copies + 64) * 8 + (P.held_map ? map_bytes : 0);
-    };
+    const int64_t elements = P.items * kRun, blocks = (P.items + 63) / 64, steps = (blocks + kBinItems - 1) / kBinItems;
+    P.places_bytes = (size_t)blocks * 64 * sizeof(Places8);
+    const size_t sums = (size_t)t->heads * t->buckets * sizeof(float);
     // Few elements: one share.
-    const int64_t few = 16384;
-    const int64_t most_shares = elements <= few ? 1 : std::max<int64_t>(1, elements / std::max<int64_t>(4 * held, 4096));
+    const int64_t most_shares = elements <= 16384 ? 1 : std::max<int64_t>(1, elements / std::max<int64_t>(4 * P.held, 4096));
     P.copies = 64;
-    while (P.copies > 1 && held * P.copies > std::max(held, std::min<int64_t>(1024, elements / most_shares / 2))) P.copies >>= 1;
-    const int64_t blocks = std::max<int64_t>(1, (t->heads + kBackWaves - 1) / kBackWaves);
-    P.waves = (int)std::max<int64_t>(1, (t->heads + blocks - 1) / blocks);
-    while (P.waves > 1 && bytes(P.waves, P.copies) > kBiasLds) P.waves--;
-    P.lds = (size_t)bytes(P.waves, P.copies);
+    while (P.copies > 1 && bins_of(P.held, P.copies) > std::max<int64_t>(bins_of(P.held, 1), std::min<int64_t>(t->buckets <= 64 ? 1024 : 2048, elements / most_shares / 2))) P.copies >>= 1;
+    auto bytes = [&](int64_t w) { return w * (bins_of(P.held, P.copies) + 64) * 8; };
+    const int64_t head_blocks_8 = std::max<int64_t>(1, (t->heads + 7) / 8);
+    P.waves = (int)std::max<int64_t>(1, (t->heads + head_blocks_8 - 1) / head_blocks_8);
+    while (P.waves > 1 && bytes(P.waves) > kBiasLds) P.waves--;
+    P.lds = (size_t)bytes(P.waves);
     const int64_t head_blocks = std::max<int64_t>(1, (t->heads + P.waves - 1) / P.waves);
     const int64_t resident = 256 * std::max<int64_t>(1, std::min<int64_t>(16 / P.waves, (int64_t)(160 * 1024 / P.lds)));
-    P.shares = std::max<int64_t>(1, std::min<int64_t>(most_shares, resident / (head_blocks * P.ranges)));
-    P.share_items = (A.items + P.shares - 1) / P.shares;
-    P.share_items = (P.share_items + 63) / 64 * 64;
-    P.shares = P.share_items ? std::max<int64_t>(1, (A.items + P.share_items - 1) / P.share_items) : 1;
+    P.shares = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most_shares, steps), resident / head_blocks));
+    P.live_bytes = (size_t)(blocks + 1) / 2 * 2 * 8;
+    P.part_bytes = P.shares == 1 ? 0 : (size_t)P.shares * sums;
     return P;
 }
-size_t bias_work(const pcr_position_table* t, const BiasPlan& P) { return P.shares == 1 ? 0 : (size_t)P.shares * t->heads * t->buckets * sizeof(float); }
 
 template <typename K> bool allow_lds(K kernel, size_t bytes) {
     return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
@@ -241,10 +241,19 @@ int pcr_position_bias(int device_id, const pcr_position_table* t, void* hip_stre
     bool ok = true;
     with_type(t->dtype, [&](auto v) {
         typedef decltype(v) T;
-        auto launch = [&](auto h, auto in_lds) {
-            const auto kernel = k_bias<T, decltype(h)::value, decltype(in_lds)::value>;
+        auto launch_axes = [&](auto h, auto in_lds, auto axes) {
+            const auto kernel = k_bias<T, decltype(h)::value, decltype(in_lds)::value, decltype(axes)::value>;
             ok = allow_lds(kernel, bytes);
             if (ok) hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)blocks), dim3(threads), bytes, (hipStream_t)hip_stream, A);
+        };
+        const int plain = held ? plain_axes(t, (int)(16 / size)) : 0;
+        auto launch = [&](auto h, auto in_lds) {
+            if constexpr (decltype(in_lds)::value) {
+                if (plain == 1) return launch_axes(h, in_lds, Int<1>());
+                if (plain == 2) return launch_axes(h, in_lds, Int<2>());
+                if (plain == 3) return launch_axes(h, in_lds, Int<3>());
+            }
+            launch_axes(h, in_lds, Int<0>());
         };
         if (!held) launch(Int<4>(), std::false_type());
         else if (together == 8) { if constexpr (sizeof(T) == 2) launch(Int<8>(), std::true_type()); }
@@ -261,7 +270,7 @@ int pcr_position_bias_workspace(const pcr_position_table* t, size_t* nbytes) {
     const int rc = check_bias(t, true);
     if (rc) return rc;
     const BiasPlan P = plan_bias(t);
-    *nbytes = bias_work(t, P);
+    *nbytes = P.places_bytes + P.live_bytes + P.part_bytes;
     return PCR_OK;
 }
 
@@ -271,23 +280,50 @@ int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float
     if (!t->heads) return PCR_OK;
     if (!table_grad) return PCR_E_ARG;
     const BiasPlan P = plan_bias(t);
-    const bool none = !t->batch || !t->queries || !t->keys;
-    const bool direct = !none && P.shares == 1;
-    if (!none && !direct && !d_work) return PCR_E_ARG;
-    if (!none && !direct && work_bytes < bias_work(t, P)) return PCR_E_RANGE;
-    BiasArgs A = bias_args(t);
-    if (!none) set_step(A, P.waves * 64);
-    A.direct = direct; A.part = direct ? table_grad : (float*)d_work; A.share_items = P.share_items; A.held_buckets = P.held; A.waves = P.waves; A.copies = P.copies;
+    const bool none = !t->batch || !t->queries || !t->keys, direct = !none && P.shares == 1;
+    if (!none && !d_work) return PCR_E_ARG;
+    if (!none && work_bytes < P.places_bytes + P.live_bytes + P.part_bytes) return PCR_E_RANGE;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
     const hipStream_t s = (hipStream_t)hip_stream;
+    BiasArgs A = bias_args(t);
+    A.runs = P.runs; A.items = P.items;
+    A.places = (Places8*)d_work; A.live = (uint64_t*)((char*)d_work + P.places_bytes);
+    A.part = direct ? table_grad : (float*)((char*)d_work + P.places_bytes + P.live_bytes);
+    A.direct = direct; A.held_buckets = P.held; A.waves = P.waves; A.copies = P.copies;
     bool ok = true;
-    if (!none)
-        with_type(t->dtype, [&](auto v) {
-            const auto kernel = P.held_map ? k_bias_back<decltype(v), true> : k_bias_back<decltype(v), false>;
-            ok = allow_lds(kernel, P.lds);
-            if (ok) hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares, (unsigned)((t->heads + P.waves - 1) / P.waves), (unsigned)P.ranges), dim3(P.waves * 64), P.lds, s, A);
-        });
+    if (!none) {
+        auto steps = [&](int64_t items) { return Steps{(uint32_t)(items % A.runs), (uint32_t)(items / A.runs % A.queries), (uint32_t)(items / A.runs / A.queries)}; };
+        A.near = steps(64);
+        A.far = steps((P.shares - 1) * kBinItems * 64);
+        const size_t map_bytes = (size_t)t->axes * (2 * t->reach + 1) * 4;
+        const bool held_map = map_bytes <= 32 * 1024;
+        const unsigned groups = (unsigned)std::min<int64_t>((P.items + 255) / 256, 4096);
+        set_step(A, (int64_t)groups * 256);
+        for (int r = 0; ok && r < P.ranges; r++) {
+            A.first_bucket = r * P.held;
+            A.held_buckets = std::min<int64_t>(P.held, t->buckets - A.first_bucket);
+            const int plain = held_map ? plain_axes(t, kRun) : 0;
+            auto places = [&](auto held, auto axes) {
+                hipLaunchKernelGGL((k_bias_places<decltype(held)::value, decltype(axes)::value>), dim3(groups), dim3(256), decltype(held)::value ? map_bytes : 0, s, A);
+            };
+            if (!held_map) places(std::false_type(), Int<0>());
+            else if (plain == 1) places(std::true_type(), Int<1>());
+            else if (plain == 2) places(std::true_type(), Int<2>());
+            else if (plain == 3) places(std::true_type(), Int<3>());
+            else places(std::true_type(), Int<0>());
+            with_type(t->dtype, [&](auto v) {
+                typedef decltype(v) T;
+                auto launch = [&](auto whole) {
+                    const auto kernel = k_bias_bins<T, decltype(whole)::value>;
+                    ok = allow_lds(kernel, P.lds);
+                    if (ok) hipLaunchKernelGGL(kernel, dim3((unsigned)P.shares, (unsigned)((t->heads + P.waves - 1) / P.waves)), dim3(P.waves * 64), P.lds, s, A);
+                };
+                if (t->keys >= kRun) launch(std::true_type());
+                else launch(std::false_type());
+            });
+        }
+    }
     if (!ok) return PCR_E_DEVICE;
     if (direct) return launched();
     BiasSums S = {A.part, table_grad, none ? 0 : P.shares, t->heads, t->buckets};
