@@ -20,6 +20,11 @@ template <int N> using Int = std::integral_constant<int, N>;
 
 bool multiple(const void* p, int64_t a, int64_t b, size_t size, int unit) { return ((uint64_t)(uintptr_t)p / size | (uint64_t)a | (uint64_t)b) % unit == 0; }
 
+// Lets a kernel have more LDS than is common.
+template <typename K> bool allow_lds(K kernel, size_t bytes) {
+    return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+}
+
 // ---- group norm ----
 
 int check_norm(const pcr_group_norm* N, bool back) {
@@ -35,46 +40,117 @@ int check_norm(const pcr_group_norm* N, bool back) {
 struct NormPlan {
     int64_t chunk;
     int chunks, run;
-    size_t part_bytes, sums_bytes;
+    int held, threads, block, blocks;                          // one pass: runs that a thread holds (0: two passes), threads and channels of a workgroup, workgroups of a picture
+    size_t part_bytes, sums_bytes, joined_bytes;
+    size_t bytes() const { return part_bytes + sums_bytes + joined_bytes; }
 };
 NormPlan plan_norm(const pcr_group_norm* N, bool back) {
     NormPlan P = {};
     const size_t size = type_size(N->dtype);
-    // Chunks of a picture's pixels: 2048 workgroups in all, of 64 KB at least.
-    const int64_t row = N->channels * (int64_t)size;
-    int64_t chunks = std::min<int64_t>((2048 + N->images - 1) / std::max<int64_t>(1, N->images), (N->pixels * row + 65535) / 65536);
-    chunks = std::max<int64_t>(1, std::min<int64_t>(chunks, N->pixels));
-    P.chunk = (N->pixels + chunks - 1) / chunks;
-    P.chunks = P.chunk ? (int)((N->pixels + P.chunk - 1) / P.chunk) : 0;
-    P.part_bytes = (size_t)N->images * P.chunks * N->groups * 2 * sizeof(float);
-    P.sums_bytes = back ? (size_t)N->images * P.chunks * N->channels * 2 * sizeof(float) : 0;
-    // Runs of up to 16 bytes of channels.
+    // Runs of 16 bytes of channels, of two or of one.
     P.run = (int)(16 / size);
-    for (; P.run > 1; P.run >>= 1) {
+    for (; P.run > 1; P.run = P.run == 8 ? 2 : P.run >> 1) {
         if (N->channels % P.run) continue;
         if (multiple(N->x, N->x_image, N->x_pixel, size, P.run) && multiple(N->out, N->out_image, N->out_pixel, size, P.run) &&
             (!back || multiple(N->grad, N->grad_image, N->grad_pixel, size, P.run)))
             break;
     }
+    const int64_t each = N->channels / N->groups;
+    if (N->images && N->pixels) {
+        // One pass: channels of whole groups and whole runs, 128 bytes of them where that many fit, fewer where there are few workgroups.
+        const int64_t unit = each * P.run / std::__gcd(each, (int64_t)P.run), units = N->channels / unit;
+        const int64_t target = 256, most = P.run * size < 16 ? 256 * 8 : 512 * (back ? 8 : 16);
+        int64_t many = std::max<int64_t>(1, std::min<int64_t>((128 + unit * size - 1) / (unit * size), std::max<int64_t>(1, N->images * units / target)));
+        const int64_t of_unit = N->pixels * (unit / P.run);
+        while (many > 1 && of_unit * many > most) many >>= 1;
+        many = std::min(many, units);
+        const int64_t columns = many * unit / P.run;
+        if (of_unit * many <= most && columns <= 256) {
+            P.block = (int)(many * unit);
+            P.blocks = (int)((units + many - 1) / many);
+            P.threads = P.run * size < 16 || of_unit * many <= 256 * 4 ? 256 : 512;
+            const int64_t lanes = P.threads / columns, need = (N->pixels + lanes - 1) / lanes;
+            for (P.held = 1; P.held < need;) P.held <<= 1;
+            if (P.held > (P.run * size < 16 || back ? 8 : 16)) P.held = 0;
+            // (Rows of 16 bytes: 64 pictures of 56 x 56 x 256 take 66 us, and 65 in two passes; their gradient 201, and 113.)
+            if (P.block < N->channels && P.block * (int64_t)size < 32 && N->images * N->pixels * N->channels * (int64_t)size > (64 << 20)) P.held = 0;
+        }
+    }
+    if (P.held) {
+        P.chunk = N->pixels;
+        P.chunks = 1;
+        P.sums_bytes = back ? (size_t)N->images * N->channels * 2 * sizeof(float) : 0;
+        return P;
+    }
+    // Two passes.  Chunks of a picture's pixels: 768 workgroups in all, 512 of a gradient, of 16 pixels to a thread at least.  (us with 512 / 768 / 1024 / 2048: 64 pictures of
+    // 112 x 112 x 64 59.8 / 57.9 / 59.3 / 64.6, gradient of 64 of 56 x 56 x 256 99 / 105 / 107 / 113, of 32 of 112 x 112 x 64 57 / 62 / 66 / 66.)
+    const int64_t columns = std::min<int64_t>(N->channels / P.run, kNormThreads), lanes = kNormThreads / columns, step = kNormTogether * lanes;
+    int64_t chunks = std::min<int64_t>(((back ? 512 : 768) + N->images - 1) / std::max<int64_t>(1, N->images), (N->pixels + 4 * step - 1) / (4 * step));
+    chunks = std::max<int64_t>(1, chunks);
+    P.chunk = ((N->pixels + chunks - 1) / chunks + step - 1) / step * step;
+    P.chunks = N->pixels ? (int)((N->pixels + P.chunk - 1) / P.chunk) : 0;
+    P.part_bytes = (size_t)N->images * P.chunks * N->groups * 2 * sizeof(float);
+    P.sums_bytes = back ? (size_t)N->images * P.chunks * N->channels * 2 * sizeof(float) : 0;
+    P.joined_bytes = back && P.chunks > kMergedChunks ? (size_t)N->images * N->groups * 2 * sizeof(float) : 0;
     return P;
 }
 NormArgs norm_args(const pcr_group_norm* N, const NormPlan& P, void* d_work) {
     NormArgs A = {};
     A.x = N->x; A.grad = N->grad; A.weight = N->weight; A.bias = N->bias; A.out = N->out; A.stats = N->stats;
-    A.part = (float*)d_work; A.sums = (float*)((char*)d_work + P.part_bytes);
+    A.part = (float*)d_work; A.sums = (float*)((char*)d_work + P.part_bytes); A.joined = (float*)((char*)A.sums + P.sums_bytes);
     A.images = N->images; A.pixels = N->pixels;
     A.x_image = N->x_image; A.x_pixel = N->x_pixel; A.grad_image = N->grad_image; A.grad_pixel = N->grad_pixel; A.out_image = N->out_image; A.out_pixel = N->out_pixel;
     A.chunk = P.chunk; A.chunks = P.chunks; A.channels = (int)N->channels; A.groups = N->groups; A.each = (int)(N->channels / N->groups);
+    A.block = P.block; A.blocks = P.blocks;
     A.activation = N->activation; A.weight_float = N->weight_dtype == PCR_FLOAT; A.eps = N->eps;
     return A;
 }
 template <typename F> void with_run(int dtype, int run, F f) {
     with_type(dtype, [&](auto t) {
         if (run == 8) { if constexpr (sizeof(t) == 2) f(t, Int<8>()); }
-        else if (run == 4) f(t, Int<4>());
+        else if (run == 4) { if constexpr (sizeof(t) == 4) f(t, Int<4>()); }
         else if (run == 2) f(t, Int<2>());
         else f(t, Int<1>());
     });
+}
+
+// One pass of either kind.
+template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, NormArgs A, hipStream_t s) {
+    bool ok = true;
+    const bool one = A.each % P.run == 0;
+    with_run(N->dtype, P.run, [&](auto t, auto v) {
+        typedef decltype(t) T;
+        constexpr int V = decltype(v)::value;
+        auto launch = [&](auto k, auto threads, auto in_one) {
+            constexpr int K = decltype(k)::value, THREADS = decltype(threads)::value;
+            constexpr bool ONE = decltype(in_one)::value;
+            const size_t of_block = A.block + A.block / A.each;
+            const size_t lds = BACK ? (THREADS * V + 2 * of_block) * sizeof(float) : (THREADS * (ONE ? 1 : V) + 3 * (A.block / A.each)) * sizeof(float);
+            in_ranges(A.images * A.blocks, THREADS, [&](int64_t begin, unsigned groups) {
+                A.begin = begin;
+                if constexpr (BACK) {
+                    ok = ok && allow_lds(k_norm_back_held<T, V, K, THREADS, ONE>, lds);
+                    if (ok) hipLaunchKernelGGL((k_norm_back_held<T, V, K, THREADS, ONE>), dim3(groups), dim3(THREADS), lds, s, A);
+                } else {
+                    ok = ok && allow_lds(k_norm_held<T, V, K, THREADS, ONE>, lds);
+                    if (ok) hipLaunchKernelGGL((k_norm_held<T, V, K, THREADS, ONE>), dim3(groups), dim3(THREADS), lds, s, A);
+                }
+            });
+        };
+        auto by_one = [&](auto k, auto threads) {
+            if (one) launch(k, threads, std::true_type());
+            else if constexpr (V > 1) launch(k, threads, std::false_type());
+        };
+        if constexpr (V * sizeof(T) < 16) {
+            if (P.held <= 2) by_one(Int<2>(), Int<256>());
+            else by_one(Int<8>(), Int<256>());
+        } else if (P.threads == 256) {
+            if (P.held <= 1) by_one(Int<1>(), Int<256>());
+            else by_one(Int<4>(), Int<256>());
+        } else if (P.held <= 8) by_one(Int<8>(), Int<512>());
+        else if constexpr (!BACK) by_one(Int<16>(), Int<512>());
+    });
+    return ok;
 }
 
 // ---- position bias ----
@@ -149,10 +225,6 @@ BiasPlan plan_bias(const pcr_position_table* t) {
     return P;
 }
 
-template <typename K> bool allow_lds(K kernel, size_t bytes) {
-    return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
-}
-
 }  // namespace
 
 extern "C" {
@@ -163,7 +235,7 @@ int pcr_group_norm_workspace(const pcr_group_norm* norm, int backward, size_t* n
     if (norm->channels < 1 || norm->channels > 16384 || norm->groups < 1 || norm->groups > 4096 || norm->channels % norm->groups || norm->images < 0 || norm->pixels < 0 ||
         norm->images > kMaxGrid || norm->pixels > (1ll << 40)) return PCR_E_RANGE;
     const NormPlan P = plan_norm(norm, backward != 0);
-    *nbytes = P.part_bytes + P.sums_bytes;
+    *nbytes = P.bytes();
     return PCR_OK;
 }
 
@@ -172,20 +244,30 @@ int pcr_group_norm_forward(int device_id, const pcr_group_norm* norm, void* d_wo
     if (rc) return rc;
     if (!norm->images || !norm->pixels) return PCR_OK;
     const NormPlan P = plan_norm(norm, false);
-    if (!d_work) return PCR_E_ARG;
-    if (work_bytes < P.part_bytes) return PCR_E_RANGE;
-    if (norm->images * P.chunks > groups_of_a_launch(kNormThreads)) return PCR_E_RANGE;
+    if (P.bytes() && !d_work) return PCR_E_ARG;
+    if (work_bytes < P.bytes()) return PCR_E_RANGE;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
-    const NormArgs A = norm_args(norm, P, d_work);
+    NormArgs A = norm_args(norm, P, d_work);
     const hipStream_t s = (hipStream_t)hip_stream;
+    if (P.held) return run_held<false>(norm, P, A, s) ? launched() : PCR_E_DEVICE;
     with_run(norm->dtype, P.run, [&](auto t, auto v) {
         typedef decltype(t) T;
         constexpr int V = decltype(v)::value;
-        const unsigned groups = (unsigned)(A.images * A.chunks);
-        hipLaunchKernelGGL((k_norm_sums<T, V>), dim3(groups), dim3(kNormThreads), (kNormThreads * V + 2 * A.groups) * sizeof(float), s, A);
-        hipLaunchKernelGGL(k_norm_stats, dim3((unsigned)((A.images * A.groups + 63) / 64)), dim3(64), 0, s, A);
-        hipLaunchKernelGGL((k_norm_apply<T, V>), dim3(groups), dim3(kNormThreads), 0, s, A);
+        in_ranges(A.images * A.chunks, kNormThreads, [&](int64_t begin, unsigned groups) {
+            A.begin = begin;
+            hipLaunchKernelGGL((k_norm_sums<T, V>), dim3(groups), dim3(kNormThreads), (kNormThreads * V + 2 * A.groups) * sizeof(float), s, A);
+        });
+        if (A.chunks > kMergedChunks)
+            in_ranges((A.images * A.groups + 3) / 4, 256, [&](int64_t begin, unsigned groups) {
+                A.begin = begin;
+                hipLaunchKernelGGL((k_norm_join<false>), dim3(groups), dim3(256), 0, s, A);
+            });
+        in_ranges(A.images * A.chunks, kNormThreads, [&](int64_t begin, unsigned groups) {
+            A.begin = begin;
+            if (A.each % V == 0) hipLaunchKernelGGL((k_norm_apply<T, V, true>), dim3(groups), dim3(kNormThreads), 2 * A.groups * sizeof(float), s, A);
+            else if constexpr (V > 1) hipLaunchKernelGGL((k_norm_apply<T, V, false>), dim3(groups), dim3(kNormThreads), 2 * A.groups * sizeof(float), s, A);
+        });
     });
     return launched();
 }
@@ -196,19 +278,36 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
     const NormPlan P = plan_norm(norm, true);
     const bool none = !norm->images || !norm->pixels;
     if (!none && !d_work) return PCR_E_ARG;
-    if (!none && work_bytes < P.part_bytes + P.sums_bytes) return PCR_E_RANGE;
-    if (norm->images * P.chunks > groups_of_a_launch(kNormThreads)) return PCR_E_RANGE;
+    if (!none && work_bytes < P.bytes()) return PCR_E_RANGE;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
-    const NormArgs A = norm_args(norm, P, d_work);
+    NormArgs A = norm_args(norm, P, d_work);
     const hipStream_t s = (hipStream_t)hip_stream;
-    if (!none)
+    if (!none && P.held) {
+        if (!run_held<true>(norm, P, A, s)) return PCR_E_DEVICE;
+    } else if (!none)
         with_run(norm->dtype, P.run, [&](auto t, auto v) {
             typedef decltype(t) T;
             constexpr int V = decltype(v)::value;
-            const unsigned groups = (unsigned)(A.images * A.chunks);
-            hipLaunchKernelGGL((k_norm_back_sums<T, V>), dim3(groups), dim3(kNormThreads), (kNormThreads * V + 2 * A.groups) * sizeof(float), s, A);
-            hipLaunchKernelGGL((k_norm_back_apply<T, V>), dim3(groups), dim3(kNormThreads), 2 * A.groups * sizeof(float), s, A);
+            const int block = std::min(A.channels, kNormThreads * V);
+            in_ranges(A.images * A.chunks, kNormThreads, [&](int64_t begin, unsigned groups) {
+                A.begin = begin;
+                const size_t lds = (kNormThreads * V + 2 * A.groups + 2 * block) * sizeof(float);
+                if (A.each % V == 0) hipLaunchKernelGGL((k_norm_back_sums<T, V, true>), dim3(groups), dim3(kNormThreads), lds, s, A);
+                else if constexpr (V > 1) hipLaunchKernelGGL((k_norm_back_sums<T, V, false>), dim3(groups), dim3(kNormThreads), lds, s, A);
+            });
+            if (A.chunks > kMergedChunks)
+                in_ranges((A.images * A.groups + 3) / 4, 256, [&](int64_t begin, unsigned groups) {
+                    NormArgs J = A;
+                    J.begin = begin;
+                    J.stats = A.joined;
+                    hipLaunchKernelGGL((k_norm_join<true>), dim3(groups), dim3(256), 0, s, J);
+                });
+            in_ranges(A.images * A.chunks, kNormThreads, [&](int64_t begin, unsigned groups) {
+                A.begin = begin;
+                if (A.each % V == 0) hipLaunchKernelGGL((k_norm_back_apply<T, V, true>), dim3(groups), dim3(kNormThreads), 2 * A.groups * sizeof(float), s, A);
+                else if constexpr (V > 1) hipLaunchKernelGGL((k_norm_back_apply<T, V, false>), dim3(groups), dim3(kNormThreads), 2 * A.groups * sizeof(float), s, A);
+            });
         });
     if (norm->weight_grad || norm->bias_grad) {
         NormWeightSums W = {A.sums, norm->weight_grad, norm->bias_grad, none ? 0 : A.images * A.chunks, A.channels};

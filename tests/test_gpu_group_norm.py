@@ -209,7 +209,7 @@ def test_infinite_values_stay_in_their_group(dtype):
         y, s = pkg.group_norm_forward(bad, 4, None, None, EPS, "relu")
         at = torch.zeros_like(x, dtype=torch.bool)
         at[1, :, :, 16:24] = True
-        assert bool(y[at].isnan().all()) and torch.equal(y[~at], clean[~at]) and bool(s[1, 2].isnan().all())
+        assert bool(y[at].isnan().all()) and torch.equal(y[~at], clean[~at]) and not bool(s[1, 2, 0].isfinite()) and bool(s[1, 2, 1].isnan())       # (a mean may be infinite)
         g = torch.ones_like(x)
         dx, dw, db = pkg.group_norm_backward(g, bad, 4, torch.ones(32, device="cuda"), torch.zeros(32, device="cuda"), s, "silu")
         assert bool(dx[at].isnan().all()) and not bool(dx[~at].isnan().any())

@@ -67,7 +67,7 @@ def test_group_norm():
         assert L.pcr_group_norm_forward(0, by(norm(eps=eps)), at, 1 << 40, None) == pkg.E_RANGE
     assert L.pcr_group_norm_backward(0, by(norm(grad=None)), at, 1 << 40, None) == pkg.E_ARG
     assert L.pcr_group_norm_forward(0, None, at, 64, None) == pkg.E_ARG and L.pcr_group_norm_backward(0, None, at, 64, None) == pkg.E_ARG
-    large = dict(images=3, pixels=1 << 20)
+    large = dict(images=3, pixels=1 << 24)
     for backward, f in ((0, L.pcr_group_norm_forward), (1, L.pcr_group_norm_backward)):
         assert L.pcr_group_norm_workspace(by(norm(**large)), backward, by(need)) == pkg.OK and need.value > 0
         assert f(0, by(norm(**large)), None, need.value, None) == pkg.E_ARG
