@@ -566,7 +566,7 @@ int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weigh
 
 /* ---- layers of a network that trains on the pictures ----
  *
- * What stands between its matrix products, under the same rules as above: group norm with an activation over feature maps, a bias of attention for the
+ * What stands between its matrix products, under the same rules as above (and d_work at a multiple of 16 bytes): group norm with an activation over feature maps, a bias of attention for the
  * relative position of its tokens, dropout onto a residual.
  *
  * Group norm, channels last: x [image][pixel][channel] with strides of images and pixels, channels contiguous; `groups` groups of channels / groups channels each
@@ -576,7 +576,8 @@ int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weigh
  * pcr_group_norm_forward: out: y (it may be x with its strides; otherwise they must not overlap); stats float [image][group][2]: m and r.
  * pcr_group_norm_backward: grad: the gradient of y; stats: as forward gave them; out: the gradient of x (it may be grad or x with its strides); weight_grad, bias_grad: float
  *   [channel], summed over images and pixels in a fixed order (NULL: not asked for).  eps is not used.  No images or pixels: weight and bias gradients are zeros.
- * d_work: pcr_group_norm_workspace bytes for the pass that is to be made (backward: 0 or 1), its content is of no account before and after. */
+ * d_work: pcr_group_norm_workspace bytes for the same struct and the pass that is to be made (backward: 0 or 1), its content is of no account before and after (0 bytes: NULL).
+ * Without images or pixels nothing is written but zeros in weight_grad and bias_grad. */
 enum { PCR_ACT_NONE = 0, PCR_ACT_RELU = 1, PCR_ACT_SILU = 2, PCR_ACT_GELU = 3 };
 typedef struct pcr_group_norm {
     const void* x; int64_t x_image, x_pixel;
@@ -601,7 +602,8 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
  *   table        [bucket][head] of table_dtype (float, or dtype)
  *   values       dtype, with strides of batch, heads and queries, keys contiguous: the bias, written; of the backward pass its gradient, read
  * pcr_position_bias_backward: table_grad float [bucket][head]: the sum of the gradient over the pairs of each bucket, in a fixed order; pairs that have no
- *   bias add nothing, whatever their gradient holds.  d_work: pcr_position_bias_workspace bytes. */
+ *   bias add nothing, whatever their gradient holds.  Sums are held in 64 bits, those of shares of the pairs rounded to 32 in between.
+ *   d_work: pcr_position_bias_workspace bytes (2 for every pair of tokens, and the shares' sums). */
 typedef struct pcr_places {
     const void* position; int64_t axis_stride, batch_stride, token_stride;
     const int32_t* segment; int64_t segment_batch_stride, segment_token_stride;

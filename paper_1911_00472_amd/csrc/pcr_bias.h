@@ -135,8 +135,9 @@ template <typename T> __device__ __forceinline__ T table_value(const BiasArgs& A
     return A.table_float ? (T)((const float*)A.table)[at] : ((const T*)A.table)[at];
 }
 
-// The bias.  H: heads of a workgroup, whose values of a bucket lie side by side in LDS, so that a key costs one read for all of them; HELD: the map and the table of these
-// heads are in LDS (else read where they are).  V keys of H heads are V reads and H stores of 16 bytes.
+// The bias.  Bound by its stores.  H: heads of a workgroup, whose values of a bucket lie side by side in LDS, so that a key costs one read for all of them and its bucket is found
+// once; V keys of H heads are V reads and H stores of 16 bytes.  HELD: the map and the table of these heads are in LDS (else read where they are).  us: 16 sequences of 1024 packed
+// tokens, 12 heads, 3969 buckets, half, 403 MB 88 (81 at 5.0 TB/s; 136 with the axes in a loop and divisions in 64 bits), one query of 32 sequences against 4099 keys 5.5.
 template <typename T, int H, bool HELD, int AXES> __global__ __launch_bounds__(1024) void k_bias(BiasArgs A) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int V = 16 / sizeof(T);
@@ -202,6 +203,8 @@ template <typename T, int H, bool HELD, int AXES> __global__ __launch_bounds__(1
 //
 // First every pair's bucket is found once for all heads (k_bias_places), as 16 bits; then the values are added by a kernel that reads both side by side, share by
 // share of the items (k_bias_bins), and the shares' sums are added in 64 bits (k_bias_sums).  Items are runs of eight keys here whatever the type.
+// us (what reading the gradient takes at 5.0 TB/s): 4096 x 4096 pairs of 12 heads in 31 buckets, bfloat 122 (81): 17 + 104 + 5; four sequences of 1501 packed tokens, 12 heads, 3969 buckets
+// 109 (43): 14 + 85 + 7.  With the buckets found by every workgroup for its own heads, in a tile that its wavefronts shared, these were 144 and 239.
 constexpr int kRun = 8;                                            // keys of an item
 
 __host__ __device__ __forceinline__ int bins_of(int64_t held, int copies) { return (int)held * copies; }
@@ -290,8 +293,9 @@ template <typename T> struct Eight {
 // A wavefront has a share and a head, and bins for that in LDS, in 64 bits, which are its own: they are added to in the order of its instructions, and lanes
 // of one instruction that meet in a bin in the order in which the LDS unit takes lanes of the same address, which nothing else has a part in.  Where there are few buckets
 // there are several copies of the bins, for the lanes in turn, so that few meet.
-// (LDS adds floats of 64 bits in 9 clocks a wavefront's instruction, those of 32 in 193.  Sums of up to 64 buckets as matrix products, each pair a row with a one at its
-// bucket, took 94 to 99 % of this kernel's time with 8 and more heads and 120 to 200 % with fewer: both wait for memory.)
+// (LDS adds floats of 64 bits in 9 clocks a wavefront's instruction, those of 32 in 193: the long sequence took 1063 us with these.  Sums of up to 64 buckets as matrix products, each
+// pair a row with a one at its bucket, took 94 to 99 % of this kernel's time with 8 and more heads and 120 to 200 % with fewer: both wait for memory.  Six or eight items under way
+// took 1 to 9 % longer than four.)
 constexpr int kBinItems = 4;                                       // items of a lane that are under way together
 // WHOLE: rows have eight keys at least.
 template <typename T, bool WHOLE> __global__ __launch_bounds__(512) void k_bias_bins(BiasArgs A) {
@@ -372,10 +376,10 @@ template <typename T, bool WHOLE> __global__ __launch_bounds__(512) void k_bias_
 }
 
 // Sums of the shares' parts [share][head][bucket], in 64 bits and in a fixed order, into [bucket][head]: 64 bins to a workgroup, 16 threads to a bin.
-struct BiasSums { const float* part; float* out; int64_t shares, heads, buckets; };
+struct BiasSums { const float* part; float* out; int64_t shares, heads, buckets, begin; };       // begin: workgroups of earlier launches
 __global__ __launch_bounds__(1024) void k_bias_sums(BiasSums A) {
     __shared__ double joined[1024];
-    const int64_t n = A.heads * A.buckets, e = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const int64_t n = A.heads * A.buckets, e = (blockIdx.x + A.begin) * 64 + (threadIdx.x & 63);
     double sum = 0.0;
     if (e < n) {
 #pragma unroll 8

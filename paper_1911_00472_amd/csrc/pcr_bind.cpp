@@ -509,7 +509,9 @@ PyObject* group_norm_forward(PyObject*, PyObject* const* a, Py_ssize_t given) { 
         const double eps = number(a[4]);
         need(eps >= 0, "eps", "not below 0");
         G.n.eps = (float)eps;
-        const at::Tensor out = G.into(a[6], "out"), stats = at::empty({G.n.images, G.n.groups, 2}, G.x.options().dtype(at::kFloat));
+        const at::Tensor out = G.into(a[6], "out");
+        const auto floats = G.x.options().dtype(at::kFloat);
+        const at::Tensor stats = G.n.pixels ? at::empty({G.n.images, G.n.groups, 2}, floats) : at::full({G.n.images, G.n.groups, 2}, NAN, floats);
         G.n.stats = (float*)stats.data_ptr();
         size_t bytes = 0;
         const at::Tensor work = G.work(0, bytes);

@@ -320,23 +320,19 @@ template <typename T, int V, int K, int THREADS, bool ONE> __global__ __launch_b
         group_totals(values, total + z * S.channels, S.lanes, S.channels, 0, 1, 0, S.channels);
         __syncthreads();
     }
+    // Those of the groups, from their channels'.
     float* of_group = total + 2 * S.channels;
     const float inv = 1.f / ((float)pixels * A.each);
-    for (int e = threadIdx.x; e < 2 * S.channels; e += THREADS) {
-        const int z = e >= S.channels, ch = e - z * S.channels;
-        A.sums[(S.image * A.channels + S.first + ch) * 2 + z] = total[e];
+    for (int e = threadIdx.x; e < S.channels; e += THREADS) {
+        ((float2*)A.sums)[S.image * A.channels + S.first + e] = make_float2(total[e], total[S.channels + e]);
+        float by[1];
+        load_parameters<T, 1>(A, A.weight, S.first + e, 1.f, by);
+        total[e] *= by[0] * inv;
+        total[S.channels + e] *= by[0] * inv;
     }
-    for (int e = threadIdx.x; e < 2 * groups; e += THREADS) {
-        const int z = e >= groups, g = e - z * groups;
-        float sum = 0.f;
-        for (int i = 0; i < A.each; i++) {
-            const int ch = g * A.each + i;
-            float by[1];
-            load_parameters<T, 1>(A, A.weight, S.first + ch, 1.f, by);
-            sum = __builtin_fmaf(total[z * S.channels + ch], by[0], sum);
-        }
-        of_group[e] = sum * inv;
-    }
+    __syncthreads();
+    group_totals(total, of_group, 1, S.channels, 0, A.each, 0, groups);
+    group_totals(total + S.channels, of_group + groups, 1, S.channels, 0, A.each, 0, groups);
     __syncthreads();
     if (!S.works) return;
     float su[ONE ? 1 : V], sh[ONE ? 1 : V];

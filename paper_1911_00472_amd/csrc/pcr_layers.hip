@@ -18,6 +18,8 @@ namespace {
 
 template <int N> using Int = std::integral_constant<int, N>;
 
+// Working memory lies at a multiple of 16 bytes.
+bool at_16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool multiple(const void* p, int64_t a, int64_t b, size_t size, int unit) { return ((uint64_t)(uintptr_t)p / size | (uint64_t)a | (uint64_t)b) % unit == 0; }
 
 // Lets a kernel have more LDS than is common.
@@ -57,7 +59,8 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
     }
     const int64_t each = N->channels / N->groups;
     if (N->images && N->pixels) {
-        // One pass: channels of whole groups and whole runs, 128 bytes of them where that many fit, fewer where there are few workgroups.
+        // One pass: channels of whole groups and whole runs, 128 bytes of them where that many fit, fewer where there would be less than 256 workgroups.  A thread holds 16 runs at most (8 of
+        // input and gradient each): with 32 there is one workgroup a compute unit, which loads, sums and stores one after another (64 pictures of 56 x 56 x 256 54 us and 48).
         const int64_t unit = each * P.run / std::__gcd(each, (int64_t)P.run), units = N->channels / unit;
         const int64_t target = 256, most = P.run * size < 16 ? 256 * 8 : 512 * (back ? 8 : 16);
         int64_t many = std::max<int64_t>(1, std::min<int64_t>((128 + unit * size - 1) / (unit * size), std::max<int64_t>(1, N->images * units / target)));
@@ -68,9 +71,9 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
         if (of_unit * many <= most && columns <= 256) {
             P.block = (int)(many * unit);
             P.blocks = (int)((units + many - 1) / many);
-            P.threads = P.run * size < 16 || of_unit * many <= 256 * 4 ? 256 : 512;
-            const int64_t lanes = P.threads / columns, need = (N->pixels + lanes - 1) / lanes;
-            for (P.held = 1; P.held < need;) P.held <<= 1;
+            auto need = [&](int threads) { return (N->pixels + threads / columns - 1) / (threads / columns); };
+            P.threads = P.run * size < 16 || need(256) <= 4 ? 256 : 512;
+            for (P.held = 1; P.held < need(P.threads);) P.held <<= 1;
             if (P.held > (P.run * size < 16 || back ? 8 : 16)) P.held = 0;
             // (Rows of 16 bytes: 64 pictures of 56 x 56 x 256 take 66 us, and 65 in two passes; their gradient 201, and 113.)
             if (P.block < N->channels && P.block * (int64_t)size < 32 && N->images * N->pixels * N->channels * (int64_t)size > (64 << 20)) P.held = 0;
@@ -208,10 +211,12 @@ BiasPlan plan_bias(const pcr_position_table* t) {
     const int64_t elements = P.items * kRun, blocks = (P.items + 63) / 64, steps = (blocks + kBinItems - 1) / kBinItems;
     P.places_bytes = (size_t)blocks * 64 * sizeof(Places8);
     const size_t sums = (size_t)t->heads * t->buckets * sizeof(float);
-    // Few elements: one share.
+    // Shares: of four values to a bin at least, of 16384 values one, whose sums are the result; as many as are resident together.  Copies: up to 1024 bins of a wavefront, 2048 where there
+    // are more than 64 buckets, whose lanes meet more than once where differences are held at the reach (us with 1024 / 2048: four sequences of 32 x 32 patches, 12 heads, 31 x 31 buckets
+    // 137 / 79, 15 x 15 75 / 61; 4096 tokens in 31 buckets 154 / 202), and an eighth of the share's values, as bins are cleared and summed.
     const int64_t most_shares = elements <= 16384 ? 1 : std::max<int64_t>(1, elements / std::max<int64_t>(4 * P.held, 4096));
     P.copies = 64;
-    while (P.copies > 1 && bins_of(P.held, P.copies) > std::max<int64_t>(bins_of(P.held, 1), std::min<int64_t>(t->buckets <= 64 ? 1024 : 2048, elements / most_shares / 2))) P.copies >>= 1;
+    while (P.copies > 1 && bins_of(P.held, P.copies) > std::max<int64_t>(bins_of(P.held, 1), std::min<int64_t>(t->buckets <= 64 ? 1024 : 2048, elements / most_shares / 8))) P.copies >>= 1;
     auto bytes = [&](int64_t w) { return w * (bins_of(P.held, P.copies) + 64) * 8; };
     const int64_t head_blocks_8 = std::max<int64_t>(1, (t->heads + 7) / 8);
     P.waves = (int)std::max<int64_t>(1, (t->heads + head_blocks_8 - 1) / head_blocks_8);
@@ -246,6 +251,7 @@ int pcr_group_norm_forward(int device_id, const pcr_group_norm* norm, void* d_wo
     const NormPlan P = plan_norm(norm, false);
     if (P.bytes() && !d_work) return PCR_E_ARG;
     if (work_bytes < P.bytes()) return PCR_E_RANGE;
+    if (!at_16(d_work)) return PCR_E_ARG;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
     NormArgs A = norm_args(norm, P, d_work);
@@ -279,6 +285,7 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
     const bool none = !norm->images || !norm->pixels;
     if (!none && !d_work) return PCR_E_ARG;
     if (!none && work_bytes < P.bytes()) return PCR_E_RANGE;
+    if (!at_16(d_work)) return PCR_E_ARG;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
     NormArgs A = norm_args(norm, P, d_work);
@@ -324,7 +331,7 @@ int pcr_position_bias(int device_id, const pcr_position_table* t, void* hip_stre
     const size_t size = type_size(t->dtype);
     const size_t map_bytes = (size_t)t->axes * (2 * t->reach + 1) * 4;
     auto lds = [&](int heads) { return ((size_t)(t->buckets + 2) * heads * size + 15) / 16 * 16 + map_bytes; };
-    // Heads side by side: 16 bytes of them, fewer where the table is long.
+    // Heads side by side: 16 bytes of them, fewer where the table is long; workgroups of 1024 threads, and no more of them than fit side by side, where the tables take LDS.
     int together = (int)(16 / size);
     while (together > 1 && (together >= 2 * t->heads || lds(together) > 72 * 1024)) together >>= 1;
     const bool held = lds(together) <= (size_t)kBiasLds;
@@ -382,6 +389,7 @@ int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float
     const bool none = !t->batch || !t->queries || !t->keys, direct = !none && P.shares == 1;
     if (!none && !d_work) return PCR_E_ARG;
     if (!none && work_bytes < P.places_bytes + P.live_bytes + P.part_bytes) return PCR_E_RANGE;
+    if (!at_16(d_work)) return PCR_E_ARG;
     const OnDevice on(device_id);
     if (!on.ok) return PCR_E_DEVICE;
     const hipStream_t s = (hipStream_t)hip_stream;
@@ -425,8 +433,11 @@ int pcr_position_bias_backward(int device_id, const pcr_position_table* t, float
     }
     if (!ok) return PCR_E_DEVICE;
     if (direct) return launched();
-    BiasSums S = {A.part, table_grad, none ? 0 : P.shares, t->heads, t->buckets};
-    hipLaunchKernelGGL(k_bias_sums, dim3((unsigned)((t->heads * t->buckets + 63) / 64)), dim3(1024), 0, s, S);
+    BiasSums S = {A.part, table_grad, none ? 0 : P.shares, t->heads, t->buckets, 0};
+    in_ranges((t->heads * t->buckets + 63) / 64, 1024, [&](int64_t begin, unsigned groups) {
+        S.begin = begin;
+        hipLaunchKernelGGL(k_bias_sums, dim3(groups), dim3(1024), 0, s, S);
+    });
     return launched();
 }
 

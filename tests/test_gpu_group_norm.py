@@ -130,6 +130,20 @@ def test_norm_and_gradient(shape, G, dtype):
         assert all(p is q is None or torch.equal(p, q) for p, q in zip(found, again))
 
 
+@pytest.mark.parametrize("pixels", [1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 15, 16, 17, 31, 33])
+@pytest.mark.parametrize("C,G", [(1032, 1), (800, 1), (1376, 2), (2048, 1), (2056, 1), (688, 1), (522, 1), (258, 1), (771, 3)])
+def test_wide_groups_of_few_pixels(C, G, pixels):
+    """Runs of a pixel that do not divide a workgroup's threads: some of them have none, the others more pixels than their share."""
+    gen = generator(C + pixels)
+    for dtype in TYPES[:2]:
+        x = make((2, pixels, C), dtype, gen)
+        w, b = (torch.randn(C, generator=gen, device="cuda") for _ in range(2))
+        y, stats = pkg.group_norm_forward(x, G, w, b, EPS, "silu")
+        check_forward(x, G, w, b, EPS, "silu", y, stats)
+        g = torch.randn(x.shape, generator=gen, device="cuda").to(dtype)
+        check_backward(g, x, G, w, b, stats, "silu", *pkg.group_norm_backward(g, x, G, w, b, stats, "silu"))
+
+
 @pytest.mark.parametrize("kind", ACTIVATIONS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_many_pixels(dtype, kind):
