@@ -576,8 +576,7 @@ int pcr_distill_step(int device_id, const pcr_distill* d, const float* row_weigh
  * pcr_group_norm_forward: out: y (it may be x with its strides; otherwise they must not overlap); stats float [image][group][2]: m and r.
  * pcr_group_norm_backward: grad: the gradient of y; stats: as forward gave them; out: the gradient of x (it may be grad or x with its strides); weight_grad, bias_grad: float
  *   [channel], summed over images and pixels in a fixed order (NULL: not asked for).  eps is not used.  No images or pixels: weight and bias gradients are zeros.
- * d_work: pcr_group_norm_workspace bytes for the same struct and the pass that is to be made (backward: 0 or 1), its content is of no account before and after (0 bytes: NULL).
- * Without images or pixels nothing is written but zeros in weight_grad and bias_grad. */
+ * d_work: pcr_group_norm_workspace bytes for the same struct and the pass that is to be made (backward: 0 or 1), its content is of no account before and after (0 bytes: NULL). */
 enum { PCR_ACT_NONE = 0, PCR_ACT_RELU = 1, PCR_ACT_SILU = 2, PCR_ACT_GELU = 3 };
 typedef struct pcr_group_norm {
     const void* x; int64_t x_image, x_pixel;
