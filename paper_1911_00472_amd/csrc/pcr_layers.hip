@@ -144,13 +144,9 @@ template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, N
             if (one) launch(k, threads, std::true_type());
             else if constexpr (V > 1) launch(k, threads, std::false_type());
         };
-        if constexpr (V * sizeof(T) < 16) {
-            if (P.held <= 2) by_one(Int<2>(), Int<256>());
-            else by_one(Int<8>(), Int<256>());
-        } else if (P.threads == 256) {
-            if (P.held <= 1) by_one(Int<1>(), Int<256>());
-            else by_one(Int<4>(), Int<256>());
-        } else if (P.held <= 8) by_one(Int<8>(), Int<512>());
+        if constexpr (V * sizeof(T) < 16) by_one(Int<8>(), Int<256>());
+        else if (P.threads == 256) by_one(Int<4>(), Int<256>());
+        else if (P.held <= 8) by_one(Int<8>(), Int<512>());
         else if constexpr (!BACK) by_one(Int<16>(), Int<512>());
     });
     return ok;
