@@ -77,8 +77,7 @@ template <typename P, int V> __device__ __forceinline__ void load_places(const P
         for (int v = 0; v < V; v++) at[v] = v < here ? from[v * stride] : without;
     }
 }
-// The buckets of an item's keys, less `start`: `none` for one that is not below `limit`, `never` for one of another segment, all `none` for a query that is padding.  AXES: so many 32-bit
-// positions whose keys, V at least, follow each other in memory, as their segments do; 0: any.
+// Adds what the axes of any type and stride make of an item's keys.
 template <typename P, int V> __device__ __forceinline__ void sum_axes(const BiasArgs& A, const int32_t* map, const Item& I, int here, int32_t (&sum)[V]) {
     const int width = 2 * A.reach + 1;
     for (int a = 0; a < A.axes; a++) {
@@ -90,6 +89,8 @@ template <typename P, int V> __device__ __forceinline__ void sum_axes(const Bias
         for (int v = 0; v < V; v++) sum[v] = (int32_t)((uint32_t)sum[v] + (uint32_t)middle[apart(at[v], query, A.reach)]);
     }
 }
+// The buckets of an item's keys, less `start`: `none` for one that is not below `limit`, `never` for one of another segment, all `none` for a query that is padding.  AXES: so many 32-bit
+// positions whose keys, V at least, follow each other in memory, as their segments do; 0: any.
 template <int V, int AXES> __device__ __forceinline__ void buckets_of(const BiasArgs& A, const int32_t* map, const Item& I, int here, uint32_t start, uint32_t limit, uint32_t none,
                                                                        uint32_t never, uint32_t (&bucket)[V]) {
     int32_t mine = 0, other[V], sum[V];
@@ -137,7 +138,7 @@ template <typename T> __device__ __forceinline__ T table_value(const BiasArgs& A
 
 // The bias.  Bound by its stores.  H: heads of a workgroup, whose values of a bucket lie side by side in LDS, so that a key costs one read for all of them and its bucket is found
 // once; V keys of H heads are V reads and H stores of 16 bytes.  HELD: the map and the table of these heads are in LDS (else read where they are).  us: 16 sequences of 1024 packed
-// tokens, 12 heads, 3969 buckets, half, 403 MB 88 (81 at 5.0 TB/s; 136 with the axes in a loop and divisions in 64 bits), one query of 32 sequences against 4099 keys 5.5.
+// tokens, 12 heads, 3969 buckets, half, 403 MB 88 (81 at 5.0 TB/s; 136 with the axes in a loop and divisions in 64 bits), 16 heads for one query each of 32 sequences of 4099 keys 5.2.
 template <typename T, int H, bool HELD, int AXES> __global__ __launch_bounds__(1024) void k_bias(BiasArgs A) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int V = 16 / sizeof(T);
@@ -203,8 +204,8 @@ template <typename T, int H, bool HELD, int AXES> __global__ __launch_bounds__(1
 //
 // First every pair's bucket is found once for all heads (k_bias_places), as 16 bits; then the values are added by a kernel that reads both side by side, share by
 // share of the items (k_bias_bins), and the shares' sums are added in 64 bits (k_bias_sums).  Items are runs of eight keys here whatever the type.
-// us (what reading the gradient takes at 5.0 TB/s): 4096 x 4096 pairs of 12 heads in 31 buckets, bfloat 122 (81): 17 + 104 + 5; four sequences of 1501 packed tokens, 12 heads, 3969 buckets
-// 109 (43): 14 + 85 + 7.  With the buckets found by every workgroup for its own heads, in a tile that its wavefronts shared, these were 144 and 239.
+// us (what reading the gradient takes at 5.0 TB/s): 4096 x 4096 pairs of 12 heads in 31 buckets, bfloat 116 (81): 16 + 97 + 5; four sequences of 1501 packed tokens, 12 heads, 3969 buckets
+// 100 (43): 14 + 82 + 7.  With the buckets found by every workgroup for its own heads, in a tile that its wavefronts shared, these were 144 and 239.
 constexpr int kRun = 8;                                            // keys of an item
 
 __host__ __device__ __forceinline__ int bins_of(int64_t held, int copies) { return (int)held * copies; }

@@ -5,8 +5,8 @@ trains on the pictures: group norm with an activation, a bias of attention for r
 The work is done by the library's HIP kernels, enqueued on the current stream (or `stream`, a hipStream_t as an integer); arguments are checked and handed on
 by the native module _train (csrc/pcr_bind.cpp).  A tensor on another stream than the one it was made on needs the caller's
 record_stream, as with any operator.  Wrong types, shapes or devices raise ValueError before anything is enqueued, what the library
-refuses raises PcrError.  rotate_axes, norm_rotate, distill_loss, group_norm, position_bias and dropout take part in automatic differentiation; a gradient is made on the stream of its forward pass.
-There are no derivatives of forward mode (ValueError), and no traces (RuntimeError)."""
+refuses raises PcrError.  rotate_axes, norm_rotate, distill_loss, group_norm, position_bias and dropout take part in automatic differentiation; a gradient is made on the
+stream of its forward pass.  There are no derivatives of forward mode (ValueError), and no traces (RuntimeError)."""
 import os
 
 import numpy as np
@@ -285,8 +285,8 @@ def position_bias(table, positions, buckets, key_positions=None, segments=None, 
     [buckets, heads] of float32 or of the result's type (dtype, or the table's); positions (and key_positions, where keys are not the queries' tokens: a single new
     token against all before it): integers [axes, tokens] or [axes, batch, tokens], as patch_rows gives them; buckets: int32 [axes, 2 * reach + 1] (position_buckets).
     The pair's bucket is the sum over the axes of buckets[axis, reach + difference], the difference key - query held between -reach and reach; outside of the table it has no
-    bias (0).  segments (and key_segments): int32 [tokens] or [batch, tokens], which of several packed sequences a token is of: pairs of different segments are -inf, rows
-    of queries whose segment is below 0 (padding) are 0.  out: where to, keys contiguous (rows may be padded); given, it keeps the call out of automatic differentiation."""
+    bias (0).  segments (and key_segments): int32 [tokens] or [batch, tokens], which of several packed sequences a token is of: pairs of different segments are -inf (a
+    query of whose segment there is no key has a row of them), rows of queries whose segment is below 0 (padding) are 0.  out: where to, keys contiguous (rows may be padded); given, it keeps the call out of automatic differentiation."""
     kind = -1 if dtype is None else _TYPES.get(dtype, 3)
     if out is None and torch.is_grad_enabled() and getattr(table, "requires_grad", False):
         return _call(stream, _PositionBias.apply, table, positions, buckets, key_positions, segments, key_segments, kind)
