@@ -13,13 +13,14 @@ struct NormArgs {
     const void* x; const void* grad; const void* weight; const void* bias; void* out;
     float* stats;                                                  // [image][group][2]: m, r
     float* part;                                                   // [image][chunk][group][2]: mean and sum of squares around it, or sums of h w and h w u
-    float* sums;                                                   // [image][chunk][channel][2]: sums of h u and h
+    float* sums;                                                   // [image][chunk][channel][2]: sums of h u and h (one pass: of a workgroup's pictures)
     float* joined;                                                 // [image][group][2]: the chunks' sums of h w and h w u, by the number of values
     int64_t images, pixels, x_image, x_pixel, grad_image, grad_pixel, out_image, out_pixel;
     int64_t chunk;                                                 // pixels of a workgroup
     int64_t begin;                                                 // workgroups of earlier launches
     int chunks, channels, groups, each, activation, weight_float;  // each: channels of a group
-    int block, blocks;                                             // one pass: channels of a workgroup, workgroups of a picture
+    int block, blocks, pack, turns;                                // one pass: channels of a workgroup, workgroups of a picture; pictures of a workgroup side by side (its threads divided
+                                                                   // among them), and one after another
     float eps;
 };
 
@@ -99,19 +100,21 @@ template <int KIND, bool ONE, int V, int N> __device__ __forceinline__ void slop
 }
 
 // Sums over a workgroup's lanes of pixels (values[lane][unit], `units` of them from `first` on) and over the `each` units of a group, added to total[group].
-// A group's team of threads adds in a fixed order, then their sums are joined; all threads of the workgroup are needed.
-__device__ __forceinline__ void group_totals(const float* values, float* total, int lanes, int units, int first, int each, int groups_from, int groups_to) {
-    const int n = groups_to - groups_from, threads = (int)blockDim.x;
+// A group's team of threads adds in a fixed order, then their sums are joined; all of `threads` threads, a power of two of them, are needed.
+__device__ __forceinline__ void group_totals(const float* values, float* total, int lanes, int units, int first, int each, int groups_from, int groups_to, int thread, int threads) {
+    const int n = groups_to - groups_from;
     int team = 64;
     while (team > 1 && team * n > threads) team >>= 1;
     for (int g0 = 0; g0 < n; g0 += threads / team) {
-        const int g = g0 + threadIdx.x / team, member = threadIdx.x & (team - 1);
+        const int g = g0 + thread / team, member = thread & (team - 1);
         float sum = 0.f;
         if (g < n) {
             const int c0 = max((groups_from + g) * each - first, 0), c1 = min((groups_from + g + 1) * each - first, units), width = c1 - c0;
             if (width == units) {                                  // (one group: everything)
+#pragma unroll 4
                 for (int e = member; e < lanes * width; e += team) sum += values[e];
             } else if (width == 1) {
+#pragma unroll 4
                 for (int lane = member; lane < lanes; lane += team) sum += values[lane * units + c0];
             } else {
                 int lane = member / width, c = member - lane * width;
@@ -144,22 +147,27 @@ template <typename T, int V> __device__ __forceinline__ void load_parameters(con
 // runs.  us: 64 pictures of 14 x 14 x 256, bfloat 8.3 (2.6 at 5.0 TB/s), the gradient 15 (3.9), one of 14 x 14 x 64 5.7: the launch, and loads, sums and stores of a workgroup, which
 // follow each other, bound it.  The workgroups of a picture run on one die (blockIdx modulo 8 goes round the dies), where they find in its cache what lies beside their own channels in a line.
 struct Slab {
-    int64_t image;
+    int64_t image, row;                                            // the first of the thread's pictures; where its workgroup's sums go
     int first, channels, columns, lanes, lane, column;             // of the workgroup's channels; runs of a pixel; threads to a run, the thread's place
+    int slot, thread, threads;                                     // of the workgroup's pictures; of the picture's threads
     bool works;
 };
 __device__ __forceinline__ Slab slab_of(const NormArgs& A, int V) {
     Slab S;
     const int64_t at = blockIdx.x + A.begin;
-    const int dies = A.images % 8 ? 1 : 8;
+    const int dies = A.images % 8 || A.blocks == 1 ? 1 : 8;
     const int64_t row = at / dies, turn = row / A.blocks;
-    S.image = turn * dies + at % dies;
+    S.threads = (int)blockDim.x / A.pack;
+    S.slot = threadIdx.x / S.threads;
+    S.thread = threadIdx.x & (S.threads - 1);
+    S.row = turn * dies + at % dies;
+    S.image = S.row * A.pack * A.turns + S.slot;
     S.first = (int)(row - turn * A.blocks) * A.block;
     S.channels = min(A.block, A.channels - S.first);
     S.columns = S.channels / V;
-    S.lanes = (int)blockDim.x / S.columns;
-    S.lane = threadIdx.x / S.columns;
-    S.column = threadIdx.x - S.lane * S.columns;
+    S.lanes = S.threads / S.columns;
+    S.lane = S.thread / S.columns;
+    S.column = S.thread - S.lane * S.columns;
     S.works = S.lane < S.lanes;
     return S;
 }
@@ -192,177 +200,212 @@ template <typename T, int V, int K> __device__ __forceinline__ void hold(Held<T,
         if (k * S.lanes < pixels) h[k].v = reinterpret_cast<const typename Run<T, V>::Loose*>(from + (int64_t)min(S.lane + k * S.lanes, pixels - 1) * pixel)->v;
 }
 
-template <typename T, int V, int K, int THREADS, bool ONE> __global__ __launch_bounds__(THREADS) void k_norm_held(NormArgs A) {
+// MANY: a workgroup has several pictures, A.pack side by side and A.turns after one another.
+template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS) void k_norm_held(NormArgs A) {
     extern __shared__ __attribute__((aligned(16))) float shared[];
-    float* values = shared;                                        // [lane][unit]
-    float* total = shared + THREADS * (ONE ? 1 : V);               // [group of the block]: sums; then means; then r
     const Slab S = slab_of(A, V);
-    const int groups = S.channels / A.each, pixels = (int)A.pixels, c = S.first + S.column * V, unit_groups = ONE ? A.each / V : A.each;
-    Held<T, V> x[K];
-    hold<T, V, K>(x, (const T*)A.x + S.image * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
-    for (int g = threadIdx.x; g < 3 * groups; g += THREADS) total[g] = 0.f;
-    float sum[V];
-#pragma unroll
-    for (int i = 0; i < V; i++) sum[i] = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; k++)
-        if (k * S.lanes < pixels) {
-            float a[V];
-            take(x[k], a);
-            if (S.lane + k * S.lanes < pixels) {
-#pragma unroll
-                for (int i = 0; i < V; i++) sum[i] += a[i];
-            }
-        }
+    const int groups = S.channels / A.each;
+    float* values = shared + S.slot * S.threads * (ONE ? 1 : V);   // [lane][unit]
+    float* total = shared + THREADS * (ONE ? 1 : V) + S.slot * 3 * groups;     // [group of the block]: sums; then means; then r
+    const int pixels = (int)A.pixels, c = S.first + S.column * V, unit_groups = ONE ? A.each / V : A.each;
+    constexpr bool EARLY = THREADS == 256;                         // (workgroups of 512 threads have registers for the parameters when the sums are made)
+    float w[V], b[V];
+    auto parameters = [&]() {
+        load_parameters<T, V>(A, A.weight, S.works ? c : S.first, 1.f, w);
+        load_parameters<T, V>(A, A.bias, S.works ? c : S.first, 0.f, b);
+    };
     const int units = value_units<V, ONE>(S.channels);
     const float inv = 1.f / ((float)pixels * A.each);
-    put_values<V, ONE>(values, S, sum);
-    __syncthreads();
-    group_totals(values, total, S.lanes, units, 0, unit_groups, 0, groups);
-    __syncthreads();
-    float m[ONE ? 1 : V];
+    for (int turn = 0;; turn++) {
+        const int64_t image = S.image + turn * A.pack;
+        const bool last = !MANY || turn + 1 == A.turns, there = image < A.images;
+        Held<T, V> x[K];
+        hold<T, V, K>(x, (const T*)A.x + min(image, A.images - 1) * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
+        if (EARLY && turn == 0) parameters();
+        for (int g = S.thread; g < 3 * groups; g += S.threads) total[g] = 0.f;
+        float sum[V];
 #pragma unroll
-    for (int i = 0; i < (ONE ? 1 : V); i++) m[i] = S.works ? total[(S.column * V + i) / A.each] * inv : 0.f;
-#pragma unroll
-    for (int i = 0; i < V; i++) sum[i] = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; k++)
-        if (k * S.lanes < pixels) {
-            float a[V];
-            take(x[k], a);
-            if (S.lane + k * S.lanes < pixels) {
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const float d = a[i] - m[ONE ? 0 : i];
-                    sum[i] = __builtin_fmaf(d, d, sum[i]);
-                }
-            }
-        }
-    put_values<V, ONE>(values, S, sum);
-    __syncthreads();
-    group_totals(values, total + groups, S.lanes, units, 0, unit_groups, 0, groups);
-    __syncthreads();
-    for (int g = threadIdx.x; g < groups; g += THREADS) {
-        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(total[groups + g], inv, A.eps));
-        total[2 * groups + g] = r;
-        float* to = A.stats + (S.image * A.groups + S.first / A.each + g) * 2;
-        to[0] = total[g] * inv;
-        to[1] = r;
-    }
-    __syncthreads();
-    if (!S.works) return;
-    float w[V], b[V];
-    load_parameters<T, V>(A, A.weight, c, 1.f, w);
-    load_parameters<T, V>(A, A.bias, c, 0.f, b);
-#pragma unroll
-    for (int i = 0; i < V; i++) w[i] *= total[2 * groups + (S.column * V + i) / A.each];
-    T* out = (T*)A.out + S.image * A.out_image + c;
-    with_kind(A.activation, [&](auto kind) {
-#pragma unroll
-        for (int k = 0; k < K; k++) {
-            const int p = S.lane + k * S.lanes;
-            if (p < pixels) {
-                float a[V];
-                take(x[k], a);
-#pragma unroll
-                for (int i = 0; i < V; i++) a[i] = __builtin_fmaf(a[i] - m[ONE ? 0 : i], w[i], b[i]);
-                activate<decltype(kind)::value>(a);
-                store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
-            }
-            one_after_another();
-        }
-    });
-}
-
-// The gradient: sums by channels of h u and h, from which those of the groups are made.
-template <typename T, int V, int K, int THREADS, bool ONE> __global__ __launch_bounds__(THREADS) void k_norm_back_held(NormArgs A) {
-    extern __shared__ __attribute__((aligned(16))) float shared[];
-    float* values = shared;                                        // [lane][channel]
-    float* total = shared + THREADS * V;                           // [2][channel of the block]; [2][group]
-    const Slab S = slab_of(A, V);
-    const int groups = S.channels / A.each, pixels = (int)A.pixels, c = S.first + S.column * V;
-    Held<T, V> x[K], h[K];
-    hold<T, V, K>(x, (const T*)A.x + S.image * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
-    hold<T, V, K>(h, (const T*)A.grad + S.image * A.grad_image + (S.works ? c : S.first), A.grad_pixel, S, pixels);
-    for (int e = threadIdx.x; e < 2 * (S.channels + groups); e += THREADS) total[e] = 0.f;
-    float w[V], b[V], m[ONE ? 1 : V], r[ONE ? 1 : V], s[2][V];
-    load_parameters<T, V>(A, A.weight, S.works ? c : S.first, 1.f, w);
-    load_parameters<T, V>(A, A.bias, S.works ? c : S.first, 0.f, b);
-#pragma unroll
-    for (int i = 0; i < (ONE ? 1 : V); i++) {
-        const float* q = A.stats + (S.image * A.groups + ((S.works ? c : S.first) + i) / A.each) * 2;
-        m[i] = q[0];
-        r[i] = q[1];
-    }
-#pragma unroll
-    for (int i = 0; i < V; i++) s[0][i] = s[1][i] = 0.f;
-    with_kind(A.activation, [&](auto kind) {
+        for (int i = 0; i < V; i++) sum[i] = 0.f;
 #pragma unroll
         for (int k = 0; k < K; k++)
             if (k * S.lanes < pixels) {
-                float a[V], g[V];
+                float a[V];
                 take(x[k], a);
-                take(h[k], g);
-                slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
+                if (S.lane + k * S.lanes < pixels) {
+#pragma unroll
+                    for (int i = 0; i < V; i++) sum[i] += a[i];
+                }
+            }
+        put_values<V, ONE>(values, S, sum);
+        __syncthreads();
+        group_totals(values, total, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
+        __syncthreads();
+        float m[ONE ? 1 : V];
+#pragma unroll
+        for (int i = 0; i < (ONE ? 1 : V); i++) m[i] = S.works ? total[(S.column * V + i) / A.each] * inv : 0.f;
+#pragma unroll
+        for (int i = 0; i < V; i++) sum[i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; k++)
+            if (k * S.lanes < pixels) {
+                float a[V];
+                take(x[k], a);
                 if (S.lane + k * S.lanes < pixels) {
 #pragma unroll
                     for (int i = 0; i < V; i++) {
-                        s[0][i] = __builtin_fmaf(g[i], a[i], s[0][i]);
-                        s[1][i] += g[i];
+                        const float d = a[i] - m[ONE ? 0 : i];
+                        sum[i] = __builtin_fmaf(d, d, sum[i]);
                     }
                 }
-                one_after_another();
             }
-    });
-#pragma unroll
-    for (int z = 0; z < 2; z++) {
-        put_values<V, false>(values, S, s[z]);
+        put_values<V, ONE>(values, S, sum);
         __syncthreads();
-        group_totals(values, total + z * S.channels, S.lanes, S.channels, 0, 1, 0, S.channels);
+        group_totals(values, total + groups, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
         __syncthreads();
-    }
-    // Those of the groups, from their channels'.
-    float* of_group = total + 2 * S.channels;
-    const float inv = 1.f / ((float)pixels * A.each);
-    for (int e = threadIdx.x; e < S.channels; e += THREADS) {
-        ((float2*)A.sums)[S.image * A.channels + S.first + e] = make_float2(total[e], total[S.channels + e]);
-        float by[1];
-        load_parameters<T, 1>(A, A.weight, S.first + e, 1.f, by);
-        total[e] *= by[0] * inv;
-        total[S.channels + e] *= by[0] * inv;
-    }
-    __syncthreads();
-    group_totals(total, of_group, 1, S.channels, 0, A.each, 0, groups);
-    group_totals(total + S.channels, of_group + groups, 1, S.channels, 0, A.each, 0, groups);
-    __syncthreads();
-    if (!S.works) return;
-    float su[ONE ? 1 : V], sh[ONE ? 1 : V];
-#pragma unroll
-    for (int i = 0; i < (ONE ? 1 : V); i++) {
-        const int g = (S.column * V + i) / A.each;
-        su[i] = of_group[g];
-        sh[i] = of_group[groups + g];
-    }
-    T* out = (T*)A.out + S.image * A.out_image + c;
-    with_kind(A.activation, [&](auto kind) {
-#pragma unroll
-        for (int k = 0; k < K; k++) {
-            const int p = S.lane + k * S.lanes;
-            if (p < pixels) {
-                float a[V], g[V];
-                take(x[k], a);
-                take(h[k], g);
-                slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const int j = ONE ? 0 : i;
-                    a[i] = r[j] * (__builtin_fmaf(g[i], w[i], -sh[j]) - a[i] * su[j]);
-                }
-                store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
-            }
-            one_after_another();
+        for (int g = S.thread; g < groups; g += S.threads) {
+            const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(total[groups + g], inv, A.eps));
+            total[2 * groups + g] = r;
+            float2* to = (float2*)A.stats + image * A.groups + S.first / A.each + g;
+            if (there) *to = make_float2(total[g] * inv, r);
         }
-    });
+        __syncthreads();
+        if (S.works && there) {
+            float by[V];
+            if (!EARLY) parameters();
+#pragma unroll
+            for (int i = 0; i < V; i++) by[i] = w[i] * total[2 * groups + (S.column * V + i) / A.each];
+            T* out = (T*)A.out + image * A.out_image + c;
+            with_kind(A.activation, [&](auto kind) {
+#pragma unroll
+                for (int k = 0; k < K; k++) {
+                    const int p = S.lane + k * S.lanes;
+                    if (p < pixels) {
+                        float a[V];
+                        take(x[k], a);
+#pragma unroll
+                        for (int i = 0; i < V; i++) a[i] = __builtin_fmaf(a[i] - m[ONE ? 0 : i], by[i], b[i]);
+                        activate<decltype(kind)::value>(a);
+                        store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
+                    }
+                    one_after_another();
+                }
+            });
+        }
+        if (last) break;
+        __syncthreads();
+    }
+}
+
+// The gradient.  What a thread has summed over its pictures, by channels, is summed over the workgroup at the end.
+template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS) void k_norm_back_held(NormArgs A) {
+    extern __shared__ __attribute__((aligned(16))) float shared[];
+    const Slab S = slab_of(A, V);
+    const int groups = S.channels / A.each, pixels = (int)A.pixels, c = S.first + S.column * V, unit_groups = ONE ? A.each / V : A.each;
+    const int units = value_units<V, ONE>(S.channels), half = S.threads * (ONE ? 1 : V);
+    float* values = shared + S.slot * 2 * half;                    // [2][lane][unit]; at the end [lane of all pictures][channel]
+    float* total = shared + 2 * THREADS * (ONE ? 1 : V) + S.slot * 2 * groups;             // [2][group]
+    float w[V], b[V], sums[2][V];                                  // sums: of h u and h
+    load_parameters<T, V>(A, A.weight, S.works ? c : S.first, 1.f, w);
+    load_parameters<T, V>(A, A.bias, S.works ? c : S.first, 0.f, b);
+#pragma unroll
+    for (int i = 0; i < V; i++) sums[0][i] = sums[1][i] = 0.f;
+    const float inv = 1.f / ((float)pixels * A.each);
+    for (int turn = 0;; turn++) {
+        const int64_t image = S.image + turn * A.pack, at = min(image, A.images - 1);
+        const bool last = !MANY || turn + 1 == A.turns, there = image < A.images;
+        Held<T, V> x[K], h[K];
+        hold<T, V, K>(x, (const T*)A.x + at * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
+        hold<T, V, K>(h, (const T*)A.grad + at * A.grad_image + (S.works ? c : S.first), A.grad_pixel, S, pixels);
+        for (int e = S.thread; e < 2 * groups; e += S.threads) total[e] = 0.f;
+        float m[ONE ? 1 : V], r[ONE ? 1 : V], s[2][V];
+#pragma unroll
+        for (int i = 0; i < (ONE ? 1 : V); i++) {
+            const float2 of = ((const float2*)A.stats)[at * A.groups + ((S.works ? c : S.first) + i) / A.each];
+            m[i] = of.x;
+            r[i] = of.y;
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) s[0][i] = s[1][i] = 0.f;
+        with_kind(A.activation, [&](auto kind) {
+#pragma unroll
+            for (int k = 0; k < K; k++)
+                if (k * S.lanes < pixels) {
+                    float a[V], g[V];
+                    take(x[k], a);
+                    take(h[k], g);
+                    slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
+                    if (S.lane + k * S.lanes < pixels) {
+#pragma unroll
+                        for (int i = 0; i < V; i++) {
+                            s[0][i] = __builtin_fmaf(g[i], a[i], s[0][i]);
+                            s[1][i] += g[i];
+                        }
+                    }
+                    one_after_another();
+                }
+        });
+        // The groups'.
+#pragma unroll
+        for (int z = 0; z < 2; z++) {
+            float weighted[V];
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                if (there) sums[z][i] += s[z][i];
+                weighted[i] = s[z][i] * w[i];
+            }
+            put_values<V, ONE>(values + z * half, S, weighted);
+        }
+        __syncthreads();
+        group_totals(values, total, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
+        group_totals(values + half, total + groups, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
+        __syncthreads();
+        if (S.works && there) {
+            float su[ONE ? 1 : V], sh[ONE ? 1 : V];
+#pragma unroll
+            for (int i = 0; i < (ONE ? 1 : V); i++) {
+                const int g = (S.column * V + i) / A.each;
+                su[i] = total[g] * inv;
+                sh[i] = total[groups + g] * inv;
+            }
+            T* out = (T*)A.out + image * A.out_image + c;
+            with_kind(A.activation, [&](auto kind) {
+#pragma unroll
+                for (int k = 0; k < K; k++) {
+                    const int p = S.lane + k * S.lanes;
+                    if (p < pixels) {
+                        float a[V], g[V];
+                        take(x[k], a);
+                        take(h[k], g);
+                        slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
+#pragma unroll
+                        for (int i = 0; i < V; i++) {
+                            const int j = ONE ? 0 : i;
+                            a[i] = r[j] * (__builtin_fmaf(g[i], w[i], -sh[j]) - a[i] * su[j]);
+                        }
+                        store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
+                    }
+                    one_after_another();
+                }
+            });
+        }
+        if (last) break;
+        __syncthreads();
+    }
+    // The channels'.
+    float* channel = shared + THREADS * V;                         // [channel]
+    float2* to = (float2*)A.sums + S.row * A.channels + S.first;
+    for (int z = 0; z < 2; z++) {
+        __syncthreads();
+        if (S.works) {
+#pragma unroll
+            for (int i = 0; i < V; i++) shared[((S.slot * S.lanes + S.lane) * S.columns + S.column) * V + i] = z ? sums[1][i] : sums[0][i];
+        }
+        for (int e = threadIdx.x; e < S.channels; e += THREADS) channel[e] = 0.f;
+        __syncthreads();
+        group_totals(shared, channel, (MANY ? A.pack : 1) * S.lanes, S.channels, 0, 1, 0, S.channels, (int)threadIdx.x, THREADS);
+        __syncthreads();
+        for (int e = threadIdx.x; e < S.channels; e += THREADS) (z ? to[e].y : to[e].x) = channel[e];
+    }
 }
 
 // ---- in two passes ----
@@ -469,7 +512,7 @@ template <typename T, int V> __global__ __launch_bounds__(256) void k_norm_sums(
                 }
             }
             __syncthreads();
-            group_totals(values, total, C.lanes, width, first, A.each, g0, g1);
+            group_totals(values, total, C.lanes, width, first, A.each, g0, g1, (int)threadIdx.x, kNormThreads);
             __syncthreads();
         }
         const float count = (float)(K.end - K.first) * A.each;
@@ -662,7 +705,7 @@ template <typename T, int V, bool ONE> __global__ __launch_bounds__(256) void k_
                 for (int i = 0; i < V; i++) values[C.lane * width + C.column * V + i] = s[z][i];
             }
             __syncthreads();
-            group_totals(values, channel + z * width, C.lanes, width, 0, 1, 0, width);
+            group_totals(values, channel + z * width, C.lanes, width, 0, 1, 0, width, (int)threadIdx.x, kNormThreads);
             __syncthreads();
         }
         // The groups' from their channels'.
@@ -675,8 +718,8 @@ template <typename T, int V, bool ONE> __global__ __launch_bounds__(256) void k_
             channel[width + e] *= by[0];
         }
         __syncthreads();
-        group_totals(channel + width, total, 1, width, first, A.each, g0, g1);
-        group_totals(channel, total + A.groups, 1, width, first, A.each, g0, g1);
+        group_totals(channel + width, total, 1, width, first, A.each, g0, g1, (int)threadIdx.x, kNormThreads);
+        group_totals(channel, total + A.groups, 1, width, first, A.each, g0, g1, (int)threadIdx.x, kNormThreads);
         __syncthreads();
     }
     float2* part = (float2*)A.part + (blockIdx.x + A.begin) * A.groups;

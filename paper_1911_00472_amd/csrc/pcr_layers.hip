@@ -39,10 +39,15 @@ int check_norm(const pcr_group_norm* N, bool back) {
     return PCR_OK;
 }
 
+constexpr int64_t kSmallImages = 2048;                           // workgroups at least, where pictures share one
+
 struct NormPlan {
     int64_t chunk;
     int chunks, run;
-    int held, threads, block, blocks;                          // one pass: runs that a thread holds (0: two passes), threads and channels of a workgroup, workgroups of a picture
+    int held, threads, block, blocks, pack;                    // one pass: runs that a thread holds (0: two passes), threads and channels of a workgroup, workgroups of a picture, pictures of one
+    int turns;
+    bool many;
+    int64_t rows;                                              // of channels' sums
     size_t part_bytes, sums_bytes, joined_bytes;
     size_t bytes() const { return part_bytes + sums_bytes + joined_bytes; }
 };
@@ -67,6 +72,11 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
         const int64_t of_unit = N->pixels * (unit / P.run);
         while (many > 1 && of_unit * many > most) many >>= 1;
         many = std::min(many, units);
+        // Many small pictures: a workgroup has whole ones, several where a picture has fewer runs than a workgroup's threads hold (one each, two of fewer than 16 bytes), and some after one another; the channels' sums of all of them are one row.  (us with one picture, and one piece of 128 bytes of its
+        // channels, to a workgroup: 32768 of a pixel of 1024 channels 114, their gradient 440; 100000 of 2 x 2 x 32 324 and 788.)
+        const int64_t runs_held = P.run * size < 16 ? 2 : 1;
+        P.many = N->images >= kSmallImages && of_unit * units <= 256 * runs_held && units * unit / P.run <= 256;
+        if (P.many) many = units;
         const int64_t columns = many * unit / P.run;
         if (of_unit * many <= most && columns <= 256) {
             P.block = (int)(many * unit);
@@ -75,6 +85,10 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
             P.threads = P.run * size < 16 || need(256) <= 4 ? 256 : 512;
             for (P.held = 1; P.held < need(P.threads);) P.held <<= 1;
             if (P.held > (P.run * size < 16 || back ? 8 : 16)) P.held = 0;
+            P.pack = 1;
+            if (P.many)
+                while (N->images >= 2 * P.pack * kSmallImages && 128 / P.pack >= columns && need(128 / P.pack) <= runs_held) P.pack *= 2;
+            P.turns = P.many ? (int)std::min<int64_t>(16, std::max<int64_t>(1, N->images / (P.pack * kSmallImages))) : 1;
             // (Rows of 16 bytes: 64 pictures of 56 x 56 x 256 take 66 us, and 65 in two passes; their gradient 201, and 113.)
             if (P.block < N->channels && P.block * (int64_t)size < 32 && N->images * N->pixels * N->channels * (int64_t)size > (64 << 20)) P.held = 0;
         }
@@ -82,7 +96,8 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
     if (P.held) {
         P.chunk = N->pixels;
         P.chunks = 1;
-        P.sums_bytes = back ? (size_t)N->images * N->channels * 2 * sizeof(float) : 0;
+        P.rows = (N->images + P.pack * P.turns - 1) / (P.pack * P.turns);
+        P.sums_bytes = back ? (size_t)P.rows * N->channels * 2 * sizeof(float) : 0;
         return P;
     }
     // Two passes.  Chunks of a picture's pixels: 768 workgroups in all, 512 of a gradient, of 16 pixels to a thread at least.  (us with 512 / 768 / 1024 / 2048: 64 pictures of
@@ -93,7 +108,8 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
     P.chunk = ((N->pixels + chunks - 1) / chunks + step - 1) / step * step;
     P.chunks = N->pixels ? (int)((N->pixels + P.chunk - 1) / P.chunk) : 0;
     P.part_bytes = (size_t)N->images * P.chunks * N->groups * 2 * sizeof(float);
-    P.sums_bytes = back ? (size_t)N->images * P.chunks * N->channels * 2 * sizeof(float) : 0;
+    P.rows = N->images * P.chunks;
+    P.sums_bytes = back ? (size_t)P.rows * N->channels * 2 * sizeof(float) : 0;
     P.joined_bytes = back && P.chunks > kMergedChunks ? (size_t)N->images * N->groups * 2 * sizeof(float) : 0;
     return P;
 }
@@ -104,7 +120,7 @@ NormArgs norm_args(const pcr_group_norm* N, const NormPlan& P, void* d_work) {
     A.images = N->images; A.pixels = N->pixels;
     A.x_image = N->x_image; A.x_pixel = N->x_pixel; A.grad_image = N->grad_image; A.grad_pixel = N->grad_pixel; A.out_image = N->out_image; A.out_pixel = N->out_pixel;
     A.chunk = P.chunk; A.chunks = P.chunks; A.channels = (int)N->channels; A.groups = N->groups; A.each = (int)(N->channels / N->groups);
-    A.block = P.block; A.blocks = P.blocks;
+    A.block = P.block; A.blocks = P.blocks; A.pack = P.pack; A.turns = P.turns;
     A.activation = N->activation; A.weight_float = N->weight_dtype == PCR_FLOAT; A.eps = N->eps;
     return A;
 }
@@ -124,30 +140,33 @@ template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, N
     with_run(N->dtype, P.run, [&](auto t, auto v) {
         typedef decltype(t) T;
         constexpr int V = decltype(v)::value;
-        auto launch = [&](auto k, auto threads, auto in_one) {
+        auto launch = [&](auto k, auto threads, auto in_one, auto of_many) {
             constexpr int K = decltype(k)::value, THREADS = decltype(threads)::value;
-            constexpr bool ONE = decltype(in_one)::value;
-            const size_t of_block = A.block + A.block / A.each;
-            const size_t lds = BACK ? (THREADS * V + 2 * of_block) * sizeof(float) : (THREADS * (ONE ? 1 : V) + 3 * (A.block / A.each)) * sizeof(float);
-            in_ranges(A.images * A.blocks, THREADS, [&](int64_t begin, unsigned groups) {
+            constexpr bool ONE = decltype(in_one)::value, MANY = decltype(of_many)::value;
+            const size_t groups = A.block / A.each, values = THREADS * (ONE ? 1 : V);
+            const size_t lds = (BACK ? std::max(2 * values + A.pack * 2 * groups, (size_t)THREADS * V + A.block) : values + A.pack * 3 * groups) * sizeof(float);
+            in_ranges(P.rows * A.blocks, THREADS, [&](int64_t begin, unsigned workgroups) {
                 A.begin = begin;
                 if constexpr (BACK) {
-                    ok = ok && allow_lds(k_norm_back_held<T, V, K, THREADS, ONE>, lds);
-                    if (ok) hipLaunchKernelGGL((k_norm_back_held<T, V, K, THREADS, ONE>), dim3(groups), dim3(THREADS), lds, s, A);
+                    ok = ok && allow_lds(k_norm_back_held<T, V, K, THREADS, ONE, MANY>, lds);
+                    if (ok) hipLaunchKernelGGL((k_norm_back_held<T, V, K, THREADS, ONE, MANY>), dim3(workgroups), dim3(THREADS), lds, s, A);
                 } else {
-                    ok = ok && allow_lds(k_norm_held<T, V, K, THREADS, ONE>, lds);
-                    if (ok) hipLaunchKernelGGL((k_norm_held<T, V, K, THREADS, ONE>), dim3(groups), dim3(THREADS), lds, s, A);
+                    ok = ok && allow_lds(k_norm_held<T, V, K, THREADS, ONE, MANY>, lds);
+                    if (ok) hipLaunchKernelGGL((k_norm_held<T, V, K, THREADS, ONE, MANY>), dim3(workgroups), dim3(THREADS), lds, s, A);
                 }
             });
         };
-        auto by_one = [&](auto k, auto threads) {
-            if (one) launch(k, threads, std::true_type());
-            else if constexpr (V > 1) launch(k, threads, std::false_type());
+        auto by_one = [&](auto k, auto threads, auto of_many) {
+            if (one) launch(k, threads, std::true_type(), of_many);
+            else if constexpr (V > 1) launch(k, threads, std::false_type(), of_many);
         };
-        if constexpr (V * sizeof(T) < 16) by_one(Int<8>(), Int<256>());
-        else if (P.threads == 256) by_one(Int<4>(), Int<256>());
-        else if (P.held <= 8) by_one(Int<8>(), Int<512>());
-        else if constexpr (!BACK) by_one(Int<16>(), Int<512>());
+        constexpr bool WHOLE = V * sizeof(T) == 16;
+        if (P.many) by_one(Int<WHOLE ? 1 : 2>(), Int<256>(), std::true_type());
+        else if (P.threads == 256) by_one(Int<WHOLE ? 4 : 8>(), Int<256>(), std::false_type());
+        else if constexpr (WHOLE) {
+            if (P.held <= 8) by_one(Int<8>(), Int<512>(), std::false_type());
+            else if constexpr (!BACK) by_one(Int<16>(), Int<512>(), std::false_type());
+        }
     });
     return ok;
 }
@@ -313,7 +332,7 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
             });
         });
     if (norm->weight_grad || norm->bias_grad) {
-        NormWeightSums W = {A.sums, norm->weight_grad, norm->bias_grad, none ? 0 : A.images * A.chunks, A.channels};
+        NormWeightSums W = {A.sums, norm->weight_grad, norm->bias_grad, none ? 0 : P.rows, A.channels};
         hipLaunchKernelGGL(k_norm_weight_sums, dim3((2 * A.channels + 15) / 16), dim3(1024), 0, s, W);
     }
     return launched();

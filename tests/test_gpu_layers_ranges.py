@@ -18,25 +18,63 @@ def generator(seed):
     return gen
 
 
-@pytest.mark.parametrize("pixels,images", [(2, 2 ** 24 + 8), (1, 2 ** 24 + 3)])
-def test_more_pictures_than_a_launch_has_workgroups(pixels, images):
-    """2^24 workgroups of 256 threads and some more: pictures of two channels, with a group each.  A group has one or two values, a and b: m = (a + b) / 2, u = +-d / sqrt(d^2 + eps) for d = (a - b) / 2."""
-    x = torch.randn((images, pixels, 2), generator=generator(1), device="cuda").bfloat16()
-    y, stats = pkg.group_norm_forward(x, 2)
-    dx, dw, _ = pkg.group_norm_backward(x, x, 2, torch.ones(2, device="cuda"), None, stats)
-    total = torch.zeros(2, dtype=torch.float64, device="cuda")
-    for i in range(0, images, 2 ** 22):
-        v = x[i:i + 2 ** 22].double()
+def check_pairs(x, y, dx, dw):
+    """Pictures of one or two pixels, a group to each channel: u = (x - m) r, and the gradient x of y times 1."""
+    images, pixels = x.shape[:2]
+    half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}[x.dtype]
+    total = torch.zeros(x.shape[2], dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(total)
+    step = max(1, 2 ** 23 // x.shape[2])
+    for i in range(0, images, step):
+        v = x[i:i + step].double()
         m = v.mean(1, keepdim=True)
         r = ((v - m).square().mean(1, keepdim=True) + EPS) ** -0.5
         u = (v - m) * r
         # (m to 2^-23 of the larger value, which is below 2^3: u to 2^-20 r)
-        assert bool(((y[i:i + 2 ** 22].double() - u).abs() <= 2.0 ** -8 * u.abs() + 2.0 ** -20 * r + 2.0 ** -20).all()), i
+        assert bool(((y[i:i + step].double() - u).abs() <= half * u.abs() + 2.0 ** -20 * r + 2.0 ** -20).all()), i
         total += (v * u).sum((0, 1))
+        size += (v * u).abs().sum((0, 1)) + 2.0 ** -6 * (v.abs() * r).sum((0, 1))
         want = r * (v - m - u * (v * u).mean(1, keepdim=True))
-        assert bool(((dx[i:i + 2 ** 22].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -14 * r * (v.abs() + v.abs().mean(1, keepdim=True)) * (1 + 2.0 ** -4 * r) + 2.0 ** -100).all()), i
-    if pixels == 2:
-        assert bool(((dw.double() - total).abs() <= 2.0 ** -10 * total.abs()).all())
+        assert bool(((dx[i:i + step].double() - want).abs() <= half * want.abs() + 2.0 ** -14 * r * (v.abs() + v.abs().mean(1, keepdim=True)) * (1 + 2.0 ** -4 * r) + 2.0 ** -100).all()), i
+    assert bool(((dw.double() - total).abs() <= 2.0 ** -12 * size).all())
+
+
+@pytest.mark.parametrize("pixels,images", [(2, 2 ** 24 + 8), (1, 2 ** 24 + 3)])
+def test_millions_of_small_pictures(pixels, images):
+    """Hundreds of them to a workgroup, the last of them not full."""
+    x = torch.randn((images, pixels, 2), generator=generator(1), device="cuda").bfloat16()
+    y, stats = pkg.group_norm_forward(x, 2)
+    dx, dw, _ = pkg.group_norm_backward(x, x, 2, torch.ones(2, device="cuda"), None, stats)
+    check_pairs(x, y, dx, dw)
+
+
+def test_more_workgroups_than_a_launch_has():
+    """2^24 workgroups of 256 threads and 128 more: pictures of two pixels of 4096 channels, 32 channels to a workgroup."""
+    x = torch.randn((2 ** 17 + 1, 2, 4096), generator=generator(8), device="cuda")
+    y, stats = pkg.group_norm_forward(x, 4096)
+    dx, dw, _ = pkg.group_norm_backward(x, x, 4096, torch.ones(4096, device="cuda"), None, stats)
+    check_pairs(x, y, dx, dw)
+
+
+@pytest.mark.parametrize("dtype", norm.TYPES)
+@pytest.mark.parametrize("images", [2047, 2048, 4095, 4096, 8193, 40001])
+@pytest.mark.parametrize("pixels,C,G", [(1, 8, 1), (1, 1, 1), (1, 24, 3), (4, 32, 4), (1, 1024, 1), (1, 520, 65), (3, 12, 2), (2, 6, 3), (7, 40, 5), (9, 16, 16), (1, 2000, 10), (5, 3, 1), (2, 90, 9)])
+def test_many_small_pictures(pixels, C, G, images, dtype):
+    """Several pictures of a workgroup, whose threads are divided among them, or one of all channels."""
+    if images * pixels * C > 12e6:
+        images = max(2048, int(12e6 / pixels / C)) + 1
+    gen = generator(images + C)
+    x = norm.make((images, pixels, C), dtype, gen)
+    w, b = (torch.randn(C, generator=gen, device="cuda") for _ in range(2))
+    kind = norm.ACTIVATIONS[(images + C) % 4]
+    y, stats = pkg.group_norm_forward(x, G, w, b, EPS, kind)
+    norm.check_forward(x, G, w, b, EPS, kind, y, stats)
+    g = torch.randn(x.shape, generator=gen, device="cuda").to(dtype)
+    found = pkg.group_norm_backward(g, x, G, w, b, stats, kind)
+    norm.check_backward(g, x, G, w, b, stats, kind, *found)
+    inside = torch.full((images + 3, pixels, C), 7.0, device="cuda").to(dtype)          # (what lies behind the last picture stays as it was)
+    pkg.group_norm_forward(x, G, w, b, EPS, kind, out=inside[:images])
+    assert torch.equal(inside[:images], y) and bool((inside[images:] == 7).all())
 
 
 def test_a_picture_of_more_than_2_to_the_32_values():
