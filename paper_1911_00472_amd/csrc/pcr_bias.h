@@ -205,7 +205,7 @@ template <typename T, int H, bool HELD, int AXES> __global__ __launch_bounds__(1
 // First every pair's bucket is found once for all heads (k_bias_places), as 16 bits; then the values are added by a kernel that reads both side by side, share by
 // share of the items (k_bias_bins), and the shares' sums are added in 64 bits (k_bias_sums).  Items are runs of eight keys here whatever the type.
 // us (what reading the gradient takes at 5.0 TB/s): 4096 x 4096 pairs of 12 heads in 31 buckets, bfloat 116 (81): 16 + 97 + 5; four sequences of 1501 packed tokens, 12 heads, 3969 buckets
-// 100 (43): 14 + 82 + 7.  With the buckets found by every workgroup for its own heads, in a tile that its wavefronts shared, these were 144 and 239.
+// 106 (43): 14 + 85 + 7.  With the buckets found by every workgroup for its own heads, in a tile that its wavefronts shared, these were 144 and 239.
 constexpr int kRun = 8;                                            // keys of an item
 
 __host__ __device__ __forceinline__ int bins_of(int64_t held, int copies) { return (int)held * copies; }

@@ -72,8 +72,9 @@ NormPlan plan_norm(const pcr_group_norm* N, bool back) {
         const int64_t of_unit = N->pixels * (unit / P.run);
         while (many > 1 && of_unit * many > most) many >>= 1;
         many = std::min(many, units);
-        // Many small pictures: a workgroup has whole ones, several where a picture has fewer runs than a workgroup's threads hold (one each, two of fewer than 16 bytes), and some after one another; the channels' sums of all of them are one row.  (us with one picture, and one piece of 128 bytes of its
-        // channels, to a workgroup: 32768 of a pixel of 1024 channels 114, their gradient 440; 100000 of 2 x 2 x 32 324 and 788.)
+        // Many small pictures: where a picture has no more runs than a workgroup's threads hold (one each, two of fewer than 16 bytes), it has whole ones, side by side and after one another,
+        // whose channels' sums are one row.  (us, with a picture or 128 bytes of its channels to a workgroup: 32768 of a pixel of 1024 channels 114, now 66, their gradient 440, 90;
+        // 100000 of 2 x 2 x 32 324, 29, and 788, 46.)
         const int64_t runs_held = P.run * size < 16 ? 2 : 1;
         P.many = N->images >= kSmallImages && of_unit * units <= 256 * runs_held && units * unit / P.run <= 256;
         if (P.many) many = units;
@@ -174,6 +175,7 @@ template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, N
 // ---- position bias ----
 
 constexpr int64_t kBiasLds = 152 * 1024;                         // of a workgroup, at most
+constexpr size_t kBiasTwo = 80 * 1024;                           // where two share a compute unit
 
 int check_bias(const pcr_position_table* t, bool back) {
     if (!t || !known_type(t->dtype)) return PCR_E_ARG;
@@ -346,14 +348,16 @@ int pcr_position_bias(int device_id, const pcr_position_table* t, void* hip_stre
     const size_t size = type_size(t->dtype);
     const size_t map_bytes = (size_t)t->axes * (2 * t->reach + 1) * 4;
     auto lds = [&](int heads) { return ((size_t)(t->buckets + 2) * heads * size + 15) / 16 * 16 + map_bytes; };
-    // Heads side by side: 16 bytes of them, fewer where the table is long; workgroups of 1024 threads, and no more of them than fit side by side, where the tables take LDS.
+    // Heads side by side: 16 bytes of them, fewer where fewer than two workgroups' tables fit (us with a limit of 72 / 80 KB: two sequences of 2048 tokens, 12 heads, 19321 buckets 98 / 85).
+    // Workgroups of 1024 threads where a table takes more than 16 KB, and as many as fit side by side, as each loads its own (us with more than 36 / 16 KB: four sequences of
+    // 2048, 3 heads, 3969 buckets 59 / 29; from 4 or 8 KB on the same).
     int together = (int)(16 / size);
-    while (together > 1 && (together >= 2 * t->heads || lds(together) > 72 * 1024)) together >>= 1;
+    while (together > 1 && (together >= 2 * t->heads || lds(together) > kBiasTwo)) together >>= 1;
     const bool held = lds(together) <= (size_t)kBiasLds;
     if (!held) together = 4;
     const size_t bytes = held ? lds(together) : 0;
-    const int threads = bytes > 36 * 1024 ? 1024 : 256;
-    const int64_t most = bytes > 72 * 1024 ? 256 : bytes > 36 * 1024 ? 512 : 2048;
+    const int threads = bytes > 16 * 1024 ? 1024 : 256;
+    const int64_t most = bytes > kBiasTwo ? 256 : threads == 1024 ? 512 : 2048;
     const int64_t blocks = (t->heads + together - 1) / together;
     const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((A.items + 2 * threads - 1) / (2 * threads), (most + blocks - 1) / blocks));
     set_step(A, groups * threads);
