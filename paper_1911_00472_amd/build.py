@@ -8,6 +8,8 @@ SRC = os.path.join(HERE, "csrc", "pcr_lib.hip")                # the decoder, th
 SRC_TRAIN = os.path.join(HERE, "csrc", "pcr_train.hip")        # the operators behind the decode
 SRC_DISTILL = os.path.join(HERE, "csrc", "pcr_distill.hip")
 SRC_LAYERS = os.path.join(HERE, "csrc", "pcr_layers.hip")      # group norm, position bias, dropout
+SRC_NORM_HELD = os.path.join(HERE, "csrc", "pcr_norm_held.hip")            # group norm in one pass
+SRC_NORM_BACK_HELD = os.path.join(HERE, "csrc", "pcr_norm_back_held.hip")
 SRC_BIND = os.path.join(HERE, "csrc", "pcr_bind.cpp")          # their arguments, as a Python module
 LIB = os.path.join(HERE, "libpcr.so")
 MODULE = os.path.join(HERE, "_train.so")
@@ -28,7 +30,7 @@ def build_library():
     """Compile csrc/ into libpcr.so (always recompiles): the C ABI, which needs neither PyTorch nor Python's headers."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     compile_only = [hipcc, "-c"] + [f for f in HIPCC_FLAGS if f != "-shared"]
-    sources = (SRC, SRC_TRAIN, SRC_DISTILL, SRC_LAYERS)
+    sources = (SRC, SRC_TRAIN, SRC_DISTILL, SRC_LAYERS, SRC_NORM_HELD, SRC_NORM_BACK_HELD)
     objects = [os.path.join(os.path.dirname(LIB), os.path.basename(s)[:-len(".hip")] + ".o") for s in sources]
     running = [subprocess.Popen(compile_only + ["-o", o, s]) for s, o in zip(sources, objects)]
     failed = [p.args for p in running if p.wait() != 0]

@@ -1,419 +1,14 @@
-// Group norm with an activation, channels last, and its gradients.
-//
-// Over the pixels of a picture and the channels of a group:  m = mean x, r = (mean (x - m)^2 + eps)^-1/2, u = (x - m) r, z = u w + b, y = act(z).
-// With the incoming gradient g and h = g act'(z):  dw = sum h u and db = sum h over pictures and pixels,  dx = r (h w - mean(h w) - u mean(h w u)).
-#pragma once
-#include "pcr_vec.h"
-
-namespace pcr {
-
-enum { kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3 };
-
-struct NormArgs {
-    const void* x; const void* grad; const void* weight; const void* bias; void* out;
-    float* stats;                                                  // [image][group][2]: m, r
-    float* part;                                                   // [image][chunk][group][2]: mean and sum of squares around it, or sums of h w and h w u
-    float* sums;                                                   // [image][chunk][channel][2]: sums of h u and h (one pass: of a workgroup's pictures)
-    float* joined;                                                 // [image][group][2]: the chunks' sums of h w and h w u, by the number of values
-    int64_t images, pixels, x_image, x_pixel, grad_image, grad_pixel, out_image, out_pixel;
-    int64_t chunk;                                                 // pixels of a workgroup
-    int64_t begin;                                                 // workgroups of earlier launches
-    int chunks, channels, groups, each, activation, weight_float;  // each: channels of a group
-    int block, blocks, pack, turns;                                // one pass: channels of a workgroup, workgroups of a picture; pictures of a workgroup side by side (its threads divided
-                                                                   // among them), and one after another
-    float eps;
-};
-
-// What runs become is computed one after another: side by side their intermediate values would take the registers of whole wavefronts (168 and spills for 90 in the gradient's sums).
-__device__ __forceinline__ void one_after_another() { __builtin_amdgcn_sched_barrier(0); }
-
-// exp(-v), and 1 / v to a unit or two in the last place: a division has ten instructions.
-__device__ __forceinline__ float exp_of_minus(float v) { return __builtin_amdgcn_exp2f(v * -1.4426950408889634f); }
-__device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
-// The normal distribution at z, and exp(-z^2 / 2), by Abramowitz and Stegun's 7.1.26 (Handbook of Mathematical Functions, 1964): with t = 1 / (1 + 0.3275911 |z| / sqrt 2)
-// the upper tail is half of a polynomial of t times that exponential, 7.5e-8 off at most.
-__device__ __forceinline__ float normal_of(float z, float& bell) {
-    const float far = __builtin_fabsf(z), t = inverse(__builtin_fmaf(0.23164188770f, far, 1.f));
-    bell = exp_of_minus(0.5f * z * z);
-    const float tail = t * __builtin_fmaf(t, __builtin_fmaf(t, __builtin_fmaf(t, __builtin_fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f) * bell;
-    return z < 0.f ? tail : 1.f - tail;
-}
-template <int KIND> __device__ __forceinline__ float activated(float z) {
-    if (KIND == kActRelu) return z <= 0.f ? 0.f : z;
-    if (KIND == kActSilu) return z * inverse(1.f + exp_of_minus(z));
-    if (KIND == kActGelu) {
-        float bell;
-        return z * normal_of(z, bell);
-    }
-    return z;
-}
-template <int KIND, int V> __device__ __forceinline__ void activate(float (&z)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; i++) z[i] = activated<KIND>(z[i]);
-}
-// f with the activation as a constant: asked once for a loop, not in it, where the ways that it might go take registers side by side.
-template <int K> struct Kind { static constexpr int value = K; };
-template <typename F> __device__ __forceinline__ void with_kind(int kind, F f) {
-    if (kind == kActSilu) f(Kind<kActSilu>());
-    else if (kind == kActRelu) f(Kind<kActRelu>());
-    else if (kind == kActGelu) f(Kind<kActGelu>());
-    else f(Kind<kActNone>());
-}
-// (x - m) r w + b where that is near 0, with the roundings of difference and products added: what the sum of two floats for each leaves out is 2^-45 of b.
-__device__ __forceinline__ float sum_near_0(float x, float m, float r, float w, float b) {
-#pragma clang fp contract(off)
-    const float d = x - m, of_m = x - d, d_low = (x - (d + of_m)) + (of_m - m);         // x - m = d + d_low
-    const float q = r * w, q_low = __builtin_fmaf(r, w, -q), p = d * q, p_low = __builtin_fmaf(d, q, -p);
-    return (p + b) + (p_low + __builtin_fmaf(d, q_low, d_low * q));
-}
-// x becomes u = (x - m) r, and g becomes g act'(u w + b).  On which side of 0 a rectified z lies is asked more exactly where 32 bits might not tell.  (ONE: the run's channels are of one group.)
-template <int KIND, bool ONE, int V, int N> __device__ __forceinline__ void slopes(float (&x)[V], float (&g)[V], const float (&m)[N], const float (&r)[N], const float (&w)[V], const float (&b)[V]) {
-    bool near = false;
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        const int j = ONE ? 0 : i;
-        const float u = (x[i] - m[j]) * r[j], z = __builtin_fmaf(u, w[i], b[i]);
-        if (KIND == kActRelu) near = near || __builtin_fabsf(z) <= 9.5367431640625e-7f * __builtin_fabsf(b[i]);      // 2^-20
-        if (KIND == kActSilu) {
-            const float s = inverse(1.f + exp_of_minus(z));
-            g[i] *= s * __builtin_fmaf(z, 1.f - s, 1.f);
-        }
-        if (KIND == kActGelu) {
-            float bell;
-            const float under = normal_of(z, bell);
-            g[i] *= __builtin_fmaf(z * 0.39894228040143268f, bell, under);
-        }
-        if (KIND != kActRelu) x[i] = u;
-    }
-    if (KIND == kActRelu) {
-        if (__builtin_expect(near, 0)) {
-#pragma unroll
-            for (int i = 0; i < V; i++) g[i] = sum_near_0(x[i], m[ONE ? 0 : i], r[ONE ? 0 : i], w[i], b[i]) <= 0.f ? g[i] * 0.f : g[i];
-        }
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int j = ONE ? 0 : i;
-            x[i] = (x[i] - m[j]) * r[j];
-            if (!near) g[i] = __builtin_fmaf(x[i], w[i], b[i]) <= 0.f ? g[i] * 0.f : g[i];
-        }
-    }
-}
-
-// Sums over a workgroup's lanes of pixels (values[lane][unit], `units` of them from `first` on) and over the `each` units of a group, added to total[group].
-// A group's team of threads adds in a fixed order, then their sums are joined; all of `threads` threads, a power of two of them, are needed.
-__device__ __forceinline__ void group_totals(const float* values, float* total, int lanes, int units, int first, int each, int groups_from, int groups_to, int thread, int threads) {
-    const int n = groups_to - groups_from;
-    int team = 64;
-    while (team > 1 && team * n > threads) team >>= 1;
-    for (int g0 = 0; g0 < n; g0 += threads / team) {
-        const int g = g0 + thread / team, member = thread & (team - 1);
-        float sum = 0.f;
-        if (g < n) {
-            const int c0 = max((groups_from + g) * each - first, 0), c1 = min((groups_from + g + 1) * each - first, units), width = c1 - c0;
-            if (width == units) {                                  // (one group: everything)
-#pragma unroll 4
-                for (int e = member; e < lanes * width; e += team) sum += values[e];
-            } else if (width == 1) {
-#pragma unroll 4
-                for (int lane = member; lane < lanes; lane += team) sum += values[lane * units + c0];
-            } else {
-                int lane = member / width, c = member - lane * width;
-                const int down = team / width, across_ = team - down * width;
-                for (int e = member; e < lanes * width; e += team) {
-                    sum += values[lane * units + c0 + c];
-                    lane += down;
-                    c += across_;
-                    if (c >= width) { c -= width; lane++; }
-                }
-            }
-        }
-        for (int d = 1; d < team; d <<= 1) sum += __shfl_xor(sum, d);
-        if (g < n && member == 0) total[groups_from + g] += sum;
-    }
-}
-
-template <typename T, int V> __device__ __forceinline__ void load_parameters(const NormArgs& A, const void* p, int at, float without, float (&x)[V]) {
-    if (!p) {
-#pragma unroll
-        for (int i = 0; i < V; i++) x[i] = without;
-    } else if (A.weight_float) load_run<float, V>((const float*)p + at, x);
-    else load_run<T, V>((const T*)p + at, x);
-}
-
-// ---- in one pass ----
-//
-// Where the pixels of a picture with a few groups' channels fit into the registers of a workgroup, it reads them once: the mean, then the squares around it, are
-// summed from registers, and what is written is made from them.  A thread has a run of V channels of every few pixels; block: channels of a workgroup, whole groups and whole
-// runs.  us: 64 pictures of 14 x 14 x 256, bfloat 8.3 (2.6 at 5.0 TB/s), the gradient 15 (3.9), one of 14 x 14 x 64 5.7: the launch, and loads, sums and stores of a workgroup, which
-// follow each other, bound it.  The workgroups of a picture run on one die (blockIdx modulo 8 goes round the dies), where they find in its cache what lies beside their own channels in a line.
-struct Slab {
-    int64_t image, row;                                            // the first of the thread's pictures; where its workgroup's sums go
-    int first, channels, columns, lanes, lane, column;             // of the workgroup's channels; runs of a pixel; threads to a run, the thread's place
-    int slot, thread, threads;                                     // of the workgroup's pictures; of the picture's threads
-    bool works;
-};
-__device__ __forceinline__ Slab slab_of(const NormArgs& A, int V) {
-    Slab S;
-    const int64_t at = blockIdx.x + A.begin;
-    const int dies = A.images % 8 || A.blocks == 1 ? 1 : 8;
-    const int64_t row = at / dies, turn = row / A.blocks;
-    S.threads = (int)blockDim.x / A.pack;
-    S.slot = threadIdx.x / S.threads;
-    S.thread = threadIdx.x & (S.threads - 1);
-    S.row = turn * dies + at % dies;
-    S.image = S.row * A.pack * A.turns + S.slot;
-    S.first = (int)(row - turn * A.blocks) * A.block;
-    S.channels = min(A.block, A.channels - S.first);
-    S.columns = S.channels / V;
-    S.lanes = S.threads / S.columns;
-    S.lane = S.thread / S.columns;
-    S.column = S.thread - S.lane * S.columns;
-    S.works = S.lane < S.lanes;
-    return S;
-}
-// ONE: the channels of a run are of one group.
-template <int V, bool ONE> __device__ __forceinline__ int value_units(int channels) { return ONE ? channels / V : channels; }
-template <int V, bool ONE> __device__ __forceinline__ void put_values(float* values, const Slab& S, const float (&x)[V]) {
-    if (!S.works) return;
-    if constexpr (ONE) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < V; i++) sum += x[i];
-        values[S.lane * S.columns + S.column] = sum;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i++) values[(S.lane * S.columns + S.column) * V + i] = x[i];
-    }
-}
-
-template <typename T, int V> struct Held { typename Run<T, V>::Vec v; };
-template <typename T, int V> __device__ __forceinline__ void take(const Held<T, V>& from, float (&x)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        if constexpr (V == 1) x[i] = (float)from.v;
-        else x[i] = (float)from.v[i];
-    }
-}
-template <typename T, int V, int K> __device__ __forceinline__ void hold(Held<T, V> (&h)[K], const T* from, int64_t pixel, const Slab& S, int pixels) {
-#pragma unroll
-    for (int k = 0; k < K; k++)
-        if (k * S.lanes < pixels) h[k].v = reinterpret_cast<const typename Run<T, V>::Loose*>(from + (int64_t)min(S.lane + k * S.lanes, pixels - 1) * pixel)->v;
-}
-
-// MANY: a workgroup has several pictures, A.pack side by side and A.turns after one another.
-template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS) void k_norm_held(NormArgs A) {
-    extern __shared__ __attribute__((aligned(16))) float shared[];
-    const Slab S = slab_of(A, V);
-    const int groups = S.channels / A.each;
-    float* values = shared + S.slot * S.threads * (ONE ? 1 : V);   // [lane][unit]
-    float* total = shared + THREADS * (ONE ? 1 : V) + S.slot * 3 * groups;     // [group of the block]: sums; then means; then r
-    const int pixels = (int)A.pixels, c = S.first + S.column * V, unit_groups = ONE ? A.each / V : A.each;
-    constexpr bool EARLY = THREADS == 256;                         // (workgroups of 512 threads have registers for the parameters when the sums are made)
-    float w[V], b[V];
-    auto parameters = [&]() {
-        load_parameters<T, V>(A, A.weight, S.works ? c : S.first, 1.f, w);
-        load_parameters<T, V>(A, A.bias, S.works ? c : S.first, 0.f, b);
-    };
-    const int units = value_units<V, ONE>(S.channels);
-    const float inv = 1.f / ((float)pixels * A.each);
-    for (int turn = 0;; turn++) {
-        const int64_t image = S.image + turn * A.pack;
-        const bool last = !MANY || turn + 1 == A.turns, there = image < A.images;
-        Held<T, V> x[K];
-        hold<T, V, K>(x, (const T*)A.x + min(image, A.images - 1) * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
-        if (EARLY && turn == 0) parameters();
-        for (int g = S.thread; g < 3 * groups; g += S.threads) total[g] = 0.f;
-        float sum[V];
-#pragma unroll
-        for (int i = 0; i < V; i++) sum[i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < K; k++)
-            if (k * S.lanes < pixels) {
-                float a[V];
-                take(x[k], a);
-                if (S.lane + k * S.lanes < pixels) {
-#pragma unroll
-                    for (int i = 0; i < V; i++) sum[i] += a[i];
-                }
-            }
-        put_values<V, ONE>(values, S, sum);
-        __syncthreads();
-        group_totals(values, total, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
-        __syncthreads();
-        float m[ONE ? 1 : V];
-#pragma unroll
-        for (int i = 0; i < (ONE ? 1 : V); i++) m[i] = S.works ? total[(S.column * V + i) / A.each] * inv : 0.f;
-#pragma unroll
-        for (int i = 0; i < V; i++) sum[i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < K; k++)
-            if (k * S.lanes < pixels) {
-                float a[V];
-                take(x[k], a);
-                if (S.lane + k * S.lanes < pixels) {
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        const float d = a[i] - m[ONE ? 0 : i];
-                        sum[i] = __builtin_fmaf(d, d, sum[i]);
-                    }
-                }
-            }
-        put_values<V, ONE>(values, S, sum);
-        __syncthreads();
-        group_totals(values, total + groups, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
-        __syncthreads();
-        for (int g = S.thread; g < groups; g += S.threads) {
-            const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(total[groups + g], inv, A.eps));
-            total[2 * groups + g] = r;
-            float2* to = (float2*)A.stats + image * A.groups + S.first / A.each + g;
-            if (there) *to = make_float2(total[g] * inv, r);
-        }
-        __syncthreads();
-        if (S.works && there) {
-            float by[V];
-            if (!EARLY) parameters();
-#pragma unroll
-            for (int i = 0; i < V; i++) by[i] = w[i] * total[2 * groups + (S.column * V + i) / A.each];
-            T* out = (T*)A.out + image * A.out_image + c;
-            with_kind(A.activation, [&](auto kind) {
-#pragma unroll
-                for (int k = 0; k < K; k++) {
-                    const int p = S.lane + k * S.lanes;
-                    if (p < pixels) {
-                        float a[V];
-                        take(x[k], a);
-#pragma unroll
-                        for (int i = 0; i < V; i++) a[i] = __builtin_fmaf(a[i] - m[ONE ? 0 : i], by[i], b[i]);
-                        activate<decltype(kind)::value>(a);
-                        store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
-                    }
-                    one_after_another();
-                }
-            });
-        }
-        if (last) break;
-        __syncthreads();
-    }
-}
-
-// The gradient.  What a thread has summed over its pictures, by channels, is summed over the workgroup at the end.
-template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS) void k_norm_back_held(NormArgs A) {
-    extern __shared__ __attribute__((aligned(16))) float shared[];
-    const Slab S = slab_of(A, V);
-    const int groups = S.channels / A.each, pixels = (int)A.pixels, c = S.first + S.column * V, unit_groups = ONE ? A.each / V : A.each;
-    const int units = value_units<V, ONE>(S.channels), half = S.threads * (ONE ? 1 : V);
-    float* values = shared + S.slot * 2 * half;                    // [2][lane][unit]; at the end [lane of all pictures][channel]
-    float* total = shared + 2 * THREADS * (ONE ? 1 : V) + S.slot * 2 * groups;             // [2][group]
-    float w[V], b[V], sums[2][V];                                  // sums: of h u and h
-    load_parameters<T, V>(A, A.weight, S.works ? c : S.first, 1.f, w);
-    load_parameters<T, V>(A, A.bias, S.works ? c : S.first, 0.f, b);
-#pragma unroll
-    for (int i = 0; i < V; i++) sums[0][i] = sums[1][i] = 0.f;
-    const float inv = 1.f / ((float)pixels * A.each);
-    for (int turn = 0;; turn++) {
-        const int64_t image = S.image + turn * A.pack, at = min(image, A.images - 1);
-        const bool last = !MANY || turn + 1 == A.turns, there = image < A.images;
-        Held<T, V> x[K], h[K];
-        hold<T, V, K>(x, (const T*)A.x + at * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
-        hold<T, V, K>(h, (const T*)A.grad + at * A.grad_image + (S.works ? c : S.first), A.grad_pixel, S, pixels);
-        for (int e = S.thread; e < 2 * groups; e += S.threads) total[e] = 0.f;
-        float m[ONE ? 1 : V], r[ONE ? 1 : V], s[2][V];
-#pragma unroll
-        for (int i = 0; i < (ONE ? 1 : V); i++) {
-            const float2 of = ((const float2*)A.stats)[at * A.groups + ((S.works ? c : S.first) + i) / A.each];
-            m[i] = of.x;
-            r[i] = of.y;
-        }
-#pragma unroll
-        for (int i = 0; i < V; i++) s[0][i] = s[1][i] = 0.f;
-        with_kind(A.activation, [&](auto kind) {
-#pragma unroll
-            for (int k = 0; k < K; k++)
-                if (k * S.lanes < pixels) {
-                    float a[V], g[V];
-                    take(x[k], a);
-                    take(h[k], g);
-                    slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
-                    if (S.lane + k * S.lanes < pixels) {
-#pragma unroll
-                        for (int i = 0; i < V; i++) {
-                            s[0][i] = __builtin_fmaf(g[i], a[i], s[0][i]);
-                            s[1][i] += g[i];
-                        }
-                    }
-                    one_after_another();
-                }
-        });
-        // The groups'.
-#pragma unroll
-        for (int z = 0; z < 2; z++) {
-            float weighted[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                if (there) sums[z][i] += s[z][i];
-                weighted[i] = s[z][i] * w[i];
-            }
-            put_values<V, ONE>(values + z * half, S, weighted);
-        }
-        __syncthreads();
-        group_totals(values, total, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
-        group_totals(values + half, total + groups, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
-        __syncthreads();
-        if (S.works && there) {
-            float su[ONE ? 1 : V], sh[ONE ? 1 : V];
-#pragma unroll
-            for (int i = 0; i < (ONE ? 1 : V); i++) {
-                const int g = (S.column * V + i) / A.each;
-                su[i] = total[g] * inv;
-                sh[i] = total[groups + g] * inv;
-            }
-            T* out = (T*)A.out + image * A.out_image + c;
-            with_kind(A.activation, [&](auto kind) {
-#pragma unroll
-                for (int k = 0; k < K; k++) {
-                    const int p = S.lane + k * S.lanes;
-                    if (p < pixels) {
-                        float a[V], g[V];
-                        take(x[k], a);
-                        take(h[k], g);
-                        slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
-#pragma unroll
-                        for (int i = 0; i < V; i++) {
-                            const int j = ONE ? 0 : i;
-                            a[i] = r[j] * (__builtin_fmaf(g[i], w[i], -sh[j]) - a[i] * su[j]);
-                        }
-                        store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
-                    }
-                    one_after_another();
-                }
-            });
-        }
-        if (last) break;
-        __syncthreads();
-    }
-    // The channels'.
-    float* channel = shared + THREADS * V;                         // [channel]
-    float2* to = (float2*)A.sums + S.row * A.channels + S.first;
-    for (int z = 0; z < 2; z++) {
-        __syncthreads();
-        if (S.works) {
-#pragma unroll
-            for (int i = 0; i < V; i++) shared[((S.slot * S.lanes + S.lane) * S.columns + S.column) * V + i] = z ? sums[1][i] : sums[0][i];
-        }
-        for (int e = threadIdx.x; e < S.channels; e += THREADS) channel[e] = 0.f;
-        __syncthreads();
-        group_totals(shared, channel, (MANY ? A.pack : 1) * S.lanes, S.channels, 0, 1, 0, S.channels, (int)threadIdx.x, THREADS);
-        __syncthreads();
-        for (int e = threadIdx.x; e < S.channels; e += THREADS) (z ? to[e].y : to[e].x) = channel[e];
-    }
-}
-
-// ---- in two passes ----
+// Group norm and its gradient in two passes.
 //
 // Larger pictures are gone through twice, chunk by chunk of their pixels: sums of every chunk, then what is written; what the second pass reads mostly comes out of the
 // memory-side cache.  Loads of four pixels are under way together, without conditions about them (behind which the compiler would wait for those before).
 // Bound by memory.  us: 64 pictures of 112 x 112 x 64, bfloat, sums 32 (103 MB, 3.2 TB/s; 26 where x is in the cache), result 39 (206 MB, 5.3 TB/s); gradient of 64 of 56 x 56 x 256 sums 57
 // (206 MB, 3.6 TB/s), result 55 (308 MB, 5.6 TB/s), sums of the weights' gradients 5.
+#pragma once
+#include "pcr_norm.h"
+
+namespace pcr {
+
 constexpr int kNormThreads = 256;
 constexpr int kNormTogether = 4;
 constexpr int kMergedChunks = 64;                                  // so many of a picture's chunks are joined by every workgroup that needs them

@@ -4,7 +4,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "../../include/pcr.h"
 #include "pcr_bias.h"
@@ -16,16 +15,9 @@ using namespace pcr;
 
 namespace {
 
-template <int N> using Int = std::integral_constant<int, N>;
-
 // Working memory lies at a multiple of 16 bytes.
 bool at_16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool multiple(const void* p, int64_t a, int64_t b, size_t size, int unit) { return ((uint64_t)(uintptr_t)p / size | (uint64_t)a | (uint64_t)b) % unit == 0; }
-
-// Lets a kernel have more LDS than is common.
-template <typename K> bool allow_lds(K kernel, size_t bytes) {
-    return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
-}
 
 // ---- group norm ----
 
@@ -41,16 +33,6 @@ int check_norm(const pcr_group_norm* N, bool back) {
 
 constexpr int64_t kSmallImages = 2048;                           // workgroups at least, where pictures share one
 
-struct NormPlan {
-    int64_t chunk;
-    int chunks, run;
-    int held, threads, block, blocks, pack;                    // one pass: runs that a thread holds (0: two passes), threads and channels of a workgroup, workgroups of a picture, pictures of one
-    int turns;
-    bool many;
-    int64_t rows;                                              // of channels' sums
-    size_t part_bytes, sums_bytes, joined_bytes;
-    size_t bytes() const { return part_bytes + sums_bytes + joined_bytes; }
-};
 NormPlan plan_norm(const pcr_group_norm* N, bool back) {
     NormPlan P = {};
     const size_t size = type_size(N->dtype);
@@ -125,53 +107,6 @@ NormArgs norm_args(const pcr_group_norm* N, const NormPlan& P, void* d_work) {
     A.activation = N->activation; A.weight_float = N->weight_dtype == PCR_FLOAT; A.eps = N->eps;
     return A;
 }
-template <typename F> void with_run(int dtype, int run, F f) {
-    with_type(dtype, [&](auto t) {
-        if (run == 8) { if constexpr (sizeof(t) == 2) f(t, Int<8>()); }
-        else if (run == 4) { if constexpr (sizeof(t) == 4) f(t, Int<4>()); }
-        else if (run == 2) f(t, Int<2>());
-        else f(t, Int<1>());
-    });
-}
-
-// One pass of either kind.
-template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, NormArgs A, hipStream_t s) {
-    bool ok = true;
-    const bool one = A.each % P.run == 0;
-    with_run(N->dtype, P.run, [&](auto t, auto v) {
-        typedef decltype(t) T;
-        constexpr int V = decltype(v)::value;
-        auto launch = [&](auto k, auto threads, auto in_one, auto of_many) {
-            constexpr int K = decltype(k)::value, THREADS = decltype(threads)::value;
-            constexpr bool ONE = decltype(in_one)::value, MANY = decltype(of_many)::value;
-            const size_t groups = A.block / A.each, values = THREADS * (ONE ? 1 : V);
-            const size_t lds = (BACK ? std::max(2 * values + A.pack * 2 * groups, (size_t)THREADS * V + A.block) : values + A.pack * 3 * groups) * sizeof(float);
-            in_ranges(P.rows * A.blocks, THREADS, [&](int64_t begin, unsigned workgroups) {
-                A.begin = begin;
-                if constexpr (BACK) {
-                    ok = ok && allow_lds(k_norm_back_held<T, V, K, THREADS, ONE, MANY>, lds);
-                    if (ok) hipLaunchKernelGGL((k_norm_back_held<T, V, K, THREADS, ONE, MANY>), dim3(workgroups), dim3(THREADS), lds, s, A);
-                } else {
-                    ok = ok && allow_lds(k_norm_held<T, V, K, THREADS, ONE, MANY>, lds);
-                    if (ok) hipLaunchKernelGGL((k_norm_held<T, V, K, THREADS, ONE, MANY>), dim3(workgroups), dim3(THREADS), lds, s, A);
-                }
-            });
-        };
-        auto by_one = [&](auto k, auto threads, auto of_many) {
-            if (one) launch(k, threads, std::true_type(), of_many);
-            else if constexpr (V > 1) launch(k, threads, std::false_type(), of_many);
-        };
-        constexpr bool WHOLE = V * sizeof(T) == 16;
-        if (P.many) by_one(Int<WHOLE ? 1 : 2>(), Int<256>(), std::true_type());
-        else if (P.threads == 256) by_one(Int<WHOLE ? 4 : 8>(), Int<256>(), std::false_type());
-        else if constexpr (WHOLE) {
-            if (P.held <= 8) by_one(Int<8>(), Int<512>(), std::false_type());
-            else if constexpr (!BACK) by_one(Int<16>(), Int<512>(), std::false_type());
-        }
-    });
-    return ok;
-}
-
 // ---- position bias ----
 
 constexpr int64_t kBiasLds = 152 * 1024;                         // of a workgroup, at most
@@ -273,7 +208,7 @@ int pcr_group_norm_forward(int device_id, const pcr_group_norm* norm, void* d_wo
     if (!on.ok) return PCR_E_DEVICE;
     NormArgs A = norm_args(norm, P, d_work);
     const hipStream_t s = (hipStream_t)hip_stream;
-    if (P.held) return run_held<false>(norm, P, A, s) ? launched() : PCR_E_DEVICE;
+    if (P.held) return run_norm_held(norm, P, A, s) ? launched() : PCR_E_DEVICE;
     with_run(norm->dtype, P.run, [&](auto t, auto v) {
         typedef decltype(t) T;
         constexpr int V = decltype(v)::value;
@@ -308,7 +243,7 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
     NormArgs A = norm_args(norm, P, d_work);
     const hipStream_t s = (hipStream_t)hip_stream;
     if (!none && P.held) {
-        if (!run_held<true>(norm, P, A, s)) return PCR_E_DEVICE;
+        if (!run_norm_back_held(norm, P, A, s)) return PCR_E_DEVICE;
     } else if (!none)
         with_run(norm->dtype, P.run, [&](auto t, auto v) {
             typedef decltype(t) T;

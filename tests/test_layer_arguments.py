@@ -137,9 +137,11 @@ def test_buckets_of_windows_and_lines():
 
 def test_no_kernel_spills_to_scratch_memory(tmp_path):
     from paper_1911_00472_amd import build
-    asm = tmp_path / "kernels.s"
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
-    subprocess.check_call([hipcc] + flags + ["-S", "--cuda-device-only", "-o", str(asm), build.SRC_LAYERS], stderr=subprocess.DEVNULL)
-    sizes = [line.split()[-1] for line in asm.read_text().splitlines() if ".amdhsa_private_segment_fixed_size" in line]
+    sources = [build.SRC_LAYERS, build.SRC_NORM_HELD, build.SRC_NORM_BACK_HELD]
+    listings = [tmp_path / (os.path.basename(s) + ".s") for s in sources]
+    running = [subprocess.Popen([hipcc] + flags + ["-S", "--cuda-device-only", "-o", str(to), s], stderr=subprocess.DEVNULL) for s, to in zip(sources, listings)]
+    assert [p.wait() for p in running] == [0] * len(sources)
+    sizes = [line.split()[-1] for to in listings for line in to.read_text().splitlines() if ".amdhsa_private_segment_fixed_size" in line]
     assert len(sizes) > 30 and all(s == "0" for s in sizes), sizes
