@@ -72,9 +72,20 @@ def test_group_norm():
         assert L.pcr_group_norm_workspace(by(norm(**large)), backward, by(need)) == pkg.OK and need.value > 0
         assert f(0, by(norm(**large)), None, need.value, None) == pkg.E_ARG
         assert f(0, by(norm(**large)), at, need.value - 1, None) == pkg.E_RANGE
+        assert f(0, by(norm(**large)), (at + 15) // 16 * 16 + 8, need.value, None) == pkg.E_ARG          # (working memory not at a multiple of 16)
     assert L.pcr_group_norm_workspace(None, 0, by(need)) == pkg.E_ARG and L.pcr_group_norm_workspace(by(norm()), 0, None) == pkg.E_ARG
     assert L.pcr_group_norm_workspace(by(norm(groups=3)), 0, by(need)) == pkg.E_RANGE
     assert L.pcr_group_norm_forward(0, by(norm(images=0, x=None, out=None, stats=None)), None, 0, None) == pkg.OK
+
+
+def test_rows_of_many_small_pictures():
+    """Working memory for channels' sums goes by workgroups, not by pictures, and covers pictures that do not divide evenly."""
+    need, L = ctypes.c_size_t(0), pkg.lib()
+    for images in (2048, 4097, 100000, 2 ** 24 + 3):
+        assert L.pcr_group_norm_workspace(by(norm(images=images, pixels=4, channels=32, groups=4, x_pixel=32, out_pixel=32, grad_pixel=32, x_image=128, out_image=128, grad_image=128, dtype=2, weight_dtype=2)),
+                                          1, by(need)) == pkg.OK
+        rows, rest = divmod(need.value, 32 * 8)
+        assert rest == 0 and images / 512 <= rows <= images, (images, rows)
 
 
 def test_position_bias():
@@ -96,6 +107,7 @@ def test_position_bias():
     assert L.pcr_position_bias_backward(0, by(table(**long)), None, at, need.value, None) == pkg.E_ARG
     assert L.pcr_position_bias_backward(0, by(table(**long)), at, None, need.value, None) == pkg.E_ARG
     assert L.pcr_position_bias_backward(0, by(table(**long)), at, at, need.value - 1, None) == pkg.E_RANGE
+    assert L.pcr_position_bias_backward(0, by(table(**long)), at, (at + 15) // 16 * 16 + 8, need.value, None) == pkg.E_ARG
     assert L.pcr_position_bias(0, by(table(keys=0, query=Places(), key=Places(), map=None, values=None)), None) == pkg.OK
 
 
