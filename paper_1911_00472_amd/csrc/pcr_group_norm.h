@@ -9,10 +9,6 @@
 
 namespace pcr {
 
-constexpr int kNormThreads = 256;
-constexpr int kNormTogether = 4;
-constexpr int kMergedChunks = 64;                                  // so many of a picture's chunks are joined by every workgroup that needs them
-
 // A block of columns: runs of V channels, as many as there are threads; `lanes` threads to a column take the pixels in turn.
 struct Columns { int count, lanes, lane, column; bool works; };
 __device__ __forceinline__ Columns columns_of(int from, int all) {

@@ -17,7 +17,6 @@ namespace {
 
 // Working memory lies at a multiple of 16 bytes.
 bool at_16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-bool multiple(const void* p, int64_t a, int64_t b, size_t size, int unit) { return ((uint64_t)(uintptr_t)p / size | (uint64_t)a | (uint64_t)b) % unit == 0; }
 
 // ---- group norm ----
 
@@ -31,71 +30,6 @@ int check_norm(const pcr_group_norm* N, bool back) {
     return PCR_OK;
 }
 
-constexpr int64_t kSmallImages = 2048;                           // workgroups at least, where pictures share one
-
-NormPlan plan_norm(const pcr_group_norm* N, bool back) {
-    NormPlan P = {};
-    const size_t size = type_size(N->dtype);
-    // Runs of 16 bytes of channels, of two or of one.
-    P.run = (int)(16 / size);
-    for (; P.run > 1; P.run = P.run == 8 ? 2 : P.run >> 1) {
-        if (N->channels % P.run) continue;
-        if (multiple(N->x, N->x_image, N->x_pixel, size, P.run) && multiple(N->out, N->out_image, N->out_pixel, size, P.run) &&
-            (!back || multiple(N->grad, N->grad_image, N->grad_pixel, size, P.run)))
-            break;
-    }
-    const int64_t each = N->channels / N->groups;
-    if (N->images && N->pixels) {
-        // One pass: channels of whole groups and whole runs, 128 bytes of them where that many fit, fewer where there would be less than 256 workgroups.  A thread holds 16 runs at most (8 of
-        // input and gradient each): with 32 there is one workgroup a compute unit, which loads, sums and stores one after another (64 pictures of 56 x 56 x 256 54 us and 48).
-        const int64_t unit = each * P.run / std::__gcd(each, (int64_t)P.run), units = N->channels / unit;
-        const int64_t target = 256, most = P.run * size < 16 ? 256 * 8 : 512 * (back ? 8 : 16);
-        int64_t many = std::max<int64_t>(1, std::min<int64_t>((128 + unit * size - 1) / (unit * size), std::max<int64_t>(1, N->images * units / target)));
-        const int64_t of_unit = N->pixels * (unit / P.run);
-        while (many > 1 && of_unit * many > most) many >>= 1;
-        many = std::min(many, units);
-        // Many small pictures: where a picture has no more runs than a workgroup's threads hold (one each, two of fewer than 16 bytes), it has whole ones, side by side and after one another,
-        // whose channels' sums are one row.  (us, with a picture or 128 bytes of its channels to a workgroup: 32768 of a pixel of 1024 channels 114, now 66, their gradient 440, 90;
-        // 100000 of 2 x 2 x 32 324, 29, and 788, 46.)
-        const int64_t runs_held = P.run * size < 16 ? 2 : 1;
-        P.many = N->images >= kSmallImages && of_unit * units <= 256 * runs_held && units * unit / P.run <= 256;
-        if (P.many) many = units;
-        const int64_t columns = many * unit / P.run;
-        if (of_unit * many <= most && columns <= 256) {
-            P.block = (int)(many * unit);
-            P.blocks = (int)((units + many - 1) / many);
-            auto need = [&](int threads) { return (N->pixels + threads / columns - 1) / (threads / columns); };
-            P.threads = P.run * size < 16 || need(256) <= 4 ? 256 : 512;
-            for (P.held = 1; P.held < need(P.threads);) P.held <<= 1;
-            if (P.held > (P.run * size < 16 || back ? 8 : 16)) P.held = 0;
-            P.pack = 1;
-            if (P.many)
-                while (N->images >= 2 * P.pack * kSmallImages && 128 / P.pack >= columns && need(128 / P.pack) <= runs_held) P.pack *= 2;
-            P.turns = P.many ? (int)std::min<int64_t>(16, std::max<int64_t>(1, N->images / (P.pack * kSmallImages))) : 1;
-            // (Rows of 16 bytes: 64 pictures of 56 x 56 x 256 take 66 us, and 65 in two passes; their gradient 201, and 113.)
-            if (P.block < N->channels && P.block * (int64_t)size < 32 && N->images * N->pixels * N->channels * (int64_t)size > (64 << 20)) P.held = 0;
-        }
-    }
-    if (P.held) {
-        P.chunk = N->pixels;
-        P.chunks = 1;
-        P.rows = (N->images + P.pack * P.turns - 1) / (P.pack * P.turns);
-        P.sums_bytes = back ? (size_t)P.rows * N->channels * 2 * sizeof(float) : 0;
-        return P;
-    }
-    // Two passes.  Chunks of a picture's pixels: 768 workgroups in all, 512 of a gradient, of 16 pixels to a thread at least.  (us with 512 / 768 / 1024 / 2048: 64 pictures of
-    // 112 x 112 x 64 59.8 / 57.9 / 59.3 / 64.6, gradient of 64 of 56 x 56 x 256 99 / 105 / 107 / 113, of 32 of 112 x 112 x 64 57 / 62 / 66 / 66.)
-    const int64_t columns = std::min<int64_t>(N->channels / P.run, kNormThreads), lanes = kNormThreads / columns, step = kNormTogether * lanes;
-    int64_t chunks = std::min<int64_t>(((back ? 512 : 768) + N->images - 1) / std::max<int64_t>(1, N->images), (N->pixels + 4 * step - 1) / (4 * step));
-    chunks = std::max<int64_t>(1, chunks);
-    P.chunk = ((N->pixels + chunks - 1) / chunks + step - 1) / step * step;
-    P.chunks = N->pixels ? (int)((N->pixels + P.chunk - 1) / P.chunk) : 0;
-    P.part_bytes = (size_t)N->images * P.chunks * N->groups * 2 * sizeof(float);
-    P.rows = N->images * P.chunks;
-    P.sums_bytes = back ? (size_t)P.rows * N->channels * 2 * sizeof(float) : 0;
-    P.joined_bytes = back && P.chunks > kMergedChunks ? (size_t)N->images * N->groups * 2 * sizeof(float) : 0;
-    return P;
-}
 NormArgs norm_args(const pcr_group_norm* N, const NormPlan& P, void* d_work) {
     NormArgs A = {};
     A.x = N->x; A.grad = N->grad; A.weight = N->weight; A.bias = N->bias; A.out = N->out; A.stats = N->stats;

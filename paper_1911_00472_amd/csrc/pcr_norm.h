@@ -9,6 +9,7 @@
 
 #include "../../include/pcr.h"
 #include "pcr_host.h"
+#include "pcr_norm_plan.h"
 #include "pcr_vec.h"
 
 namespace pcr {
@@ -165,17 +166,6 @@ template <typename K> bool allow_lds(K kernel, size_t bytes) {
     return bytes <= 65536 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
 }
 
-// What a call is made of.
-struct NormPlan {
-    int64_t chunk;                                                 // pixels of a workgroup
-    int chunks, run;                                               // of a picture; channels that are loaded together
-    int held, threads, block, blocks;                              // one pass: runs that a thread holds (0: two passes), threads and channels of a workgroup, workgroups of a picture
-    int pack, turns;                                               // one pass: pictures of a workgroup side by side, and after one another
-    bool many;                                                     // several pictures to a workgroup
-    int64_t rows;                                                  // of channels' sums
-    size_t part_bytes, sums_bytes, joined_bytes;
-    size_t bytes() const { return part_bytes + sums_bytes + joined_bytes; }
-};
 template <typename F> void with_run(int dtype, int run, F f) {
     with_type(dtype, [&](auto t) {
         if (run == 8) { if constexpr (sizeof(t) == 2) f(t, Int<8>()); }

@@ -263,7 +263,7 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
     }
 }
 
-// One pass of either kind.
+// One pass of either kind.  (A kernel whose threads would not hold the picture, or that is not the one of the plan, is not launched.)
 template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, NormArgs A, hipStream_t s) {
     bool ok = true;
     const bool one = A.each % P.run == 0;
@@ -273,6 +273,8 @@ template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, N
         auto launch = [&](auto k, auto threads, auto in_one, auto of_many) {
             constexpr int K = decltype(k)::value, THREADS = decltype(threads)::value;
             constexpr bool ONE = decltype(in_one)::value, MANY = decltype(of_many)::value;
+            ok = ok && P.held == K && P.threads == THREADS && P.many == MANY && P.holds(N->pixels);
+            if (!ok) return;
             const size_t groups = A.block / A.each, values = THREADS * (ONE ? 1 : V);
             const size_t lds = (BACK ? std::max(2 * values + A.pack * 2 * groups, (size_t)THREADS * V + A.block) : values + A.pack * 3 * groups) * sizeof(float);
             in_ranges(P.rows * A.blocks, THREADS, [&](int64_t begin, unsigned workgroups) {
