@@ -36,16 +36,19 @@ template <typename F4, typename F> __device__ __forceinline__ void through(const
     for (; p < K.end; p += C.lanes) f(p);
 }
 
-// Mean and sum of squares around it of every group over a chunk of pixels.
+// Mean and sum of squares around it of every group over a chunk of pixels.  Running means of equal values are exact; their sum over lanes and channels is in 64 bits, so that the mean is, too.
+inline size_t norm_sums_lds(int run, int groups) { return (size_t)kNormThreads * run * 8 + (size_t)groups * 12; }
 template <typename T, int V> __global__ __launch_bounds__(256) void k_norm_sums(NormArgs A) {
     extern __shared__ __attribute__((aligned(16))) float shared[];
-    float* values = shared;                                        // [lane][channel of the block]
-    float* total = shared + kNormThreads * V;                      // [group]
-    float* mean = total + A.groups;
+    double* sums = (double*)shared;                                // [lane][channel of the block]
+    float* values = shared;                                        // [lane][channel of the block]: of squares
+    double* whole = sums + kNormThreads * V;                       // [group]
+    float* total = (float*)whole;                                  // [group]: of squares
+    float* mean = (float*)(whole + A.groups);
     const Chunk K = chunk_of(A, blockIdx.x + A.begin);
     const T* x = (const T*)A.x + K.image * A.x_image;
     const int all = A.channels / V;
-    for (int g = threadIdx.x; g < A.groups; g += kNormThreads) total[g] = 0.f;
+    for (int g = threadIdx.x; g < A.groups; g += kNormThreads) whole[g] = 0.0;
     // One block of columns holds its means and squares in registers; of more of them each is gone through twice.
     const int blocks = (all + kNormThreads - 1) / kNormThreads;
     float m[V], q[V];
@@ -93,27 +96,30 @@ template <typename T, int V> __global__ __launch_bounds__(256) void k_norm_sums(
             if (C.works) {
 #pragma unroll
                 for (int i = 0; i < V; i++) {
-                    float v;
-                    if (phase == 0) v = m[i] * n;
+                    const int at = C.lane * width + C.column * V + i;
+                    if (phase == 0) sums[at] = (double)m[i] * n;
                     else {
                         const float d = m[i] - mean[(c + i) / A.each];
-                        v = __builtin_fmaf(d * d, (float)n, q[i]);
+                        values[at] = __builtin_fmaf(d * d, (float)n, q[i]);
                     }
-                    values[C.lane * width + C.column * V + i] = v;
                 }
             }
             __syncthreads();
-            group_totals(values, total, C.lanes, width, first, A.each, g0, g1, (int)threadIdx.x, kNormThreads);
+            if (phase == 0) group_totals(sums, whole, C.lanes, width, first, A.each, g0, g1, (int)threadIdx.x, kNormThreads);
+            else group_totals(values, total, C.lanes, width, first, A.each, g0, g1, (int)threadIdx.x, kNormThreads);
             __syncthreads();
         }
-        const float count = (float)(K.end - K.first) * A.each;
+        const double count = (double)(K.end - K.first) * A.each;
         float* part = A.part + ((blockIdx.x + A.begin) * A.groups) * 2 + phase;
         for (int g = threadIdx.x; g < A.groups; g += kNormThreads) {
-            if (phase == 0) mean[g] = total[g] / count;
+            if (phase == 0) mean[g] = (float)(whole[g] / count);
             part[2 * g] = phase == 0 ? mean[g] : total[g];
-            total[g] = 0.f;
         }
         __syncthreads();
+        if (phase == 0) {
+            for (int g = threadIdx.x; g < A.groups; g += kNormThreads) total[g] = 0.f;
+            __syncthreads();
+        }
     }
 }
 

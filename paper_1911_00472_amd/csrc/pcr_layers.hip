@@ -148,7 +148,7 @@ int pcr_group_norm_forward(int device_id, const pcr_group_norm* norm, void* d_wo
         constexpr int V = decltype(v)::value;
         in_ranges(A.images * A.chunks, kNormThreads, [&](int64_t begin, unsigned groups) {
             A.begin = begin;
-            hipLaunchKernelGGL((k_norm_sums<T, V>), dim3(groups), dim3(kNormThreads), (kNormThreads * V + 2 * A.groups) * sizeof(float), s, A);
+            hipLaunchKernelGGL((k_norm_sums<T, V>), dim3(groups), dim3(kNormThreads), norm_sums_lds(V, A.groups), s, A);
         });
         if (A.chunks > kMergedChunks)
             in_ranges((A.images * A.groups + 3) / 4, 256, [&](int64_t begin, unsigned groups) {

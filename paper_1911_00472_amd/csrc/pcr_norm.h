@@ -107,14 +107,14 @@ template <int KIND, bool ONE, int V, int N> __device__ __forceinline__ void slop
 }
 
 // Sums over a workgroup's lanes of pixels (values[lane][unit], `units` of them from `first` on) and over the `each` units of a group, added to total[group].
-// A group's team of threads adds in a fixed order, then their sums are joined; all of `threads` threads, a power of two of them, are needed.
-__device__ __forceinline__ void group_totals(const float* values, float* total, int lanes, int units, int first, int each, int groups_from, int groups_to, int thread, int threads) {
+// A group's team of threads adds in a fixed order, then their sums are joined; all of `threads` threads, a power of two of them, are needed.  S: float or double.
+template <typename S> __device__ __forceinline__ void group_totals(const S* values, S* total, int lanes, int units, int first, int each, int groups_from, int groups_to, int thread, int threads) {
     const int n = groups_to - groups_from;
     int team = 64;
     while (team > 1 && team * n > threads) team >>= 1;
     for (int g0 = 0; g0 < n; g0 += threads / team) {
         const int g = g0 + thread / team, member = thread & (team - 1);
-        float sum = 0.f;
+        S sum = 0;
         if (g < n) {
             const int c0 = max((groups_from + g) * each - first, 0), c1 = min((groups_from + g + 1) * each - first, units), width = c1 - c0;
             if (width == units) {                                  // (one group: everything)

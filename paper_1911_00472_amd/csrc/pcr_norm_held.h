@@ -56,12 +56,19 @@ template <typename T, int V, int K> __device__ __forceinline__ void hold(Held<T,
 }
 
 // MANY: a workgroup has several pictures, A.pack side by side and A.turns after one another.
-template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS) void k_norm_held(NormArgs A) {
+template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void k_norm_held(NormArgs A) {
     extern __shared__ __attribute__((aligned(16))) float shared[];
     const Slab S = slab_of(A, V);
     const int groups = S.channels / A.each;
-    float* values = shared + S.slot * S.threads * (ONE ? 1 : V);   // [lane][unit]
-    float* total = shared + THREADS * (ONE ? 1 : V) + S.slot * 3 * groups;     // [group of the block]: sums; then means; then r
+    // A sum of the values in 32 bits would leave the mean off by some roundings of it, which 1 / sqrt(eps) makes seen where they are equal or close to each other (a picture of 900.1 gave 0.02
+    // for 0).  A thread sums what its values are off its first one (of each channel, where its run has several groups), and these sums are added in 64 bits.  FIRST: what is summed is
+    // off the group's first value, which is a load more, in 32 bits (for tens of thousands of small pictures 64 bits took 9 and 15 % longer, for others 1 to 4 % longer than 32).
+    constexpr bool FIRST = ONE && MANY;
+    typedef typename std::conditional<FIRST, float, double>::type Sum;
+    float* values = shared + S.slot * S.threads * (ONE ? 2 : 2 * V);           // [lane][unit]
+    float* squares = shared + THREADS * (ONE ? 2 : 2 * V) + S.slot * 4 * groups;           // [group of the block]; then r
+    float* origin = squares + groups;                              // [group of the block]: its first value, of which the sums leave it out
+    Sum* total = (Sum*)(squares + 2 * groups);                     // [group of the block]
     const int pixels = (int)A.pixels, c = S.first + S.column * V, unit_groups = ONE ? A.each / V : A.each;
     constexpr bool EARLY = THREADS == 256;                         // (workgroups of 512 threads have registers for the parameters when the sums are made)
     float w[V], b[V];
@@ -71,14 +78,30 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
     };
     const int units = value_units<V, ONE>(S.channels);
     const float inv = 1.f / ((float)pixels * A.each);
+    const double exact_inv = 1.0 / ((double)pixels * A.each);
+    auto mean_of = [&](int g) { return FIRST ? __builtin_fmaf((float)total[g], inv, origin[g]) : (float)((double)total[g] * exact_inv); };
     for (int turn = 0;; turn++) {
         const int64_t image = S.image + turn * A.pack;
         const bool last = !MANY || turn + 1 == A.turns, there = image < A.images;
         Held<T, V> x[K];
         hold<T, V, K>(x, (const T*)A.x + min(image, A.images - 1) * A.x_image + (S.works ? c : S.first), A.x_pixel, S, pixels);
+        float from[ONE ? 1 : V], sum[V];
+        const int of = S.column * V / A.each;                      // the run's group, its first
+        if (FIRST) from[0] = (float)((const T*)A.x)[min(image, A.images - 1) * A.x_image + S.first + (S.works ? of * A.each : 0)];
         if (EARLY && turn == 0) parameters();
-        for (int g = S.thread; g < 3 * groups; g += S.threads) total[g] = 0.f;
-        float sum[V];
+        for (int g = S.thread; g < groups; g += S.threads) {
+            total[g] = 0;
+            squares[g] = 0.f;
+        }
+        if (FIRST) {
+            if (S.works && S.lane == 0 && S.column * V == of * A.each) origin[of] = from[0];
+        } else {
+            float a[V];
+            take(x[0], a);
+#pragma unroll
+            for (int i = 0; i < (ONE ? 1 : V); i++) from[i] = a[i];
+        }
+        int mine = 0;
 #pragma unroll
         for (int i = 0; i < V; i++) sum[i] = 0.f;
 #pragma unroll
@@ -87,17 +110,29 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
                 float a[V];
                 take(x[k], a);
                 if (S.lane + k * S.lanes < pixels) {
+                    mine = k + 1;
 #pragma unroll
-                    for (int i = 0; i < V; i++) sum[i] += a[i];
+                    for (int i = 0; i < V; i++) sum[i] += a[i] - from[ONE ? 0 : i];
                 }
             }
-        put_values<V, ONE>(values, S, sum);
+        if constexpr (FIRST) put_values<V, ONE>(values, S, sum);
+        else if (S.works) {
+            double* to = (double*)values + (S.lane * S.columns + S.column) * (ONE ? 1 : V);
+            if constexpr (ONE) {
+#pragma unroll
+                for (int i = 1; i < V; i++) sum[0] += sum[i];
+                to[0] = __builtin_fma((double)from[0], (double)(mine * V), (double)sum[0]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++) to[i] = __builtin_fma((double)from[i], (double)mine, (double)sum[i]);
+            }
+        }
         __syncthreads();
-        group_totals(values, total, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
+        group_totals((const Sum*)values, total, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
         __syncthreads();
         float m[ONE ? 1 : V];
 #pragma unroll
-        for (int i = 0; i < (ONE ? 1 : V); i++) m[i] = S.works ? total[(S.column * V + i) / A.each] * inv : 0.f;
+        for (int i = 0; i < (ONE ? 1 : V); i++) m[i] = S.works ? mean_of((S.column * V + i) / A.each) : 0.f;
 #pragma unroll
         for (int i = 0; i < V; i++) sum[i] = 0.f;
 #pragma unroll
@@ -115,20 +150,20 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
             }
         put_values<V, ONE>(values, S, sum);
         __syncthreads();
-        group_totals(values, total + groups, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
+        group_totals(values, squares, S.lanes, units, 0, unit_groups, 0, groups, S.thread, S.threads);
         __syncthreads();
         for (int g = S.thread; g < groups; g += S.threads) {
-            const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(total[groups + g], inv, A.eps));
-            total[2 * groups + g] = r;
+            const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(squares[g], inv, A.eps));
+            squares[g] = r;
             float2* to = (float2*)A.stats + image * A.groups + S.first / A.each + g;
-            if (there) *to = make_float2(total[g] * inv, r);
+            if (there) *to = make_float2(mean_of(g), r);
         }
         __syncthreads();
         if (S.works && there) {
             float by[V];
             if (!EARLY) parameters();
 #pragma unroll
-            for (int i = 0; i < V; i++) by[i] = w[i] * total[2 * groups + (S.column * V + i) / A.each];
+            for (int i = 0; i < V; i++) by[i] = w[i] * squares[(S.column * V + i) / A.each];
             T* out = (T*)A.out + image * A.out_image + c;
             with_kind(A.activation, [&](auto kind) {
 #pragma unroll
@@ -275,8 +310,7 @@ template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, N
             constexpr bool ONE = decltype(in_one)::value, MANY = decltype(of_many)::value;
             ok = ok && P.held == K && P.threads == THREADS && P.many == MANY && P.holds(N->pixels);
             if (!ok) return;
-            const size_t groups = A.block / A.each, values = THREADS * (ONE ? 1 : V);
-            const size_t lds = (BACK ? std::max(2 * values + A.pack * 2 * groups, (size_t)THREADS * V + A.block) : values + A.pack * 3 * groups) * sizeof(float);
+            const size_t lds = P.lds(A.each, BACK);
             in_ranges(P.rows * A.blocks, THREADS, [&](int64_t begin, unsigned workgroups) {
                 A.begin = begin;
                 if constexpr (BACK) {

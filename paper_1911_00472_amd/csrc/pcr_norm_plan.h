@@ -23,6 +23,11 @@ struct NormPlan {
     int64_t rows;                                                  // of channels' sums
     size_t part_bytes, sums_bytes, joined_bytes;
     size_t bytes() const { return part_bytes + sums_bytes + joined_bytes; }
+    // LDS of a workgroup of one pass, in bytes; each: channels of a group.  (Forward: sums of 64 bits, and 16 bytes of a group.)
+    size_t lds(int64_t each, bool back) const {
+        const size_t groups = block / each, values = (size_t)threads * (each % run ? run : 1);
+        return (back ? std::max(2 * values + pack * 2 * groups, (size_t)threads * run + block) : values * 2 + pack * 4 * groups) * sizeof(float);
+    }
     // Whether the threads of a picture's part hold all of its pixels: lanes of a run of channels (rounded down), times what a thread holds.
     bool holds(int64_t pixels) const { return held && block && threads / pack / (block / run) * (int64_t)held >= pixels; }
 };

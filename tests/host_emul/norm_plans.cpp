@@ -28,11 +28,9 @@ static void look(int dtype, int64_t images, int64_t pixels, int64_t channels, in
         // what is launched: runs that a thread holds, and threads
         const bool whole = P.run * size == 16;
         ok = ok && (P.many ? P.threads == 256 && P.held == (whole ? 1 : 2) : P.threads == 256 ? P.held == (whole ? 4 : 8) : P.threads == 512 && whole && (P.held == 8 || (P.held == 16 && !back)));
-        // LDS as the launches ask for it
-        const bool one = each % P.run == 0;
-        const int64_t values = P.threads * (one ? 1 : P.run), of_block = P.block / each;
-        const int64_t floats = back ? std::max(2 * values + P.pack * 2 * of_block, (int64_t)P.threads * P.run + P.block) : values + P.pack * 3 * of_block;
-        ok = ok && floats * 4 <= 160 * 1024;
+        // what its kernels put into LDS
+        const int64_t values = P.threads * (each % P.run == 0 ? 1 : P.run), of_block = P.block / each, lds = P.lds(each, back);
+        ok = ok && lds >= (back ? 8 * (values + P.pack * of_block) : 8 * values + 16 * P.pack * of_block) && (!back || lds >= 4 * ((int64_t)P.threads * P.run + P.block)) && lds <= 160 * 1024;
     } else {
         counts[2]++;
         ok = ok && P.chunk >= 1 && P.chunks >= 1 && P.chunk * P.chunks >= pixels && P.chunk * (P.chunks - 1) < pixels && P.rows == images * P.chunks;
