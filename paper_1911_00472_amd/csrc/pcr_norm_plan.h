@@ -11,6 +11,7 @@ namespace pcr {
 
 constexpr int kNormThreads = 256;                                  // of two passes
 constexpr int kNormTogether = 4;                                   // pixels of a thread whose loads are under way together
+constexpr int kNormLong = 512;                                     // pixels that a thread adds up one after another, at most: in 32 bits its sums are off by 2^-16 of the magnitudes then
 constexpr int kMergedChunks = 64;                                  // so many of a picture's chunks are joined by every workgroup that needs them
 
 // What a call is made of.
@@ -91,7 +92,7 @@ inline NormPlan plan_norm(const pcr_group_norm* N, bool back) {
     // 112 x 112 x 64 59.8 / 57.9 / 59.3 / 64.6, gradient of 64 of 56 x 56 x 256 99 / 105 / 107 / 113, of 32 of 112 x 112 x 64 57 / 62 / 66 / 66.)
     const int64_t columns = std::min<int64_t>(N->channels / P.run, kNormThreads), lanes = kNormThreads / columns, step = kNormTogether * lanes;
     int64_t chunks = std::min<int64_t>(((back ? 512 : 768) + N->images - 1) / std::max<int64_t>(1, N->images), (N->pixels + 4 * step - 1) / (4 * step));
-    chunks = std::max<int64_t>(1, chunks);
+    chunks = std::max(std::max<int64_t>(1, chunks), std::min<int64_t>((N->pixels + kNormLong * lanes - 1) / (kNormLong * lanes), 1 << 30));
     P.chunk = ((N->pixels + chunks - 1) / chunks + step - 1) / step * step;
     P.chunks = N->pixels ? (int)((N->pixels + P.chunk - 1) / P.chunk) : 0;
     P.part_bytes = (size_t)N->images * P.chunks * N->groups * 2 * sizeof(float);

@@ -35,6 +35,8 @@ static void look(int dtype, int64_t images, int64_t pixels, int64_t channels, in
         counts[2]++;
         ok = ok && P.chunk >= 1 && P.chunks >= 1 && P.chunk * P.chunks >= pixels && P.chunk * (P.chunks - 1) < pixels && P.rows == images * P.chunks;
         ok = ok && P.part_bytes == (size_t)(images * P.chunks * groups * 8);
+        // what a thread adds up one after another: the chunk's pixels over the lanes of a column
+        ok = ok && P.chunk <= 512 * (256 / std::min<int64_t>(channels / P.run, 256));
     }
     ok = ok && P.sums_bytes == (back ? (size_t)P.rows * channels * 8 : 0);
     if (!ok && bad++ < 20)
@@ -44,7 +46,7 @@ static void look(int dtype, int64_t images, int64_t pixels, int64_t channels, in
 
 int main() {
     const int64_t images[] = {1, 7, 300, 2047, 2048, 4096, 10000, 100000};
-    const int64_t wide[] = {1, 2, 3, 5, 6, 8, 9, 12, 16, 23, 31, 33, 49, 64, 85, 100, 128, 196, 256, 300, 511, 700, 1024, 3136, 12544, 50000};
+    const int64_t wide[] = {1, 2, 3, 5, 6, 8, 9, 12, 16, 23, 31, 33, 49, 64, 85, 100, 128, 196, 256, 300, 511, 700, 1024, 3136, 12544, 50000, 3000000};
     for (int dtype = 0; dtype < 3; dtype++)
         for (int back = 0; back < 2; back++)
             for (int64_t n : images) {
