@@ -210,7 +210,7 @@ template <typename T, int V, bool ONE> __global__ __launch_bounds__(256) void k_
             auto one = [&](int64_t p, float (&a)[V]) {
 #pragma unroll
                 for (int i = 0; i < V; i++) a[i] = __builtin_fmaf(a[i] - m[ONE ? 0 : i], w[i], b[i]);
-                activate<decltype(kind)::value>(a);
+                activate<T, decltype(kind)::value>(a);
                 store_run<T, V>(out + p * A.out_pixel + c, a);
             };
             through(K, C, [&](int64_t p) {
@@ -264,7 +264,7 @@ template <typename T, int V, bool ONE> __global__ __launch_bounds__(256) void k_
             }
             with_kind(A.activation, [&](auto kind) {
                 auto one = [&](float (&a)[V], float (&h)[V]) {
-                    slopes<decltype(kind)::value, ONE>(a, h, m, r, w, b);
+                    slopes<T, decltype(kind)::value, ONE>(a, h, m, r, w, b);
 #pragma unroll
                     for (int i = 0; i < V; i++) {
                         s[0][i] = __builtin_fmaf(h[i], a[i], s[0][i]);
@@ -353,7 +353,7 @@ template <typename T, int V, bool ONE> __global__ __launch_bounds__(256) void k_
         }
         with_kind(A.activation, [&](auto kind) {
             auto one = [&](int64_t p, float (&a)[V], float (&h)[V]) {
-                slopes<decltype(kind)::value, ONE>(a, h, m, r, w, b);
+                slopes<T, decltype(kind)::value, ONE>(a, h, m, r, w, b);
 #pragma unroll
                 for (int i = 0; i < V; i++) a[i] = r[ONE ? 0 : i] * (__builtin_fmaf(h[i], w[i], -s[ONE ? 0 : i]) - a[i] * t[ONE ? 0 : i]);
                 store_run<T, V>(out + p * A.out_pixel + c, a);

@@ -174,7 +174,7 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
                         take(x[k], a);
 #pragma unroll
                         for (int i = 0; i < V; i++) a[i] = __builtin_fmaf(a[i] - m[ONE ? 0 : i], by[i], b[i]);
-                        activate<decltype(kind)::value>(a);
+                        activate<T, decltype(kind)::value>(a);
                         store_run<T, V>(out + (int64_t)p * A.out_pixel, a);
                     }
                     one_after_another();
@@ -223,7 +223,7 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
                     float a[V], g[V];
                     take(x[k], a);
                     take(h[k], g);
-                    slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
+                    slopes<T, decltype(kind)::value, ONE>(a, g, m, r, w, b);
                     if (S.lane + k * S.lanes < pixels) {
 #pragma unroll
                         for (int i = 0; i < V; i++) {
@@ -266,7 +266,7 @@ template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__
                         float a[V], g[V];
                         take(x[k], a);
                         take(h[k], g);
-                        slopes<decltype(kind)::value, ONE>(a, g, m, r, w, b);
+                        slopes<T, decltype(kind)::value, ONE>(a, g, m, r, w, b);
 #pragma unroll
                         for (int i = 0; i < V; i++) {
                             const int j = ONE ? 0 : i;
