@@ -56,7 +56,7 @@ template <typename T, int V, int K> __device__ __forceinline__ void hold(Held<T,
 }
 
 // MANY: a workgroup has several pictures, A.pack side by side and A.turns after one another.
-template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void k_norm_held(NormArgs A) {
+template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS, THREADS == 512 && ONE ? 4 : 1) void k_norm_held(NormArgs A) {
     extern __shared__ __attribute__((aligned(16))) float shared[];
     const Slab S = slab_of(A, V);
     const int groups = S.channels / A.each;
