@@ -7,7 +7,9 @@ by the native module _train (csrc/pcr_bind.cpp).  A tensor on another stream tha
 record_stream, as with any operator.  Wrong types, shapes or devices raise ValueError before anything is enqueued, what the library
 refuses raises PcrError.  rotate_axes, norm_rotate, distill_loss, group_norm, position_bias and dropout take part in automatic differentiation; a gradient is made on the
 stream of its forward pass.  There are no derivatives of forward mode (ValueError), and no traces (RuntimeError)."""
+import math
 import os
+from decimal import Decimal, localcontext
 
 import numpy as np
 import torch
@@ -234,12 +236,31 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation=None, str
 
 # ---- position bias ----
 
+def _borders(e, c, f):
+    """Where the coarse buckets 1 .. c - 1 of a side begin: the first distance x of x^c >= e^(c - j) f^j, which is found in 64-bit floats wherever they tell."""
+    j = np.arange(1, c)
+    at = e * (f / e) ** (j / c)                                # (to 2^-47 of itself)
+    border = np.ceil(at).astype(np.int64)
+    near = np.rint(at)
+    for i in np.nonzero(np.abs(at - near) < 2.0 ** -40 * at)[0].tolist():
+        x, g = int(near[i]), math.gcd(i + 1, c)
+        p, q = (i + 1) // g, c // g
+        # x = e (f / e)^(p / q) only with a q-th root of f / e that is a fraction of whole numbers below 2^25: q is 24 at most
+        if q <= 24:
+            border[i] = x if x ** q >= e ** (q - p) * f ** p else x + 1
+        else:
+            with localcontext() as precise:
+                precise.prec = 60
+                border[i] = x if q * Decimal(x).ln() >= (q - p) * Decimal(e).ln() + p * Decimal(f).ln() else x + 1
+    return border
+
+
 def position_buckets(exact, coarse=0, far=0, one_sided=False, device=0):
     """(buckets int32 [axes, 2 * reach + 1], their number) for position_bias.  On either side of an axis the distances below `exact` (0 among them) have a bucket each, those
     from `exact` to `far` share `coarse` buckets whose widths grow by a constant factor, and the last bucket takes all that is farther; one_sided: keys ahead of their query
     count as distance 0.  An axis' buckets follow each other from the farthest behind to the farthest ahead (one_sided: from distance 0 on), and those of several axes
     are combined with the last axis' together.  exact, coarse, far: numbers, or one for each axis: position_buckets((8, 8)) gives a bucket to every difference in a
-    window of 8 x 8, position_buckets(8, 8, 128) is 31 buckets for one line of tokens."""
+    window of 8 x 8, position_buckets(8, 8, 128) is 31 buckets for one line of tokens.  Distances up to 2^24 and up to 2^24 buckets in all."""
     axes = max(len(v) if isinstance(v, (tuple, list)) else 1 for v in (exact, coarse, far))
     exact, coarse, far = ([int(n) for n in v] if isinstance(v, (tuple, list)) else [int(v)] * axes for v in (exact, coarse, far))
     if not len(exact) == len(coarse) == len(far) == axes or not 1 <= axes <= 4:
@@ -247,22 +268,21 @@ def position_buckets(exact, coarse=0, far=0, one_sided=False, device=0):
     if any(e < 1 or c < 0 or (c and f <= e) for e, c, f in zip(exact, coarse, far)):
         raise ValueError("exact at least 1, coarse at least 0, and far above exact where there are coarse buckets, are wanted")
     reach = max(f if c else e - 1 for e, c, f in zip(exact, coarse, far))
-    rows, count = [], 1
-    for e, c, f in reversed(list(zip(exact, coarse, far))):
-        # bucket e + j of a side begins at the first distance x of x^c >= e^(c - j) f^j
-        side, j = [], 0
-        for x in range(reach + 1):
-            while j + 1 < c and x ** c >= e ** (c - j - 1) * f ** (j + 1):
-                j += 1
-            side.append(x if x < e else e + j if c else e - 1)
+    sides = [e + c if one_sided else 2 * (e + c) - 1 for e, c in zip(exact, coarse)]
+    count = math.prod(sides)
+    if reach > 2 ** 24 or count > 2 ** 24:                     # (what the library takes)
+        raise ValueError("distances up to 2^24 and up to 2^24 buckets are wanted")
+    rows, above = [], 1
+    for e, c, f, n in reversed(list(zip(exact, coarse, far, sides))):
+        borders = _borders(e, c, f) if c else np.empty(0, np.int64)
+        x = np.arange(reach + 1)
+        side = np.where(x < e, x, e + np.searchsorted(borders, x, side="right") if c else e - 1)
         last = e + c - 1
-        row = side[:0:-1] + [0] * (reach + 1) if one_sided else [last - b for b in side[:0:-1]] + [last + b for b in side]
-        rows.append(np.asarray(row, np.int64) * count)
-        count *= e + c if one_sided else 2 * last + 1
-    if count > 2 ** 24:
-        raise ValueError("more than 2^24 buckets")
+        row = np.concatenate([side[:0:-1], np.zeros(reach + 1, np.int64)] if one_sided else [last - side[:0:-1], last + side])
+        rows.append((row * above).astype(np.int32))
+        above *= n
     dev = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
-    return torch.from_numpy(np.stack(rows[::-1]).astype(np.int32)).to(dev), count
+    return torch.from_numpy(np.stack(rows[::-1])).to(dev), count
 
 
 class _PositionBias(torch.autograd.Function):
