@@ -602,7 +602,8 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
  *   values       dtype, with strides of batch, heads and queries, keys contiguous: the bias, written; of the backward pass its gradient, read
  * pcr_position_bias_backward: table_grad float [bucket][head]: the sum of the gradient over the pairs of each bucket, in a fixed order; pairs that have no
  *   bias add nothing, whatever their gradient holds.  Sums are held in 64 bits, those of shares of the pairs rounded to 32 in between.
- *   d_work: pcr_position_bias_workspace bytes (2 for every pair of tokens, and the shares' sums). */
+ *   d_work: pcr_position_bias_workspace bytes: for every query 16 (and a bit) for each 8 keys or part of them, and the shares' sums of all heads and buckets, of which there are
+ *   as many as work beside each other and 4 GiB hold (one share's are table_grad itself). */
 typedef struct pcr_places {
     const void* position; int64_t axis_stride, batch_stride, token_stride;
     const int32_t* segment; int64_t segment_batch_stride, segment_token_stride;

@@ -45,6 +45,7 @@ NormArgs norm_args(const pcr_group_norm* N, const NormPlan& P, void* d_work) {
 
 constexpr int64_t kBiasLds = 152 * 1024;                         // of a workgroup, at most
 constexpr size_t kBiasTwo = 80 * 1024;                           // where two share a compute unit
+constexpr size_t kBiasParts = 4ull << 30;                        // bytes of the shares' sums of a gradient, at most
 
 int check_bias(const pcr_position_table* t, bool back) {
     if (!t || !known_type(t->dtype)) return PCR_E_ARG;
@@ -110,7 +111,8 @@ BiasPlan plan_bias(const pcr_position_table* t) {
     P.lds = (size_t)bytes(P.waves);
     const int64_t head_blocks = std::max<int64_t>(1, (t->heads + P.waves - 1) / P.waves);
     const int64_t resident = 256 * std::max<int64_t>(1, std::min<int64_t>(16 / P.waves, (int64_t)(160 * 1024 / P.lds)));
-    P.shares = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most_shares, steps), resident / head_blocks));
+    P.shares = std::min<int64_t>(std::min<int64_t>(most_shares, steps), std::min<int64_t>(resident / head_blocks, (int64_t)(kBiasParts / std::max<size_t>(1, sums))));
+    P.shares = std::max<int64_t>(1, P.shares);
     P.live_bytes = (size_t)(blocks + 1) / 2 * 2 * 8;
     P.part_bytes = P.shares == 1 ? 0 : (size_t)P.shares * sums;
     return P;
