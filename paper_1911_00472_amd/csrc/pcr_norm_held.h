@@ -327,7 +327,7 @@ template <bool BACK> bool run_held(const pcr_group_norm* N, const NormPlan& P, N
             else if constexpr (V > 1) launch(k, threads, std::false_type(), of_many);
         };
         constexpr bool WHOLE = V * sizeof(T) == 16;
-        if (P.many) by_one(Int<WHOLE ? 1 : 2>(), Int<256>(), std::true_type());
+        if (P.many) by_one(Int<WHOLE ? 1 : 3>(), Int<256>(), std::true_type());
         else if (P.threads == 256) by_one(Int<WHOLE ? 4 : 8>(), Int<256>(), std::false_type());
         else if constexpr (WHOLE) {
             if (P.held <= 8) by_one(Int<8>(), Int<512>(), std::false_type());

@@ -58,20 +58,21 @@ inline NormPlan plan_norm(const pcr_group_norm* N, bool back) {
         const int64_t of_unit = N->pixels * (unit / P.run);
         while (many > 1 && of_unit * many > most) many >>= 1;
         many = std::min(many, units);
-        // Many small pictures: where the threads of a workgroup hold a picture with one run each (two of fewer than 16 bytes), it has whole ones, side by side and after one another,
+        // Many small pictures: where a picture has no more runs than a workgroup has threads (twice as many of fewer than 16 bytes), it has whole ones, side by side and after one another,
         // whose channels' sums are one row.  (us, with a picture or 128 bytes of its channels to a workgroup: 32768 of a pixel of 1024 channels 114, now 66, their gradient 440, 90;
         // 100000 of 2 x 2 x 32 324, 29, and 788, 46.)
         auto need = [&](int64_t threads, int64_t columns) { return (N->pixels + threads / columns - 1) / (threads / columns); };     // (lanes of a column are whole: 100 columns leave 56 threads of 256 without work)
         const bool whole = P.run * size == 16;
         const int64_t runs_held = whole ? 1 : 2;
-        P.many = N->images >= kSmallImages && units * unit / P.run <= 256 && need(256, units * unit / P.run) <= runs_held;
+        P.many = N->images >= kSmallImages && units * unit / P.run <= 256 && of_unit * units <= 256 * runs_held;
         if (P.many) many = units;
         const int64_t columns = many * unit / P.run;
         if (of_unit * many <= most && columns <= 256) {
             P.block = (int)(many * unit);
             P.blocks = (int)((units + many - 1) / many);
             P.threads = !whole || need(256, columns) <= 4 ? 256 : 512;
-            P.held = P.many ? (int)runs_held : !whole ? 8 : P.threads == 256 ? 4 : back || need(512, columns) <= 8 ? 8 : 16;
+            // (512 runs of a picture are three of a thread where a pixel's runs do not divide the threads: 2 x 256 / 54 pixels of 54 runs on 4 lanes.)
+            P.held = P.many ? (whole ? 1 : 3) : !whole ? 8 : P.threads == 256 ? 4 : back || need(512, columns) <= 8 ? 8 : 16;
             P.pack = 1;
             if (P.many)
                 while (N->images >= 2 * P.pack * kSmallImages && 128 / P.pack >= columns && need(128 / P.pack, columns) <= runs_held) P.pack *= 2;

@@ -27,7 +27,7 @@ static void look(int dtype, int64_t images, int64_t pixels, int64_t channels, in
         ok = ok && (P.many ? P.blocks == 1 : P.pack == 1 && P.turns == 1);
         // what is launched: runs that a thread holds, and threads
         const bool whole = P.run * size == 16;
-        ok = ok && (P.many ? P.threads == 256 && P.held == (whole ? 1 : 2) : P.threads == 256 ? P.held == (whole ? 4 : 8) : P.threads == 512 && whole && (P.held == 8 || (P.held == 16 && !back)));
+        ok = ok && (P.many ? P.threads == 256 && P.held == (whole ? 1 : 3) : P.threads == 256 ? P.held == (whole ? 4 : 8) : P.threads == 512 && whole && (P.held == 8 || (P.held == 16 && !back)));
         // what its kernels put into LDS
         const int64_t values = P.threads * (each % P.run == 0 ? 1 : P.run), of_block = P.block / each, lds = P.lds(each, back);
         ok = ok && lds >= (back ? 8 * (values + P.pack * of_block) : 8 * values + 16 * P.pack * of_block) && (!back || lds >= 4 * ((int64_t)P.threads * P.run + P.block)) && lds <= 160 * 1024;
