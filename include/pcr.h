@@ -600,8 +600,9 @@ int pcr_group_norm_backward(int device_id, const pcr_group_norm* norm, void* d_w
  *   map          int32 [axes][2 reach + 1]; axes 1 .. 4, reach 0 .. 2^24;  buckets 1 .. 2^24, heads up to 65535
  *   table        [bucket][head] of table_dtype (float, or dtype)
  *   values       dtype, with strides of batch, heads and queries, keys contiguous: the bias, written; of the backward pass its gradient, read
- * pcr_position_bias_backward: table_grad float [bucket][head]: the sum of the gradient over the pairs of each bucket, in a fixed order; pairs that have no
- *   bias add nothing, whatever their gradient holds.  Sums are held in 64 bits, those of shares of the pairs rounded to 32 in between.
+ * pcr_position_bias_backward: table_grad float [bucket][head]: the sum of the gradient over the pairs of each bucket; pairs that have no
+ *   bias add nothing, whatever their gradient holds.  Sums are held in 64 bits, those of shares of the pairs rounded to 32 in between.  The order of additions is fixed but for pairs
+ *   of a bucket that a wavefront adds in one instruction: these follow the LDS unit, whose order no document promises (sums that 64 bits hold exactly, as most are, do not depend on it).
  *   d_work: pcr_position_bias_workspace bytes: for every query 16 (and a bit) for each 8 keys or part of them, and the shares' sums of all heads and buckets, of which there are
  *   as many as work beside each other and 4 GiB hold (one share's are table_grad itself). */
 typedef struct pcr_places {

@@ -292,7 +292,8 @@ template <typename T> struct Eight {
 };
 
 // A wavefront has a share and a head, and bins for that in LDS, in 64 bits, which are its own: they are added to in the order of its instructions, and lanes
-// of one instruction that meet in a bin in the order in which the LDS unit takes lanes of the same address, which nothing else has a part in.  Where there are few buckets
+// of one instruction that meet in a bin in the order in which the LDS unit takes lanes of the same address: nothing else has a part in it and it has been the same at every call, but no
+// document promises it.  (It shows only in sums that 64 bits do not hold exactly.)  Where there are few buckets
 // there are several copies of the bins, for the lanes in turn, so that few meet.
 // (LDS adds floats of 64 bits in 9 clocks a wavefront's instruction, those of 32 in 193: the long sequence took 1063 us with these.  Sums of up to 64 buckets as matrix products, each
 // pair a row with a one at its bucket, took 94 to 99 % of this kernel's time with 8 and more heads and 120 to 200 % with fewer: both wait for memory.  Six or eight items under way

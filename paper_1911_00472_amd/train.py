@@ -314,8 +314,8 @@ def position_bias(table, positions, buckets, key_positions=None, segments=None, 
 
 
 def position_bias_backward(grad, positions, buckets, count, key_positions=None, segments=None, key_segments=None, stream=None):
-    """Gradient of position_bias's table: float32 [count, heads], the sum of grad over the pairs of each bucket, in a fixed order.  What grad holds of pairs without a
-    bias (of different segments, of padding) is not looked at."""
+    """Gradient of position_bias's table: float32 [count, heads], the sum of grad over the pairs of each bucket, in 64 bits, whose order is fixed as far as the GPU's own is
+    (include/pcr.h).  What grad holds of pairs without a bias (of different segments, of padding) is not looked at."""
     return _call(stream, _train.position_bias_backward, grad, positions, buckets, count, key_positions, segments, key_segments)
 
 
