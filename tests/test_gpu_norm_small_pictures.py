@@ -1,4 +1,5 @@
 """Group norm of thousands of small pictures whose runs of channels do not divide a workgroup's threads: no pixel of a picture is left out, of its statistics or of what is written."""
+import numpy as np
 import pytest
 import torch
 
@@ -26,3 +27,22 @@ def test_small_pictures_are_held_whole(pixels, C, G, images, dtype):
     g = torch.randn(x.shape, generator=gen, device="cuda").to(dtype)
     dx = torch.full_like(x, float("nan"))
     norm.check_backward(g, x, G, w, b, stats, kind, *pkg.group_norm_backward(g, x, G, w, b, stats, kind, dx=dx))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_small_pictures_drawn_by_chance(seed):
+    rng = np.random.default_rng(500 + seed)
+    for _ in range(4):
+        C = int(2 ** rng.uniform(0, 10.5))
+        G = int(rng.choice([g for g in range(1, min(C, 64) + 1) if C % g == 0]))
+        pixels = int(max(1, min(2 ** rng.uniform(0, 7), 1200 / C)))
+        images = int(min(rng.integers(2048, 20000), 6e6 // (C * pixels)))
+        dtype, kind, pad = norm.TYPES[rng.integers(3)], norm.ACTIVATIONS[rng.integers(4)], int(rng.integers(0, 5)) if rng.random() < 0.3 else 0
+        print(images, pixels, C, G, dtype, kind, pad, flush=True)
+        gen = norm.generator(seed)
+        x, out, dx = (norm.make((images, pixels, C + pad), dtype, gen)[..., pad:] for _ in range(3))
+        w, b = (torch.randn(C, generator=gen, device="cuda") for _ in range(2))
+        y, stats = pkg.group_norm_forward(x, G, w, b, EPS, kind, out=out.fill_(float("nan")))
+        norm.check_forward(x, G, w, b, EPS, kind, y, stats)
+        g = torch.randn(x.shape, generator=gen, device="cuda").to(dtype)
+        norm.check_backward(g, x, G, w, b, stats, kind, *pkg.group_norm_backward(g, x, G, w, b, stats, kind, dx=dx.fill_(float("nan"))))
