@@ -1,9 +1,11 @@
 // Group norm and its gradient in two passes.
 //
 // Larger pictures are gone through twice, chunk by chunk of their pixels: sums of every chunk, then what is written; what the second pass reads mostly comes out of the
-// memory-side cache.  Loads of four pixels are under way together, without conditions about them (behind which the compiler would wait for those before).
-// Bound by memory.  us: 64 pictures of 112 x 112 x 64, bfloat, sums 32 (103 MB, 3.2 TB/s; 26 where x is in the cache), result 39 (206 MB, 5.3 TB/s); gradient of 64 of 56 x 56 x 256 sums 57
-// (206 MB, 3.6 TB/s), result 55 (308 MB, 5.6 TB/s), sums of the weights' gradients 5.
+// memory-side cache.  (More than 256 runs of channels, 2048 of 16 bits, three times: the sums hold one block of columns in registers, and go through several twice.  us: 8 of
+// 112 x 112 x 2048 261, x 2304 368.)  Loads of four pixels are under way together, without conditions about them (behind which the compiler would wait for those before).
+// Results are bound by memory; sums by what follows each other in a thread, four loads, a wait for them, the running means.  us: 64 pictures of 112 x 112 x 64, bfloat, sums 32
+// (103 MB, 3.2 TB/s; 26 where x is in the cache), result 39 (206 MB, 5.3 TB/s); gradient of 64 of 56 x 56 x 256 sums 57 (206 MB, 3.6 TB/s), result 55 (308 MB, 5.6 TB/s), sums of the
+// weights' gradients 5.
 #pragma once
 #include "pcr_norm.h"
 

@@ -8,7 +8,7 @@ namespace pcr {
 
 // Where the pixels of a picture with a few groups' channels fit into the registers of a workgroup, it reads them once: the mean, then the squares around it, are
 // summed from registers, and what is written is made from them.  A thread has a run of V channels of every few pixels; block: channels of a workgroup, whole groups and whole
-// runs.  us: 64 pictures of 14 x 14 x 256, bfloat 8.3 (2.6 at 5.0 TB/s), the gradient 15 (3.9), one of 14 x 14 x 64 5.7: the launch, and loads, sums and stores of a workgroup, which
+// runs.  us: 64 pictures of 14 x 14 x 256, bfloat 8.6 (2.6 at 5.0 TB/s), the gradient 16 (3.9), one of 14 x 14 x 64 6.0: the launch, and loads, sums and stores of a workgroup, which
 // follow each other, bound it.  The workgroups of a picture run on one die (blockIdx modulo 8 goes round the dies), where they find in its cache what lies beside their own channels in a line.
 struct Slab {
     int64_t image, row;                                            // the first of the thread's pictures; where its workgroup's sums go
@@ -55,14 +55,15 @@ template <typename T, int V, int K> __device__ __forceinline__ void hold(Held<T,
         if (k * S.lanes < pixels) h[k].v = reinterpret_cast<const typename Run<T, V>::Loose*>(from + (int64_t)min(S.lane + k * S.lanes, pixels - 1) * pixel)->v;
 }
 
-// MANY: a workgroup has several pictures, A.pack side by side and A.turns after one another.
+// MANY: a workgroup has several pictures, A.pack side by side and A.turns after one another.  Workgroups of 512 threads have 128 registers, so that two fit a compute unit, where that takes no
+// scratch memory (32 pictures of 56 x 56 x 256 41 us with one, 33 with two).
 template <typename T, int V, int K, int THREADS, bool ONE, bool MANY> __global__ __launch_bounds__(THREADS, THREADS == 512 && ONE ? 4 : 1) void k_norm_held(NormArgs A) {
     extern __shared__ __attribute__((aligned(16))) float shared[];
     const Slab S = slab_of(A, V);
     const int groups = S.channels / A.each;
     // A sum of the values in 32 bits would leave the mean off by some roundings of it, which 1 / sqrt(eps) makes seen where they are equal or close to each other (a picture of 900.1 gave 0.02
     // for 0).  A thread sums what its values are off its first one (of each channel, where its run has several groups), and these sums are added in 64 bits.  FIRST: what is summed is
-    // off the group's first value, which is a load more, in 32 bits (for tens of thousands of small pictures 64 bits took 9 and 15 % longer, for others 1 to 4 % longer than 32).
+    // off the group's first value, which is a load more, in 32 bits (for tens of thousands of small pictures 64 bits took 9 and 15 % longer, for others 1 to 5 % longer than sums of the values in 32).
     constexpr bool FIRST = ONE && MANY;
     typedef typename std::conditional<FIRST, float, double>::type Sum;
     float* values = shared + S.slot * S.threads * (ONE ? 2 : 2 * V);           // [lane][unit]

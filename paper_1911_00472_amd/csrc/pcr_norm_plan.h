@@ -59,8 +59,8 @@ inline NormPlan plan_norm(const pcr_group_norm* N, bool back) {
         while (many > 1 && of_unit * many > most) many >>= 1;
         many = std::min(many, units);
         // Many small pictures: where a picture has no more runs than a workgroup has threads (twice as many of fewer than 16 bytes), it has whole ones, side by side and after one another,
-        // whose channels' sums are one row.  (us, with a picture or 128 bytes of its channels to a workgroup: 32768 of a pixel of 1024 channels 114, now 66, their gradient 440, 90;
-        // 100000 of 2 x 2 x 32 324, 29, and 788, 46.)
+        // whose channels' sums are one row.  (us, with a picture or 128 bytes of its channels to a workgroup: 32768 of a pixel of 1024 channels 114, now 67, their gradient 440, 101;
+        // 100000 of 2 x 2 x 32 324, 30, and 788, 46; 30000 of 3 x 3 x 108 285, 120, and 422, 178.)
         auto need = [&](int64_t threads, int64_t columns) { return (N->pixels + threads / columns - 1) / (threads / columns); };     // (lanes of a column are whole: 100 columns leave 56 threads of 256 without work)
         const bool whole = P.run * size == 16;
         const int64_t runs_held = whole ? 1 : 2;
@@ -78,7 +78,8 @@ inline NormPlan plan_norm(const pcr_group_norm* N, bool back) {
                 while (N->images >= 2 * P.pack * kSmallImages && 128 / P.pack >= columns && need(128 / P.pack, columns) <= runs_held) P.pack *= 2;
             if (!P.holds(N->pixels)) P.held = 0;
             P.turns = P.many ? (int)std::min<int64_t>(16, std::max<int64_t>(1, N->images / (P.pack * kSmallImages))) : 1;
-            // (Rows of 16 bytes: 64 pictures of 56 x 56 x 256 take 66 us, and 65 in two passes; their gradient 201, and 113.)
+            // Rows of 16 bytes of more than the caches hold.  (us in one pass / in two, runs of 8 channels and 4 of 32 bits: 64 pictures of 56 x 56 x 256 72 / 72 and their gradient 213 / 115;
+            // 64 of 56 x 56 x 512 126 / 126 and 413 / 229; 96 of 60 x 60 x 192 88 / 88 and 272 / 171; 60 of 72 x 72 x 128 145 / 49 and 108 / 108; 32 bits, 64 of 56 x 56 x 128 68 / 68 and 138 / 110.)
             if (P.block < N->channels && P.block * (int64_t)size < 32 && N->images * N->pixels * N->channels * (int64_t)size > (64 << 20)) P.held = 0;
         }
     }
