@@ -34,7 +34,8 @@ struct NormArgs {
 // What runs become is computed one after another: side by side their intermediate values would take the registers of whole wavefronts (168 and spills for 90 in the gradient's sums).
 __device__ __forceinline__ void one_after_another() { __builtin_amdgcn_sched_barrier(0); }
 
-// T: the type of the values that a result is rounded to.  Those of 16 bits, which round to 2^-9 and 2^-12 of themselves, take the shorter forms.
+// T: the type of values and results.  Those of 16 bits, which round to 2^-9 and 2^-12 of themselves, take the shorter forms (so do the gradients of weight and bias beside them, which are of 32 bits: sums
+// of gradients that were rounded to 16).
 template <typename T> constexpr bool kFull = sizeof(T) == 4;
 // exp(-v), and 1 / v to a unit or two in the last place: a division has ten instructions.  The exponential's argument is rounded, which leaves |v| 2^-24 of it; in 32 bits that is made good (of v
 // between -104 and 104, where it is infinite and 0).  In place of the library's exponential, error function and division, with which 32 of 56 x 56 x 128 in 32 bits took 27 us (SiLU) and 36 (GELU): 23 and 28.
